@@ -222,6 +222,118 @@ const float* tm_schedule_tail(const float* schedule, int rows, int iters);
 tm_status tm_orthogonalize_noalloc(void* X, int64_t m, int64_t n, int64_t batch, int iters,
                                    const float* coeffs, int precond, void* stream);
 
+/* ------------------------------------------------------------------ operators
+ * What a training step needs around the optimizer: layer norm, products of
+ * ragged groups of rows with one matrix per expert (whose weight gradients are
+ * the matrices that tm_muon_step_grouped takes) and the clipped policy loss
+ * with its gradient.  Matrices are row-major with a stride between rows (in
+ * elements, at least the width); pointers are aligned to their element only,
+ * though 16-byte alignment and strides are faster.  `dtype` is the type of the
+ * activations; parameters, statistics and sums are fp32.  Streams, errors,
+ * graph capture and timing are as stated above; the calls marked (W) keep
+ * partial sums in a workspace of their own per (device, stream), which grows
+ * and is captured like the orthogonalizer's.  Every result is the same on
+ * every run (no float atomics).  NaN and Inf propagate, but never out of rows
+ * that take no part.
+ */
+#define TM_DTYPE_BF16 0
+#define TM_DTYPE_F32  1
+#define TM_MAX_ROWS    1073741824  /* rows of an operator */
+#define TM_MAX_EXPERTS 8192
+#define TM_MAX_VOCAB   1073741824
+
+/*
+ * tm_layer_norm - per row of d elements
+ *   mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),
+ *   y = (x - mean) rstd weight + bias.
+ *   weight, bias  d floats each, or NULL (ones, zeros).
+ *   mean, rstd    rows floats, written.
+ *   y may be x (same stride).  rows 0..TM_MAX_ROWS, d 1..TM_MAX_DIM.
+ */
+tm_status tm_layer_norm(const void* x, int64_t ldx, const float* weight, const float* bias, void* y,
+                        int64_t ldy, float* mean, float* rstd, int64_t rows, int64_t d, float eps,
+                        int dtype, void* stream);
+
+/*
+ * tm_layer_norm_backward (W) - with h = (x - mean) rstd and g = dy weight
+ *   dx = rstd (g - sum g / d - h sum(g h) / d),
+ *   dweight = sum over rows of dy h,  dbias = sum over rows of dy.
+ *   dweight, dbias  d floats each, written in full (zeros for no rows), or
+ *                   NULL where not wanted.
+ *   dx may be dy or x (same stride).
+ */
+tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                 const float* weight, const float* mean, const float* rstd, void* dx,
+                                 int64_t lddx, float* dweight, float* dbias, int64_t rows, int64_t d,
+                                 int dtype, void* stream);
+
+/*
+ * tm_expert_matmul - y[i, :] = x[i, :] W[e], e the expert of row i.
+ *   x     rows x k;  y  rows x n, of the same type.
+ *   w     matrix e starts at w + e stride_w: k x n with row stride ldw, or
+ *         n x k where `transposed` (y = x W^T: with the forward pass's w and dy
+ *         for x this is the gradient of the rows).
+ *   ends  device array of `experts` int32, not decreasing: expert e owns rows
+ *         ends[e - 1] .. ends[e] - 1 (from 0 for e = 0).  Experts may own no
+ *         row.  Rows after the last expert's come out as zeros.  Read on the
+ *         stream: no host synchronisation.  Whatever it holds, nothing outside
+ *         the matrices is read or written.
+ *   k, n  1..TM_MAX_DIM;  experts 1..TM_MAX_EXPERTS.
+ * y overlaps nothing that is read.
+ */
+tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t stride_w,
+                           const int32_t* ends, void* y, int64_t ldy, int64_t rows, int64_t experts,
+                           int64_t k, int64_t n, int transposed, int dtype, void* stream);
+
+/*
+ * tm_expert_wgrad - dw[e] = x_e^T dy_e over the rows of each expert (k x n;
+ * zeros for an expert without rows).
+ *   x, dy      rows x k and rows x n of type `dtype`.
+ *   dw         matrix e starts at dw + e stride_dw, row stride lddw; of type
+ *              `out_dtype`: fp32, or bf16 where the rows are.
+ */
+tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* ends,
+                          void* dw, int64_t lddw, int64_t stride_dw, int64_t rows, int64_t experts,
+                          int64_t k, int64_t n, int dtype, int out_dtype, void* stream);
+
+/*
+ * tm_policy_loss (W) - clipped policy loss with a KL term over rows of logits
+ * l with target y, at temperature tau:
+ *   lse = log sum_v exp(l_v / tau),  logp = l_y / tau - lse,
+ *   r = exp(logp - old_logp),  q = exp(ref_logp - logp),
+ *   loss = sum over rows of weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *                                   + kl (q - log q - 1)),
+ *   slope = d loss / d logp,  dlogits_v = slope ([v = y] - exp(l_v / tau - lse)) / tau.
+ *   logits      rows x vocab.
+ *   targets     int64 per row.  A negative target takes its row out, as weight
+ *               0 does; a target of vocab or more makes its row's results NaN.
+ *   old_logp, advantages, weights  fp32 per row; the weights hold the mask and
+ *               whatever the loss is divided by.
+ *   ref_logp    fp32 per row, or NULL: no KL term.
+ *   loss        one float.
+ *   logp        fp32 per row, written; lse, slope likewise, or NULL.
+ *   dlogits     rows x vocab of the logits' type (it may be the logits), or
+ *               NULL: the value alone.
+ * Rows that take no part: logp, lse, slope and their gradient are zero, their
+ * logits are not read.  A row of nothing but -inf gives NaN.
+ */
+tm_status tm_policy_loss(const void* logits, int64_t ld, const int64_t* targets, const float* old_logp,
+                         const float* advantages, const float* weights, const float* ref_logp,
+                         float clip_low, float clip_high, float kl, float temperature, float* loss,
+                         float* logp, float* lse, float* slope, void* dlogits, int64_t ld_dlogits,
+                         int64_t rows, int64_t vocab, int dtype, void* stream);
+
+/*
+ * tm_policy_loss_backward - dlogits from the lse and slope of an earlier
+ * tm_policy_loss on the same logits, targets and temperature, times *grad (a
+ * device float, NULL for 1).  Rows of slope 0 are not read, their gradient is
+ * zero.  dlogits may be the logits.
+ */
+tm_status tm_policy_loss_backward(const void* logits, int64_t ld, const int64_t* targets,
+                                  const float* lse, const float* slope, const float* grad,
+                                  float temperature, void* dlogits, int64_t ld_dlogits, int64_t rows,
+                                  int64_t vocab, int dtype, void* stream);
+
 /* Bytes of workspace a call with these shapes needs (0 on invalid shapes).
  * dtype_bytes is 2 (bf16) or 4 (fp32).  An upper bound: a bf16 call that the
  * fused small-matrix kernel serves uses none. */
@@ -248,7 +360,13 @@ tm_status tm_release_workspaces(void);
 #define TM_PHASE_OPT_MOMENTUM 10  /* optimizer step: momentum and the bf16 matrix to orthogonalize */
 #define TM_PHASE_OPT_APPLY    11  /* optimizer step: parameter update */
 #define TM_PHASE_FUSED        12  /* bf16 calls of small matrices: every iteration in one launch */
-#define TM_NUM_PHASES         13
+#define TM_PHASE_LAYER_NORM   13  /* from here on: one record per call, all of its launches */
+#define TM_PHASE_LAYER_NORM_BACKWARD  14
+#define TM_PHASE_EXPERT_MATMUL        15
+#define TM_PHASE_EXPERT_WGRAD         16
+#define TM_PHASE_POLICY_LOSS          17
+#define TM_PHASE_POLICY_LOSS_BACKWARD 18
+#define TM_NUM_PHASES         19
 
 /* Timing hooks (a profiling aid for benchmarks).  While enabled, every kernel
  * launch of later calls is bracketed by a pair of HIP events recorded on the

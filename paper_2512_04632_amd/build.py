@@ -51,6 +51,10 @@ def build(verbose: bool = False) -> str:
             (os.path.join(CSRC, "tm_optim.hip"), [], "k_optim.o"),
             (os.path.join(CSRC, "tm_noalloc.hip"), [], "noalloc.o"),
             (os.path.join(CSRC, "tm_small.hip"), [], "k_small.o"),
+            (os.path.join(CSRC, "tm_norm.hip"), [], "norm.o"),
+            (os.path.join(CSRC, "tm_loss.hip"), [], "loss.o"),
+            (os.path.join(CSRC, "tm_expert.hip"), [], "expert.o"),
+            (os.path.join(CSRC, "tm_ops.cpp"), [], "ops.o"),
             (os.path.join(CSRC, "tm_api.cpp"), [], "api.o"),
         ]
         cmds = [[HIPCC] + COMMON + extra + ["-c", src, "-o", os.path.join(tmp, obj)]

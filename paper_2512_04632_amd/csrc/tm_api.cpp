@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "tm_internal.h"
+#include "tm_ops.h"
 #include "turbomuon.h"
 
 namespace tmk {
@@ -53,6 +54,7 @@ std::mutex g_mu;
 using WsCache = std::map<std::pair<int, hipStream_t>, Workspace>;
 WsCache g_ws;     // iteration workspace of every call
 WsCache g_ws_u;   // bf16 update matrices of the optimizer step
+WsCache g_ws_op;  // partial sums of the operators beside the orthogonalizer
 std::map<int, bool> g_dev_ok;
 // Workspaces replaced while a captured graph may still hold their address:
 // freed only by tm_release_workspaces.
@@ -1348,6 +1350,32 @@ tm_status run_batched_bf16_in(void* X, int64_t m, int64_t n, int64_t batch, int 
 // Record a failure for tm_last_error().
 tm_status fail_with(tm_status s, const char* msg) { return fail(s, msg); }
 
+void clear_error() { g_last_error.clear(); }
+
+tm_status run_op(int phase, size_t bytes, hipStream_t st, const Enqueue& enqueue) {
+  std::lock_guard<std::mutex> lock(g_mu);
+  int dev = 0;
+  tm_status s = check_device(&dev);
+  if (s != TM_OK) return s;
+  char* ws = nullptr;
+  if (bytes > 0) s = get_workspace(dev, st, bytes, bytes, capturing(st), &ws, g_ws_op);
+  if (s != TM_OK) return s;
+  TimedLaunch tl{phase, nullptr, nullptr};
+  if (g_timing) {
+    if (hipEventCreate(&tl.start) != hipSuccess || hipEventCreate(&tl.stop) != hipSuccess)
+      return fail(TM_ERR_HIP, "hipEventCreate failed");
+    (void)hipEventRecord(tl.start, st);
+  }
+  const hipError_t e = enqueue(ws, st);
+  if (tl.start) {
+    (void)hipEventRecord(tl.stop, st);
+    g_timed.push_back(tl);
+  }
+  if (e == hipErrorInvalidConfiguration) return fail(TM_ERR_UNSUPPORTED, "too many blocks in one launch");
+  if (e != hipSuccess) return fail(TM_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
+  return TM_OK;
+}
+
 }  // namespace tmk
 
 extern "C" {
@@ -1489,9 +1517,9 @@ uint64_t tm_workspace_bytes(const int64_t* m, const int64_t* n, int64_t count, i
 
 tm_status tm_release_workspaces(void) {
   std::lock_guard<std::mutex> lock(g_mu);
-  if (g_ws.empty() && g_ws_u.empty() && g_retired.empty()) return TM_OK;
+  if (g_ws.empty() && g_ws_u.empty() && g_ws_op.empty() && g_retired.empty()) return TM_OK;
   hipError_t e = hipDeviceSynchronize();
-  for (WsCache* c : {&g_ws, &g_ws_u}) {
+  for (WsCache* c : {&g_ws, &g_ws_u, &g_ws_op}) {
     for (auto& kv : *c)
       if (kv.second.ptr) (void)hipFree(kv.second.ptr);
     c->clear();

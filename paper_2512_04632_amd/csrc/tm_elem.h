@@ -1,0 +1,94 @@
+// Element access shared by the streaming operators (layer norm, policy loss):
+// rows of bf16 or fp32 read and written 16 bytes at a time at the element's own
+// alignment (the global memory path takes 16-byte accesses at any), values in
+// fp32.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tmk {
+namespace elem {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t u32x4_a2 __attribute__((aligned(2)));   // at a bf16 element's alignment
+typedef u32x4_t u32x4_a4 __attribute__((aligned(4)));
+
+struct Bf16 {
+  static constexpr int kBytes = 2, W = 8;   // W: elements of a 16-byte vector
+  __device__ static u32x4_t load(const char* p) { return *reinterpret_cast<const u32x4_a2*>(p); }
+  __device__ static void store(char* p, u32x4_t v) { *reinterpret_cast<u32x4_a2*>(p) = v; }
+  __device__ static void unpack(u32x4_t q, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(q[i] << 16);
+      v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+    }
+  }
+  __device__ static u32x4_t pack(const float* v) {   // rounds to nearest even
+    u32x4_t q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[2 * i]));
+      const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[2 * i + 1]));
+      q[i] = lo | hi << 16;
+    }
+    return q;
+  }
+  __device__ static float load1(const char* p) {
+    return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
+  }
+  __device__ static void store1(char* p, float v) {
+    *reinterpret_cast<uint16_t*>(p) = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+  }
+};
+
+struct F32 {
+  static constexpr int kBytes = 4, W = 4;
+  __device__ static u32x4_t load(const char* p) { return *reinterpret_cast<const u32x4_a4*>(p); }
+  __device__ static void store(char* p, u32x4_t v) { *reinterpret_cast<u32x4_a4*>(p) = v; }
+  __device__ static void unpack(u32x4_t q, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(q[i]);
+  }
+  __device__ static u32x4_t pack(const float* v) {
+    u32x4_t q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(v[i]);
+    return q;
+  }
+  __device__ static float load1(const char* p) { return *reinterpret_cast<const float*>(p); }
+  __device__ static void store1(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
+};
+
+// Elements first .. first + W - 1 of a row of n (`fill` past its end).
+template <class T>
+__device__ inline void load_vec(const char* row, int first, int n, float fill, float* v) {
+  if (first + T::W <= n) {
+    T::unpack(T::load(row + int64_t(first) * T::kBytes), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < T::W; ++i)
+      v[i] = first + i < n ? T::load1(row + int64_t(first + i) * T::kBytes) : fill;
+  }
+}
+
+template <class T>
+__device__ inline void store_vec(char* row, int first, int n, const float* v) {
+  if (first + T::W <= n) {
+    T::store(row + int64_t(first) * T::kBytes, T::pack(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < T::W; ++i)
+      if (first + i < n) T::store1(row + int64_t(first + i) * T::kBytes, v[i]);
+  }
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+}  // namespace elem
+}  // namespace tmk

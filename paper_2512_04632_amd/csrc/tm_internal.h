@@ -221,7 +221,9 @@ TM_HD int cfg_tile(int cfg) { return cfg == 0 ? 256 : (cfg == 1 ? 128 : (cfg == 
 // The numbering matches the TM_PHASE_* timing phases of turbomuon.h.
 enum Kind { kKindTransposeIn, kKindFrob, kKindGram, kKindAolVector, kKindPoly,
             kKindUpdate, kKindApplyScale, kKindCopyOut, kKindLoadIn, kKindScaleA,
-            kKindOptMomentum, kKindOptApply, kKindSmall, kNumKinds };
+            kKindOptMomentum, kKindOptApply, kKindSmall, kKindLayerNorm,
+            kKindLayerNormBackward, kKindExpertMatmul, kKindExpertWgrad, kKindPolicyLoss,
+            kKindPolicyLossBackward, kNumKinds };
 constexpr int kTransposeTile = 64;
 constexpr int kElemBlock = 2048;     // elements per block of the elementwise kernels
 

@@ -1,0 +1,340 @@
+// Clipped policy loss with a KL term, from the logits, for gfx950.
+//
+// Row t has logits l of a vocabulary of V, a target y, a weight m (0: the row
+// takes no part), an advantage A and log probabilities of the sampling and of a
+// reference policy.  With the temperature tau
+//
+//   logp  = l_y / tau - lse,  lse = log sum_v exp(l_v / tau)
+//   r     = exp(logp - old),  q = exp(ref - logp)
+//   loss += m (-min(r A, clip(r, 1 - low, 1 + high) A) + kl (q - log q - 1))
+//   slope = d loss / d logp = m (-[r within the bound on A's side] r A + kl (1 - q))
+//   dlogits_v = slope ([v = y] - exp(l_v / tau - lse)) / tau
+//
+// The passes are bound by HBM: the logits are read once for the value, and once
+// more where they are not still in a cache for the gradient, which is as large.
+// The running maximum and sum of exponentials of each thread are joined at the
+// end of a row.  Sums and statistics are fp32, exponentials are taken of the
+// distance from the maximum; only dlogits is rounded to the logits' type.
+// Rows of weight 0 or with a negative target are not read: their gradient is
+// written as zeros whatever their logits hold.
+#include <algorithm>
+
+#include "tm_elem.h"
+#include "tm_ops.h"
+
+namespace tmk {
+namespace loss {
+
+using namespace elem;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// v_exp_f32: 1 ulp, results below the smallest normal number are zero
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Running maximum m and sum s of exp2((l - m) c).
+struct Soft {
+  float m, s;
+};
+__device__ inline Soft nothing() { return Soft{-INFINITY, 0.f}; }
+
+// exp2((l - m) c) of a part's terms when its maximum moves from `from` to
+// `to`; nothing was summed while the maximum was -inf.
+__device__ inline float rescale(float from, float to, float c) {
+  return from == -INFINITY ? 0.f : exp2_fast((from - to) * c);
+}
+
+__device__ inline Soft join(Soft a, Soft b, float c) {
+  Soft o;
+  o.m = fmaxf(a.m, b.m);
+  o.s = a.s * rescale(a.m, o.m, c) + b.s * rescale(b.m, o.m, c);
+  // a NaN in either maximum must not vanish in fmaxf
+  if (a.s != a.s || b.s != b.s) o.s = NAN;
+  return o;
+}
+
+template <int N>
+__device__ inline void add_terms(Soft& a, const float* v, float c) {
+  float m = v[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+  if (m > a.m) {
+    a.s *= rescale(a.m, m, c);
+    a.m = m;
+  }
+  // while every value is -inf the terms are taken as exp(-inf - 0) = 0
+  const float at = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) a.s += exp2_fast((v[i] - at) * c);
+}
+
+__device__ inline Soft wave_join(Soft a, float c) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    Soft b;
+    b.m = __shfl_xor(a.m, o);
+    b.s = __shfl_xor(a.s, o);
+    a = join(a, b, c);
+  }
+  return a;
+}
+
+template <int NT>
+__device__ inline Soft block_join(Soft a, float c, Soft* slots) {
+  a = wave_join(a, c);
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = a;
+  __syncthreads();
+  a = slots[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) a = join(a, slots[w], c);
+  return a;
+}
+
+__device__ inline bool active(const LossArgs& A, int64_t r) {
+  return A.weights[r] != 0.f && A.targets[r] >= 0;
+}
+
+struct Row {
+  float logp, lse, slope, loss;
+};
+
+// What a row gives once its maximum and sum are known.
+template <class T>
+__device__ inline Row finish(const LossArgs& A, int64_t r, Soft s) {
+  const int64_t y = A.targets[r];
+  const float log_sum = logf(s.s);
+  const float ly = y < A.vocab ? T::load1(A.logits + (r * A.ld + y) * T::kBytes) : NAN;
+  Row o;
+  o.lse = s.m * A.inv_temp + log_sum;
+  o.logp = (ly - s.m) * A.inv_temp - log_sum;
+  const float m = A.weights[r], adv = A.advantages[r];
+  const float ratio = expf(o.logp - A.old_logp[r]);
+  const float lo = 1.f - A.clip_low, hi = 1.f + A.clip_high;
+  const bool clipped = adv >= 0.f ? ratio > hi : ratio < lo;
+  const float at = clipped ? (adv >= 0.f ? hi : lo) : ratio;
+  float value = -at * adv, grad = clipped ? 0.f : -ratio * adv;
+  if (A.ref_logp != nullptr) {
+    const float gap = A.ref_logp[r] - o.logp;
+    const float q = expf(gap);
+    value += A.kl * (q - gap - 1.f);
+    grad += A.kl * (1.f - q);
+  }
+  o.loss = m * value;
+  o.slope = m * grad;
+  return o;
+}
+
+__device__ inline void write_row(const LossArgs& A, int64_t r, const Row& o) {
+  A.logp[r] = o.logp;
+  A.lse[r] = o.lse;
+  A.slope[r] = o.slope;
+  A.row_loss[r] = o.loss;
+}
+
+// Gradient of vocabulary entries first .. first + W - 1: p = exp2((l - m) c) inv,
+// out = f ([v = y] - p).
+template <class T>
+__device__ inline void gradient_vec(float* v, int first, int64_t y, float m, float c, float inv, float f) {
+#pragma unroll
+  for (int i = 0; i < T::W; ++i) {
+    const float p = exp2_fast((v[i] - m) * c) * inv;
+    v[i] = f * ((first + i == y ? 1.f : 0.f) - p);
+  }
+}
+
+template <class T, int NT>
+__device__ inline void zero_row(char* row, int n) {
+  float z[T::W];
+#pragma unroll
+  for (int i = 0; i < T::W; ++i) z[i] = 0.f;
+  for (int c = threadIdx.x * T::W; c < n; c += NT * T::W) store_vec<T>(row, c, n, z);
+}
+
+// One workgroup per row.
+template <class T, int NT, bool GRAD>
+__global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
+  __shared__ Soft slots[NT / 64];
+  __shared__ Row row;
+  const int64_t r = blockIdx.x;
+  const int n = A.vocab;
+  if (!active(A, r)) {
+    if (threadIdx.x == 0) write_row(A, r, Row{0.f, 0.f, 0.f, 0.f});
+    if constexpr (GRAD) zero_row<T, NT>(A.dlogits + r * A.ldd * T::kBytes, n);
+    return;
+  }
+  const char* l = A.logits + r * A.ld * T::kBytes;
+  const float c = A.inv_temp * kLog2e;
+  Soft s = nothing();
+  for (int f = threadIdx.x * T::W; f < n; f += NT * T::W) {
+    float v[T::W];
+    load_vec<T>(l, f, n, -INFINITY, v);
+    add_terms<T::W>(s, v, c);
+  }
+  s = block_join<NT>(s, c, slots);
+  if (threadIdx.x == 0) {
+    row = finish<T>(A, r, s);
+    write_row(A, r, row);
+  }
+  if constexpr (GRAD) {
+    __syncthreads();
+    char* d = A.dlogits + r * A.ldd * T::kBytes;
+    const float f = row.slope * A.inv_temp, inv = 1.f / s.s;
+    const int64_t y = A.targets[r];
+    if (f == 0.f) {
+      zero_row<T, NT>(d, n);
+      return;
+    }
+    for (int at = threadIdx.x * T::W; at < n; at += NT * T::W) {
+      float v[T::W];
+      load_vec<T>(l, at, n, 0.f, v);
+      gradient_vec<T>(v, at, y, s.m, c, inv, f);
+      store_vec<T>(d, at, n, v);
+    }
+  }
+}
+
+// Few rows: a workgroup per chunk of a row.
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_part(const LossArgs A) {
+  __shared__ Soft slots[4];
+  const int64_t r = blockIdx.x / A.chunks;
+  if (!active(A, r)) return;
+  const int q = blockIdx.x - int(r) * A.chunks;
+  const int first = q * A.chunk, last = min(A.vocab, first + A.chunk);
+  const char* l = A.logits + r * A.ld * T::kBytes;
+  const float c = A.inv_temp * kLog2e;
+  Soft s = nothing();
+  for (int f = first + threadIdx.x * T::W; f < last; f += 256 * T::W) {
+    float v[T::W];
+    load_vec<T>(l, f, last, -INFINITY, v);
+    add_terms<T::W>(s, v, c);
+  }
+  s = block_join<256>(s, c, slots);
+  if (threadIdx.x == 0) A.part[blockIdx.x] = make_float2(s.m, s.s);
+}
+
+// One wave per row joins its chunks.  SUM: a single workgroup takes every row
+// and adds the loss up as well.
+template <class T, bool SUM>
+__global__ __launch_bounds__(1024) void k_loss_join(const LossArgs A) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float c = A.inv_temp * kLog2e;
+  double total = 0.0;
+  for (int64_t r = int64_t(blockIdx.x) * 16 + wave; r < A.rows; r += int64_t(gridDim.x) * 16) {
+    Row o{0.f, 0.f, 0.f, 0.f};
+    if (active(A, r)) {
+      Soft s = nothing();
+      for (int q = lane; q < A.chunks; q += 64) {
+        const float2 p = A.part[r * A.chunks + q];
+        s = join(s, Soft{p.x, p.y}, c);
+      }
+      s = wave_join(s, c);
+      o = finish<T>(A, r, s);
+    }
+    if (lane == 0) write_row(A, r, o);
+    total += double(o.loss);
+  }
+  if constexpr (SUM) {
+    __shared__ double sums[16];
+    if (lane == 0) sums[wave] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 16; ++w) total += sums[w];
+      *A.loss = float(total);
+    }
+  }
+}
+
+// The rows' shares added up in a fixed order, in 64 bits.
+__global__ __launch_bounds__(1024) void k_loss_sum(const float* row_loss, int rows, float* out) {
+  __shared__ double sums[1024];
+  double s = 0.0;
+  for (int r = threadIdx.x; r < rows; r += 1024) s += double(row_loss[r]);
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if (int(threadIdx.x) < o) sums[threadIdx.x] += sums[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *out = float(sums[0]);
+}
+
+// dlogits from lse and slope, a workgroup per chunk of a row.  Rows of slope
+// 0 are not read.  l / tau - lse is rounded once (fma).
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
+  const int64_t r = blockIdx.x / A.chunks;
+  const int q = blockIdx.x - int(r) * A.chunks;
+  const int first = q * A.chunk, last = min(A.vocab, first + A.chunk);
+  const float slope = A.slope[r];
+  const char* l = A.logits + r * A.ld * T::kBytes;
+  char* d = A.dlogits + r * A.ldd * T::kBytes;
+  const float f = slope * A.inv_temp * (A.grad != nullptr ? *A.grad : 1.f);
+  const float lse = A.lse[r];
+  const int64_t y = A.targets[r];
+  for (int at = first + threadIdx.x * T::W; at < last; at += 256 * T::W) {
+    float v[T::W];
+    if (slope == 0.f) {
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) v[i] = 0.f;
+    } else {
+      load_vec<T>(l, at, last, 0.f, v);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) {
+        const float p = exp2_fast(fmaf(v[i], A.inv_temp, -lse) * kLog2e);
+        v[i] = f * ((at + i == y ? 1.f : 0.f) - p);
+      }
+    }
+    store_vec<T>(d, at, last, v);
+  }
+}
+
+constexpr int kJoinRows = 64;   // up to here one workgroup joins and sums every row
+
+template <class T>
+hipError_t forward_t(const LossArgs& A, hipStream_t st) {
+  if (A.rows == 0) {
+    // the sum of no rows
+  } else if (A.chunks == 1) {
+    const bool wide = int64_t(A.vocab) * T::kBytes > 32768;
+    const dim3 grid(uint32_t(A.rows)), block(wide ? 1024 : 256);
+    if (A.dlogits != nullptr) {
+      if (wide) hipLaunchKernelGGL((k_loss_rows<T, 1024, true>), grid, block, 0, st, A);
+      else hipLaunchKernelGGL((k_loss_rows<T, 256, true>), grid, block, 0, st, A);
+    } else {
+      if (wide) hipLaunchKernelGGL((k_loss_rows<T, 1024, false>), grid, block, 0, st, A);
+      else hipLaunchKernelGGL((k_loss_rows<T, 256, false>), grid, block, 0, st, A);
+    }
+  } else {
+    hipLaunchKernelGGL((k_loss_part<T>), dim3(uint32_t(A.rows) * A.chunks), dim3(256), 0, st, A);
+    if (A.rows <= kJoinRows)
+      hipLaunchKernelGGL((k_loss_join<T, true>), dim3(1), dim3(1024), 0, st, A);
+    else
+      hipLaunchKernelGGL((k_loss_join<T, false>), dim3((A.rows + 15) / 16), dim3(1024), 0, st, A);
+    if (A.dlogits != nullptr)
+      hipLaunchKernelGGL((k_loss_gradient<T>), dim3(uint32_t(A.rows) * A.chunks), dim3(256), 0, st, A);
+  }
+  if (A.chunks == 1 || A.rows > kJoinRows)
+    hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(1024), 0, st, A.row_loss, A.rows, A.loss);
+  return hipGetLastError();
+}
+
+}  // namespace loss
+
+int loss_chunks(int64_t rows, int64_t vocab) {
+  if (rows >= 512 || vocab < 8192) return 1;
+  return int(std::min<int64_t>((1024 + rows - 1) / rows, vocab / 4096));
+}
+
+hipError_t launch_loss(const LossArgs& A, bool f32, hipStream_t st) {
+  return f32 ? loss::forward_t<elem::F32>(A, st) : loss::forward_t<elem::Bf16>(A, st);
+}
+
+hipError_t launch_loss_backward(const LossArgs& A, bool f32, hipStream_t st) {
+  const dim3 grid(uint32_t(A.rows) * uint32_t(A.chunks));
+  if (f32) hipLaunchKernelGGL((loss::k_loss_gradient<elem::F32>), grid, dim3(256), 0, st, A);
+  else hipLaunchKernelGGL((loss::k_loss_gradient<elem::Bf16>), grid, dim3(256), 0, st, A);
+  return hipGetLastError();
+}
+
+}  // namespace tmk

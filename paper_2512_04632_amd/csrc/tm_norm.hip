@@ -1,0 +1,381 @@
+// Layer norm over the rows of a matrix, forward and backward, for gfx950.
+//
+//   forward   mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),
+//             y = (x - mean) rstd weight + bias
+//   backward  h = (x - mean) rstd,  g = dy weight,
+//             dx = rstd (g - sum g / d - h sum(g h) / d),
+//             dweight = sum over rows of dy h,  dbias = sum over rows of dy
+//
+// A row stays in the registers of the NT threads that own it (E elements
+// each), so it is read once: the variance is the mean of the squared
+// distances from the finished mean, with none of the cancellation that sums
+// of squares have.  Each thread owns the same columns of every row it sees,
+// so the backward pass keeps its share of the weight's and the bias's
+// gradients in registers too; blocks go through the rows with a stride of the
+// grid and write one line of partial sums each, which k_norm_params adds up in
+// a fixed order (no atomics: results are the same on every run).  Statistics
+// and sums are fp32; y and dx are rounded once.
+#include <algorithm>
+
+#include "tm_elem.h"
+#include "tm_ops.h"
+
+namespace tmk {
+namespace norm {
+
+using namespace elem;
+
+// Sum of v over the NT threads of a row, in every one of them.  `slot` holds
+// NT / 64 floats and is not used again before another barrier.
+template <int NT, int N>
+__device__ inline void row_sum(float (&v)[N], float* slot) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (NT > 64) {
+    constexpr int NW = NT / 64;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) slot[i * NW + (threadIdx.x >> 6)] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) s += slot[i * NW + w];
+      v[i] = s;
+    }
+  }
+}
+
+template <int NT>
+constexpr int block_threads() { return NT < 256 ? 256 : NT; }
+
+template <int NT, int E, class T>
+__device__ inline void load_cols(const float* p, float fill, int t, int d, float* v) {
+#pragma unroll
+  for (int j = 0; j < E / T::W; ++j) {
+    const int c = (j * NT + t) * T::W;
+#pragma unroll
+    for (int i = 0; i < T::W; ++i) v[j * T::W + i] = p != nullptr && c + i < d ? p[c + i] : fill;
+  }
+}
+
+template <class T, int NT, int E>
+__global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) {
+  constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
+  __shared__ float slots[2][NW];
+  const int t = threadIdx.x % NT, d = A.d;
+  const float n = float(d);
+  float w[E], b[E];
+  load_cols<NT, E, T>(A.weight, 1.f, t, d, w);
+  load_cols<NT, E, T>(A.bias, 0.f, t, d, b);
+  for (int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT; r < A.rows; r += int64_t(gridDim.x) * RB) {
+    const char* x = A.x + r * A.ldx * T::kBytes;
+    float v[E], s[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      load_vec<T>(x, (j * NT + t) * W, d, 0.f, v + j * W);
+#pragma unroll
+      for (int i = 0; i < W; ++i) s[0] += v[j * W + i];
+    }
+    row_sum<NT>(s, slots[0]);
+    const float mean = s[0] / n;
+    s[0] = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float c = (j * NT + t) * W + i < d ? v[j * W + i] - mean : 0.f;
+        v[j * W + i] = c;
+        s[0] += c * c;
+      }
+    row_sum<NT>(s, slots[1]);
+    const float rstd = 1.f / sqrtf(s[0] / n + A.eps);
+    if (t == 0) {
+      A.mean[r] = mean;
+      A.rstd[r] = rstd;
+    }
+    char* y = A.out + r * A.ldo * T::kBytes;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float o[W];
+#pragma unroll
+      for (int i = 0; i < W; ++i) o[i] = v[j * W + i] * rstd * w[j * W + i] + b[j * W + i];
+      store_vec<T>(y, (j * NT + t) * W, d, o);
+    }
+  }
+}
+
+template <class T, int NT, int E>
+__global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const NormArgs A) {
+  constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
+  __shared__ float slots[2][2 * NW];
+  const int t = threadIdx.x % NT, d = A.d;
+  const float n = float(d);
+  float w[E], aw[E], ab[E];
+  load_cols<NT, E, T>(A.weight, 1.f, t, d, w);
+#pragma unroll
+  for (int i = 0; i < E; ++i) aw[i] = ab[i] = 0.f;
+  int turn = 0;
+  for (int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT; r < A.rows; r += int64_t(gridDim.x) * RB) {
+    const char* x = A.x + r * A.ldx * T::kBytes;
+    const char* dy = A.dy + r * A.lddy * T::kBytes;
+    const float mean = A.mean[r], rstd = A.rstd[r];
+    float h[E], g[E], s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = (j * NT + t) * W;
+      load_vec<T>(x, c, d, mean, h + j * W);
+      load_vec<T>(dy, c, d, 0.f, g + j * W);
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const int e = j * W + i;
+        h[e] = (h[e] - mean) * rstd;
+        aw[e] += g[e] * h[e];
+        ab[e] += g[e];
+        g[e] *= w[e];
+        s[0] += g[e];
+        s[1] += g[e] * h[e];
+      }
+    }
+    row_sum<NT>(s, slots[turn]);
+    turn ^= 1;
+    const float m0 = s[0] / n, m1 = s[1] / n;
+    char* dx = A.out + r * A.ldo * T::kBytes;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float o[W];
+#pragma unroll
+      for (int i = 0; i < W; ++i) o[i] = rstd * (g[j * W + i] - m0 - h[j * W + i] * m1);
+      store_vec<T>(dx, (j * NT + t) * W, d, o);
+    }
+  }
+  if (A.part == nullptr) return;
+  float* part = A.part + int64_t(blockIdx.x) * 2 * d;
+  if constexpr (RB > 1) {   // the block's rows first, one after the other
+    __shared__ float sums[2 * NT * E];
+    for (int q = 0; q < RB; ++q) {
+      if (int(threadIdx.x) / NT == q)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int at = (e / W * NT + t) * W + e % W;
+          sums[at] = (q > 0 ? sums[at] : 0.f) + aw[e];
+          sums[NT * E + at] = (q > 0 ? sums[NT * E + at] : 0.f) + ab[e];
+        }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < d; c += block_threads<NT>()) {
+      part[c] = sums[c];
+      part[d + c] = sums[NT * E + c];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e / W * NT + t) * W + e % W;
+      if (c < d) {
+        part[c] = aw[e];
+        part[d + c] = ab[e];
+      }
+    }
+  }
+}
+
+// Rows wider than a workgroup's registers (kNormMaxFused): one workgroup of
+// 1024 threads per row, which reads the row once for each sum and once for the
+// result (the later passes find it in a cache).
+constexpr int kWide = 1024;
+
+template <class T, class F>
+__device__ inline void each_vec(int d, F f) {
+  for (int c = threadIdx.x * T::W; c < d; c += kWide * T::W) f(c);
+}
+
+__device__ inline float col(const float* p, float fill, int c, int d) { return p != nullptr && c < d ? p[c] : fill; }
+
+template <class T>
+__global__ __launch_bounds__(kWide) void k_norm_wide(const NormArgs A) {
+  __shared__ float slots[2][kWide / 64];
+  const int d = A.d;
+  const float n = float(d);
+  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+    const char* x = A.x + r * A.ldx * T::kBytes;
+    char* y = A.out + r * A.ldo * T::kBytes;
+    float s[1] = {0.f}, v[T::W];
+    each_vec<T>(d, [&](int c) {
+      load_vec<T>(x, c, d, 0.f, v);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) s[0] += v[i];
+    });
+    row_sum<kWide>(s, slots[0]);
+    const float mean = s[0] / n;
+    s[0] = 0.f;
+    each_vec<T>(d, [&](int c) {
+      load_vec<T>(x, c, d, mean, v);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) s[0] += (v[i] - mean) * (v[i] - mean);
+    });
+    row_sum<kWide>(s, slots[1]);
+    const float rstd = 1.f / sqrtf(s[0] / n + A.eps);
+    if (threadIdx.x == 0) {
+      A.mean[r] = mean;
+      A.rstd[r] = rstd;
+    }
+    each_vec<T>(d, [&](int c) {
+      load_vec<T>(x, c, d, mean, v);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i)
+        v[i] = (v[i] - mean) * rstd * col(A.weight, 1.f, c + i, d) + col(A.bias, 0.f, c + i, d);
+      store_vec<T>(y, c, d, v);
+    });
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(kWide) void k_norm_backward_wide(const NormArgs A) {
+  __shared__ float slots[2][2 * kWide / 64];
+  const int d = A.d;
+  const float n = float(d);
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+    const char* x = A.x + r * A.ldx * T::kBytes;
+    const char* dy = A.dy + r * A.lddy * T::kBytes;
+    char* dx = A.out + r * A.ldo * T::kBytes;
+    const float mean = A.mean[r], rstd = A.rstd[r];
+    float s[2] = {0.f, 0.f}, h[T::W], g[T::W];
+    auto read = [&](int c) {
+      load_vec<T>(x, c, d, mean, h);
+      load_vec<T>(dy, c, d, 0.f, g);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) {
+        h[i] = (h[i] - mean) * rstd;
+        g[i] *= col(A.weight, 1.f, c + i, d);
+      }
+    };
+    each_vec<T>(d, [&](int c) {
+      read(c);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) {
+        s[0] += g[i];
+        s[1] += g[i] * h[i];
+      }
+    });
+    row_sum<kWide>(s, slots[turn]);
+    turn ^= 1;
+    const float m0 = s[0] / n, m1 = s[1] / n;
+    each_vec<T>(d, [&](int c) {
+      read(c);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) g[i] = rstd * (g[i] - m0 - h[i] * m1);
+      store_vec<T>(dx, c, d, g);
+    });
+  }
+}
+
+// Column sums of such rows: one thread per column, each block a slice of the
+// rows (x and dy are read once more).
+template <class T>
+__global__ __launch_bounds__(256) void k_norm_columns(const NormArgs A, int slices) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= A.d) return;
+  float aw = 0.f, ab = 0.f;
+  for (int64_t r = blockIdx.y; r < A.rows; r += slices) {
+    const float g = T::load1(A.dy + (r * A.lddy + c) * T::kBytes);
+    const float x = T::load1(A.x + (r * A.ldx + c) * T::kBytes);
+    aw += g * ((x - A.mean[r]) * A.rstd[r]);
+    ab += g;
+  }
+  float* part = A.part + int64_t(blockIdx.y) * 2 * A.d;
+  part[c] = aw;
+  part[A.d + c] = ab;
+}
+
+// out[c] = sum of the blocks' partial sums of column c: 32 columns a block,
+// eight threads each.
+__global__ __launch_bounds__(256) void k_norm_params(const float* part, int blocks, int d, float* dweight,
+                                                     float* dbias) {
+  float* out = blockIdx.y == 0 ? dweight : dbias;
+  if (out == nullptr) return;
+  __shared__ float sums[8][32];
+  const int lc = threadIdx.x & 31, grp = threadIdx.x >> 5, c = blockIdx.x * 32 + lc;
+  float s = 0.f;
+  if (c < d)
+    for (int b = grp; b < blocks; b += 8) s += part[(int64_t(b) * 2 + blockIdx.y) * d + c];
+  sums[grp][lc] = s;
+  __syncthreads();
+  if (grp == 0 && c < d) {
+    for (int q = 1; q < 8; ++q) s += sums[q][lc];
+    out[c] = s;
+  }
+}
+
+constexpr int kMostBlocks = 2048;   // 8 workgroups of 256 threads per compute unit
+
+template <class T, int NT, int E>
+hipError_t forward(const NormArgs& A, hipStream_t st) {
+  constexpr int RB = block_threads<NT>() / NT;
+  const int blocks = int(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, kMostBlocks));
+  hipLaunchKernelGGL((k_norm<T, NT, E>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
+  return hipGetLastError();
+}
+
+template <class T, int NT, int E>
+hipError_t backward(const NormArgs& A, int blocks, hipStream_t st) {
+  hipLaunchKernelGGL((k_norm_backward<T, NT, E>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t forward_t(const NormArgs& A, hipStream_t st) {
+  const int d = A.d;
+  if (d <= 512) return forward<T, 64, 8>(A, st);
+  if (d <= 1024) return forward<T, 64, 16>(A, st);
+  if (d <= 2048) return forward<T, 256, 8>(A, st);
+  if (d <= 4096) return forward<T, 256, 16>(A, st);
+  if (d <= 8192) return forward<T, 512, 16>(A, st);
+  if (d <= kNormMaxFused) return forward<T, 1024, 16>(A, st);
+  hipLaunchKernelGGL((k_norm_wide<T>), dim3(std::min(A.rows, kMostBlocks)), dim3(kWide), 0, st, A);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t backward_t(const NormArgs& A, int blocks, hipStream_t st) {
+  const int d = A.d;
+  if (d <= 512) return backward<T, 64, 8>(A, blocks, st);
+  if (d <= 1024) return backward<T, 64, 16>(A, blocks, st);
+  if (d <= 2048) return backward<T, 256, 8>(A, blocks, st);
+  if (d <= 4096) return backward<T, 256, 16>(A, blocks, st);
+  if (d <= 8192) return backward<T, 512, 16>(A, blocks, st);
+  if (d <= kNormMaxFused) return backward<T, 1024, 16>(A, blocks, st);
+  // dx may take the place of x or dy, so the column sums come first
+  if (A.part != nullptr) {
+    hipLaunchKernelGGL((k_norm_columns<T>), dim3((d + 255) / 256, blocks), dim3(256), 0, st, A, blocks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_norm_backward_wide<T>), dim3(std::min(A.rows, kMostBlocks)), dim3(kWide), 0, st, A);
+  return hipGetLastError();
+}
+
+}  // namespace norm
+
+hipError_t launch_norm(const NormArgs& A, bool f32, hipStream_t st) {
+  return f32 ? norm::forward_t<elem::F32>(A, st) : norm::forward_t<elem::Bf16>(A, st);
+}
+
+int norm_blocks(int64_t rows, int64_t d) {
+  const int rb = d <= 1024 ? 4 : 1;
+  const int most = d > kNormMaxFused ? 64 : d > 4096 ? 256 : 512;
+  return int(std::min<int64_t>((rows + rb - 1) / rb, most));
+}
+
+hipError_t launch_norm_backward(const NormArgs& A, bool f32, int blocks, hipStream_t st) {
+  return f32 ? norm::backward_t<elem::F32>(A, blocks, st) : norm::backward_t<elem::Bf16>(A, blocks, st);
+}
+
+hipError_t launch_norm_params(const float* part, int blocks, int d, float* dweight, float* dbias,
+                              hipStream_t st) {
+  hipLaunchKernelGGL(norm::k_norm_params, dim3((d + 31) / 32, 2), dim3(256), 0, st, part, blocks, d, dweight, dbias);
+  return hipGetLastError();
+}
+
+}  // namespace tmk

@@ -5,8 +5,9 @@ orthogonalization and keeps the rest of Muon's step.  This optimizer is a
 thin front end of the library's ``tm_muon_step_grouped``: every arithmetic
 step (momentum, the bf16 orthogonalization, the parameter update) runs in the
 library's kernels; this module only keeps the momentum buffers and passes
-pointers.  Parameters must be 2-D fp32 tensors on one GPU (vectors and
-scalars belong to another optimizer, as with Muon).
+pointers.  Parameters must be fp32 tensors on one GPU, matrices or stacks of
+matrices (experts, rows, columns) whose matrices are updated each by itself
+(vectors and scalars belong to another optimizer, as with Muon).
 """
 from __future__ import annotations
 
@@ -35,8 +36,8 @@ class TurboMuon(torch.optim.Optimizer):
         super().__init__(params, defaults)
         for group in self.param_groups:
             for p in group["params"]:
-                if p.dim() != 2 or p.dtype != torch.float32:
-                    raise ValueError("TurboMuon takes 2-D fp32 parameters only")
+                if p.dim() not in (2, 3) or p.dtype != torch.float32:
+                    raise ValueError("TurboMuon takes fp32 matrices and stacks of them only")
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -52,9 +53,9 @@ class TurboMuon(torch.optim.Optimizer):
                 state = self.state[p]
                 if "momentum_buffer" not in state:
                     state["momentum_buffer"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
-                ps.append(p)
-                gs.append(p.grad if p.grad.is_contiguous() else p.grad.contiguous())
-                ms.append(state["momentum_buffer"])
+                grad = p.grad if p.grad.is_contiguous() else p.grad.contiguous()
+                for of, t in ((ps, p), (gs, grad), (ms, state["momentum_buffer"])):
+                    of.extend(t.unbind(0) if p.dim() == 3 else (t,))
             if ps:
                 _lib.muon_step_grouped(ps, gs, ms, group["lr"], group["momentum"],
                                        group["nesterov"], group["weight_decay"],

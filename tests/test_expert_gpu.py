@@ -1,0 +1,258 @@
+"""Expert products on the GPU against products in 64 bits, group by group.
+
+Tolerances (u = 2^-24): a product of K terms accumulated in fp32, in whatever
+order and grouping, is off by at most 2 K u of the sum of the terms' absolute
+values; a bf16 result is rounded once more, 2^-8 of itself.
+"""
+import pytest
+
+from gpu_helpers import log
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2512_04632_amd import _lib as tm, ops  # noqa: E402
+
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _randn(g, shape, dtype, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(DT[dtype])
+
+
+def _ends(counts):
+    return torch.tensor(counts).cumsum(0).to(torch.int32).cuda()
+
+
+def _bounds(counts):
+    at = 0
+    for e, c in enumerate(counts):
+        yield e, at, at + c
+        at += c
+
+
+def _close(got, want, terms, K, dtype):
+    bound = 2 * K * U * terms + 1e-38
+    bound = bound + (2.0 ** -8 if dtype == "bf16" else U) * (want.abs() + bound)
+    off = (got.double() - want).abs()
+    bad = ~(off <= bound)
+    assert not bad.any(), (int(bad.sum()), float(off.max()), float((off / bound).max()))
+
+
+def _check_rows(x, w, counts, transposed, dtype, y):
+    """y against x[i] @ w[e], zeros after the last group."""
+    K = x.shape[1]
+    want = torch.zeros(y.shape, dtype=torch.float64, device="cuda")
+    terms = torch.zeros_like(want)
+    for e, a, b in _bounds(counts):
+        m = w[e].double().t() if transposed else w[e].double()
+        want[a:b] = x[a:b].double() @ m
+        terms[a:b] = x[a:b].double().abs() @ m.abs()
+    _close(y, want, terms, K, dtype)
+
+
+def _check_wgrad(x, dy, counts, out, dw):
+    for e, a, b in _bounds(counts):
+        want = x[a:b].double().t() @ dy[a:b].double()
+        _close(dw[e], want, x[a:b].double().abs().t() @ dy[a:b].double().abs(), b - a, out)
+
+
+# counts of each expert, k, n: single rows, tiles that end inside, empty experts at either end
+# and between, more experts than a wave has lanes, sizes off every multiple
+CASES = [
+    ([1], 1, 1), ([1], 8, 8), ([0], 64, 64), ([3, 0, 2], 5, 7), ([0, 1, 0, 0, 1], 64, 128),
+    ([17, 64, 1, 130], 96, 72), ([0, 65, 0, 63, 200, 0], 100, 136), ([256, 512], 64, 256),
+    ([300, 1, 0, 255, 257], 200, 264), ([1] * 70 + [0] * 60 + [5] * 10, 72, 40), ([700], 515, 777),
+    ([31, 33], 1000, 24), ([129, 127], 24, 1000), ([400, 0, 112], 768, 520), ([2, 3, 1, 2], 1024, 2048),
+    ([9, 15, 0, 8, 40], 264, 520), ([1000, 24], 320, 384), ([513, 600], 576, 1032),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_products(case, dtype):
+    counts, k, n = CASES[case]
+    log(f"case: expert products {len(counts)} experts, {sum(counts)} rows, {k} x {n} {dtype}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(case)
+    rows = sum(counts)
+    x, dy = _randn(g, (rows, k), dtype), _randn(g, (rows, n), dtype)
+    w = _randn(g, (len(counts), k, n), dtype)
+    ends = _ends(counts)
+    _check_rows(x, w, counts, False, dtype, tm.expert_matmul(x, w, ends))
+    _check_rows(dy, w, counts, True, dtype, tm.expert_matmul(dy, w, ends, transposed=True))
+    dw = tm.expert_wgrad(x, dy, ends)
+    assert dw.dtype == torch.float32
+    _check_wgrad(x, dy, counts, "f32", dw)
+    if dtype == "bf16":
+        _check_wgrad(x, dy, counts, "bf16", tm.expert_wgrad(x, dy, ends, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_no_expert_are_zero(dtype):
+    log("case: rows after the last expert's")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    for counts, rows in (([100, 0, 60], 400), ([0, 0], 70), ([5, 3], 9)):
+        x, dy = _randn(g, (rows, 128), dtype), _randn(g, (rows, 192), dtype)
+        w = _randn(g, (len(counts), 128, 192), dtype)
+        x[sum(counts):] = float("nan")   # whatever the padding holds
+        dy[sum(counts):] = float("inf")
+        y = tm.expert_matmul(x, w, _ends(counts))
+        assert not y[sum(counts):].any()
+        _check_rows(x, w, counts, False, dtype, y)
+        _check_wgrad(x, dy, counts, "f32", tm.expert_wgrad(x, dy, _ends(counts)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k,n", [(128, 256), (200, 136), (75, 53)])
+def test_nan_and_inf_stay_with_their_expert(k, n, dtype):
+    """A neighbour's NaN must not reach a tile through rows that are loaded and not used."""
+    log(f"case: NaN in one expert's rows and matrix {k} x {n} {dtype}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    counts = [70, 33, 130]
+    x, dy = _randn(g, (233, k), dtype), _randn(g, (233, n), dtype)
+    w = _randn(g, (3, k, n), dtype)
+    ends = _ends(counts)
+    ref = tm.expert_matmul(x, w, ends), tm.expert_matmul(dy, w, ends, transposed=True), tm.expert_wgrad(x, dy, ends)
+    x[70:103] = float("nan")
+    dy[70:103] = float("inf")
+    w[1] = float("nan")
+    got = tm.expert_matmul(x, w, ends), tm.expert_matmul(dy, w, ends, transposed=True), tm.expert_wgrad(x, dy, ends)
+    for a, b in zip(ref[:2], got[:2]):
+        assert torch.equal(a[:70], b[:70]) and torch.equal(a[103:], b[103:]) and not b[70:103].isfinite().any()
+    for e in (0, 2):
+        assert torch.equal(ref[2][e], got[2][e])
+    assert not got[2][1].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides(dtype):
+    log("case: expert products on strided operands")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    counts, k, n = [90, 0, 45, 200], 128, 192
+    for pad in (64, 3):                       # 16-byte rows, and rows at any element
+        xw = _randn(g, (335, k + pad), dtype)
+        dyw = _randn(g, (335, n + pad), dtype)
+        ww = _randn(g, (4, k + 2, n + pad), dtype)
+        off = pad // 2
+        x, dy, w = xw[:, off:off + k], dyw[:, off:off + n], ww[:, 1:k + 1, off:off + n]
+        ends = _ends(counts)
+        _check_rows(x, w, counts, False, dtype, tm.expert_matmul(x, w, ends))
+        _check_rows(dy, w, counts, True, dtype, tm.expert_matmul(dy, w, ends, transposed=True))
+        _check_wgrad(x, dy, counts, "f32", tm.expert_wgrad(x, dy, ends))
+        turned = w.transpose(1, 2)            # columns contiguous: copied
+        _check_rows(x, turned, counts, True, dtype, tm.expert_matmul(x, turned, ends, transposed=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_results_do_not_depend_on_what_else_is_in_the_call(dtype):
+    """Bits of an expert's product: in a call of its own, and among others at another place."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    counts = [40, 100, 7]
+    x, w = _randn(g, (147, 256), dtype), _randn(g, (3, 256, 128), dtype)
+    y = tm.expert_matmul(x, w, _ends(counts))
+    again = tm.expert_matmul(x, w, _ends(counts))
+    assert torch.equal(y, again)
+    for e, a, b in _bounds(counts):
+        assert torch.equal(y[a:b], tm.expert_matmul(x[a:b].clone(), w[e:e + 1], _ends([b - a])))
+
+
+def test_offsets_past_32_bits():
+    """Rows and matrices whose element offsets pass 2^31."""
+    log("case: expert products past 2^31 elements")
+    rows, k, n = 40000, 65536, 24          # x: 2.6e9 elements, 5.2 GB
+    x = torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x[-300:] = _randn(g, (300, k), "bf16")
+    w = _randn(g, (2, k, n), "bf16", 0.1)
+    ends = _ends([rows - 200, 200])
+    y = tm.expert_matmul(x, w, ends)
+    want = torch.cat([x[-300:-200].double() @ w[0].double(), x[-200:].double() @ w[1].double()])
+    terms = torch.cat([x[-300:-200].double().abs() @ w[0].double().abs(), x[-200:].double().abs() @ w[1].double().abs()])
+    _close(y[-300:], want, terms, k, "bf16")
+    assert not y[:-300].any()
+    dy = _randn(g, (rows, n), "bf16")
+    dw = tm.expert_wgrad(x, dy, ends)
+    for e, rng in ((0, slice(-300, -200)), (1, slice(-200, None))):
+        _close(dw[e], x[rng].double().t() @ dy[rng].double(), x[rng].double().abs().t() @ dy[rng].double().abs(), rows, "f32")
+
+
+def test_ends_that_make_no_sense_stay_in_bounds():
+    """Decreasing or too large ends: the rows that they reach are computed, nothing else is touched."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x, w = _randn(g, (100, 64), "bf16"), _randn(g, (3, 64, 64), "bf16")
+    guard = torch.full((300, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    for ends in ([50, 20, 1000], [-5, 100, 90], [2 ** 31 - 1, -2 ** 31, 5]):
+        e = torch.tensor(ends, dtype=torch.int32, device="cuda")
+        guard.fill_(7.0)
+        out = guard[100:200]
+        assert tm.lib().tm_expert_matmul(x.data_ptr(), 64, w.data_ptr(), 64, 4096, e.data_ptr(), out.data_ptr(), 64,
+                                         100, 3, 64, 64, 0, 0, s) == 0
+        assert (guard[:100] == 7).all() and (guard[200:] == 7).all()
+        tm.expert_wgrad(x, x, e)
+    torch.cuda.synchronize()
+
+
+def test_gradients_against_differences():
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    counts = [5, 0, 9, 2]
+    x = _randn(g, (16, 24), "f32").requires_grad_()
+    w = _randn(g, (4, 24, 10), "f32").requires_grad_()
+    dy = _randn(g, (16, 10), "f32")
+    ops.expert_linear(x, w, _ends(counts)).backward(dy)
+
+    def value(x, w):
+        return sum(float((x[a:b] @ w[e] * dy[a:b].double()).sum()) for e, a, b in _bounds(counts))
+
+    pick = torch.Generator().manual_seed(0)
+    for k, leaf in enumerate((x, w)):
+        for _ in range(8):
+            i = int(torch.randint(leaf.numel(), (), generator=pick))
+            args = [t.detach().double().clone() for t in (x, w)]
+            flat = args[k].view(-1)
+            flat[i] += 1e-3
+            up = value(*args)
+            flat[i] -= 2e-3
+            diff = (up - value(*args)) / 2e-3
+            assert abs(float(leaf.grad.reshape(-1)[i]) - diff) <= 1e-4 * (1 + abs(diff))
+
+
+def test_fp32_matrices_with_bf16_rows():
+    """The optimizer's fp32 parameters: rounded for the products, their gradient in fp32."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    counts = [64, 100]
+    x = _randn(g, (164, 128), "bf16").requires_grad_()
+    w = _randn(g, (2, 128, 64), "f32").requires_grad_()
+    y = ops.expert_linear(x, w, _ends(counts))
+    _check_rows(x.detach(), w.detach().bfloat16(), counts, False, "bf16", y.detach())
+    y.backward(y.detach())
+    assert w.grad.dtype == torch.float32 and x.grad.dtype == torch.bfloat16
+    _check_wgrad(x.detach(), y.detach(), counts, "f32", w.grad)
+
+
+def test_refusals():
+    x = torch.zeros((10, 16), device="cuda")
+    w = torch.zeros((2, 16, 8), device="cuda")
+    ends = _ends([4, 6])
+    for bad in (lambda: tm.expert_matmul(x.cpu(), w, ends), lambda: tm.expert_matmul(x, w[0], ends),
+                lambda: tm.expert_matmul(x, w, ends, transposed=True), lambda: tm.expert_matmul(x, w.bfloat16(), ends),
+                lambda: tm.expert_matmul(x, w, ends.long()), lambda: tm.expert_matmul(x, w, ends[:1]),
+                lambda: tm.expert_matmul(x, w, ends.cpu()), lambda: tm.expert_matmul(x.half(), w.half(), ends),
+                lambda: tm.expert_wgrad(x, x[:5], ends), lambda: tm.expert_wgrad(x, x.bfloat16(), ends)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(tm.TurboMuonError) as e:
+        tm.expert_wgrad(x, x, ends, dtype=torch.bfloat16)   # fp32 rows, bf16 out
+    assert e.value.status == tm.TM_ERR_UNSUPPORTED
+    assert tm.expert_matmul(x[:0], w, _ends([0, 0])).shape == (0, 8)
+    assert not tm.expert_wgrad(x[:0], x[:0], _ends([0, 0])).any()
