@@ -54,6 +54,7 @@ def build(verbose: bool = False) -> str:
             (os.path.join(CSRC, "tm_norm.hip"), [], "norm.o"),
             (os.path.join(CSRC, "tm_loss.hip"), [], "loss.o"),
             (os.path.join(CSRC, "tm_expert.hip"), [], "expert.o"),
+            (os.path.join(CSRC, "tm_expert_tiles.hip"), [], "expert_tiles.o"),
             (os.path.join(CSRC, "tm_ops.cpp"), [], "ops.o"),
             (os.path.join(CSRC, "tm_api.cpp"), [], "api.o"),
         ]

@@ -12,7 +12,7 @@
 #include <algorithm>
 
 #include "tm_elem.h"
-#include "tm_ops.h"
+#include "tm_expert.h"
 
 namespace tmk {
 namespace expert {
@@ -22,50 +22,6 @@ using elem::F32;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-// A run of rows [first, last) of one expert (experts: the rows of none).
-struct Group {
-  int e, first, last;
-};
-
-// First and last row of group e.  Whatever `ends` holds, the rows stay within the matrix.
-__device__ inline Group group_of(const ExpertArgs& A, int e) {
-  Group g;
-  g.e = e;
-  g.first = e == 0 ? 0 : min(max(A.ends[e - 1], 0), A.rows);
-  g.last = e == A.experts ? A.rows : min(max(A.ends[e], g.first), A.rows);
-  return g;
-}
-
-// Row tile `tile` (of T rows) of the launch: its group cut to the tile's rows.
-// Every lane of a wave calls it; the lanes look at 64 groups at a time.  False
-// past the last tile.
-template <int T>
-__device__ inline bool find_tile(const ExpertArgs& A, int tile, Group& out) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;   // tiles of the groups looked at so far
-  for (int base = 0; base <= A.experts; base += 64) {
-    const int e = base + lane;
-    Group g{e, 0, 0};
-    if (e <= A.experts) g = group_of(A, e);
-    const int tiles = (g.last - g.first + T - 1) / T;
-    int sum = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    const uint64_t past = __ballot(before + sum > tile);
-    if (past != 0) {
-      const int src = __ffsll((unsigned long long)past) - 1;
-      const int first = __shfl(g.first, src) + (tile - before - __shfl(sum - tiles, src)) * T;
-      out = Group{base + src, first, min(first + T, __shfl(g.last, src))};
-      return true;
-    }
-    before += __shfl(sum, 63);
-  }
-  return false;
-}
 
 // ---------------------------------------------------------------- any size and alignment
 // 64 x 64 tiles by four waves in a 2 x 2 grid, both operands staged through
@@ -255,12 +211,23 @@ hipError_t wgrad_any(const ExpertArgs& A, hipStream_t st) {
 
 }  // namespace expert
 
+// Whether the tiles of tm_expert_tiles.hip take an operand or result: rows of
+// whole 16-byte pieces, and a stride that keeps a tile's byte offsets below 2^32.
+static bool whole(const char* p, int64_t ld, int width) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld < (int64_t(1) << 22);
+}
+
 hipError_t launch_expert_matmul(const ExpertArgs& A, bool f32, bool transposed, hipStream_t st) {
-  return f32 ? expert::matmul_any<elem::F32>(A, transposed, st) : expert::matmul_any<elem::Bf16>(A, transposed, st);
+  if (f32) return expert::matmul_any<elem::F32>(A, transposed, st);
+  const bool fits = whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) && A.stride_b % 8 == 0 &&
+                    whole(A.out, A.ldo, A.n);
+  return fits ? launch_expert_matmul_tiles(A, transposed, st) : expert::matmul_any<elem::Bf16>(A, transposed, st);
 }
 
 hipError_t launch_expert_wgrad(const ExpertArgs& A, bool f32, bool out_f32, hipStream_t st) {
   if (f32) return expert::wgrad_any<elem::F32, elem::F32>(A, st);
+  if (whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n))
+    return launch_expert_wgrad_tiles(A, out_f32, st);
   return out_f32 ? expert::wgrad_any<elem::Bf16, elem::F32>(A, st) : expert::wgrad_any<elem::Bf16, elem::Bf16>(A, st);
 }
 

@@ -49,6 +49,8 @@ struct ExpertArgs {
 };
 
 hipError_t launch_expert_matmul(const ExpertArgs& A, bool f32, bool transposed, hipStream_t st);
+hipError_t launch_expert_matmul_tiles(const ExpertArgs& A, bool transposed, hipStream_t st);
+hipError_t launch_expert_wgrad_tiles(const ExpertArgs& A, bool out_f32, hipStream_t st);
 hipError_t launch_expert_wgrad(const ExpertArgs& A, bool f32, bool out_f32, hipStream_t st);
 
 // ---------------------------------------------------------------- policy loss
