@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace tmk {
 namespace elem {
 
@@ -35,6 +37,10 @@ struct Bf16 {
     }
     return q;
   }
+  // element i of a vector that is zero there, from memory
+  __device__ static void put1(u32x4_t& q, int i, const char* p) {
+    q[i / 2] |= uint32_t(*reinterpret_cast<const uint16_t*>(p)) << (16 * (i % 2));
+  }
   __device__ static float load1(const char* p) {
     return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
   }
@@ -57,6 +63,7 @@ struct F32 {
     for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(v[i]);
     return q;
   }
+  __device__ static void put1(u32x4_t& q, int i, const char* p) { q[i] = *reinterpret_cast<const uint32_t*>(p); }
   __device__ static float load1(const char* p) { return *reinterpret_cast<const float*>(p); }
   __device__ static void store1(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
 };
@@ -73,6 +80,20 @@ __device__ inline void load_vec(const char* row, int first, int n, float fill, f
   }
 }
 
+// The same as stored, zeros past the end: what a row that is read ahead waits in.
+template <class T>
+__device__ inline u32x4_t load_raw(const char* row, int first, int n) {
+  u32x4_t q = {0u, 0u, 0u, 0u};
+  if (first + T::W <= n) {
+    q = T::load(row + int64_t(first) * T::kBytes);
+  } else {
+#pragma unroll
+    for (int i = 0; i < T::W; ++i)
+      if (first + i < n) T::put1(q, i, row + int64_t(first + i) * T::kBytes);
+  }
+  return q;
+}
+
 template <class T>
 __device__ inline void store_vec(char* row, int first, int n, const float* v) {
   if (first + T::W <= n) {
@@ -84,10 +105,21 @@ __device__ inline void store_vec(char* row, int first, int n, const float* v) {
   }
 }
 
+// Sum over the wave, in every lane: within rows of 16 lanes, then from row to
+// row, with data-parallel moves (no trip through LDS); lane 63 holds the total.
 __device__ inline float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  auto add = [&](auto ctrl, auto rows) {
+    v += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value,
+                                                     0xf, false));
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // row_shr:1
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});   // row_shr:2
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});   // row_shr:4
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});   // row_shr:8
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // row_bcast:15
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // row_bcast:31
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 }  // namespace elem

@@ -55,9 +55,21 @@ __device__ inline void load_cols(const float* p, float fill, int t, int d, float
 #pragma unroll
   for (int j = 0; j < E / T::W; ++j) {
     const int c = (j * NT + t) * T::W;
+    if (p != nullptr && c + T::W <= d) {
 #pragma unroll
-    for (int i = 0; i < T::W; ++i) v[j * T::W + i] = p != nullptr && c + i < d ? p[c + i] : fill;
+      for (int i = 0; i < T::W; i += F32::W) load_vec<F32>(reinterpret_cast<const char*>(p), c + i, d, fill, v + j * T::W + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) v[j * T::W + i] = p != nullptr && c + i < d ? p[c + i] : fill;
+    }
   }
+}
+
+// This thread's vectors of a row, as stored.
+template <int NT, int V, class T>
+__device__ inline void load_row(const char* row, int t, int d, u32x4_t (&q)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) q[j] = load_raw<T>(row, (j * NT + t) * T::W, d);
 }
 
 template <class T, int NT, int E>
@@ -69,15 +81,20 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) 
   float w[E], b[E];
   load_cols<NT, E, T>(A.weight, 1.f, t, d, w);
   load_cols<NT, E, T>(A.bias, 0.f, t, d, b);
-  for (int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT; r < A.rows; r += int64_t(gridDim.x) * RB) {
-    const char* x = A.x + r * A.ldx * T::kBytes;
+  const int64_t step = int64_t(gridDim.x) * RB;
+  int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT;
+  u32x4_t q[V];
+  if (r < A.rows) load_row<NT, V, T>(A.x + r * A.ldx * T::kBytes, t, d, q);
+  for (; r < A.rows; r += step) {
     float v[E], s[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      load_vec<T>(x, (j * NT + t) * W, d, 0.f, v + j * W);
+      T::unpack(q[j], v + j * W);
 #pragma unroll
       for (int i = 0; i < W; ++i) s[0] += v[j * W + i];
     }
+    // the next row is on its way while this one is summed
+    if (r + step < A.rows) load_row<NT, V, T>(A.x + (r + step) * A.ldx * T::kBytes, t, d, q);
     row_sum<NT>(s, slots[0]);
     const float mean = s[0] / n;
     s[0] = 0.f;
@@ -116,21 +133,32 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
   load_cols<NT, E, T>(A.weight, 1.f, t, d, w);
 #pragma unroll
   for (int i = 0; i < E; ++i) aw[i] = ab[i] = 0.f;
+  const int64_t step = int64_t(gridDim.x) * RB;
+  int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT;
+  u32x4_t qx[V], qy[V];
+  float mean = 0.f, rstd = 0.f;
+  auto read = [&](int64_t at) __attribute__((always_inline)) {
+    load_row<NT, V, T>(A.x + at * A.ldx * T::kBytes, t, d, qx);
+    load_row<NT, V, T>(A.dy + at * A.lddy * T::kBytes, t, d, qy);
+    mean = A.mean[at];
+    rstd = A.rstd[at];
+  };
+  constexpr bool kAhead = NT < 1024;   // 1024 threads have no registers for a second row
+  if (kAhead && r < A.rows) read(r);
   int turn = 0;
-  for (int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT; r < A.rows; r += int64_t(gridDim.x) * RB) {
-    const char* x = A.x + r * A.ldx * T::kBytes;
-    const char* dy = A.dy + r * A.lddy * T::kBytes;
-    const float mean = A.mean[r], rstd = A.rstd[r];
+  for (; r < A.rows; r += step) {
+    if (!kAhead) read(r);
     float h[E], g[E], s[2] = {0.f, 0.f};
+    const float scale = rstd;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int c = (j * NT + t) * W;
-      load_vec<T>(x, c, d, mean, h + j * W);
-      load_vec<T>(dy, c, d, 0.f, g + j * W);
+      T::unpack(qx[j], h + j * W);
+      T::unpack(qy[j], g + j * W);
 #pragma unroll
       for (int i = 0; i < W; ++i) {
         const int e = j * W + i;
-        h[e] = (h[e] - mean) * rstd;
+        h[e] = c + i < d ? (h[e] - mean) * rstd : 0.f;
         aw[e] += g[e] * h[e];
         ab[e] += g[e];
         g[e] *= w[e];
@@ -138,6 +166,7 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
         s[1] += g[e] * h[e];
       }
     }
+    if (kAhead && r + step < A.rows) read(r + step);   // on its way while this row is summed
     row_sum<NT>(s, slots[turn]);
     turn ^= 1;
     const float m0 = s[0] / n, m1 = s[1] / n;
@@ -146,7 +175,7 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
     for (int j = 0; j < V; ++j) {
       float o[W];
 #pragma unroll
-      for (int i = 0; i < W; ++i) o[i] = rstd * (g[j * W + i] - m0 - h[j * W + i] * m1);
+      for (int i = 0; i < W; ++i) o[i] = scale * (g[j * W + i] - m0 - h[j * W + i] * m1);
       store_vec<T>(dx, (j * NT + t) * W, d, o);
     }
   }
@@ -289,23 +318,28 @@ __global__ __launch_bounds__(256) void k_norm_columns(const NormArgs A, int slic
   part[A.d + c] = ab;
 }
 
-// out[c] = sum of the blocks' partial sums of column c: 32 columns a block,
-// eight threads each.
-__global__ __launch_bounds__(256) void k_norm_params(const float* part, int blocks, int d, float* dweight,
-                                                     float* dbias) {
+// out[c] = sum of the blocks' partial sums of column c: 32 columns a block, 32
+// threads each.
+__global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blocks, int d, float* dweight,
+                                                      float* dbias) {
   float* out = blockIdx.y == 0 ? dweight : dbias;
   if (out == nullptr) return;
-  __shared__ float sums[8][32];
+  constexpr int G = 32;
+  __shared__ float sums[G][33];
   const int lc = threadIdx.x & 31, grp = threadIdx.x >> 5, c = blockIdx.x * 32 + lc;
   float s = 0.f;
-  if (c < d)
-    for (int b = grp; b < blocks; b += 8) s += part[(int64_t(b) * 2 + blockIdx.y) * d + c];
-  sums[grp][lc] = s;
-  __syncthreads();
-  if (grp == 0 && c < d) {
-    for (int q = 1; q < 8; ++q) s += sums[q][lc];
-    out[c] = s;
+  if (c < d) {
+#pragma unroll 4
+    for (int b = grp; b < blocks; b += G) s += part[(int64_t(b) * 2 + blockIdx.y) * d + c];
   }
+  sums[lc][grp] = s;
+  __syncthreads();
+  // a half wave per column
+  s = sums[grp][lc];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  const int col = blockIdx.x * 32 + grp;
+  if (lc == 0 && col < d) out[col] = s;
 }
 
 constexpr int kMostBlocks = 2048;   // 8 workgroups of 256 threads per compute unit
@@ -374,7 +408,7 @@ hipError_t launch_norm_backward(const NormArgs& A, bool f32, int blocks, hipStre
 
 hipError_t launch_norm_params(const float* part, int blocks, int d, float* dweight, float* dbias,
                               hipStream_t st) {
-  hipLaunchKernelGGL(norm::k_norm_params, dim3((d + 31) / 32, 2), dim3(256), 0, st, part, blocks, d, dweight, dbias);
+  hipLaunchKernelGGL(norm::k_norm_params, dim3((d + 31) / 32, 2), dim3(1024), 0, st, part, blocks, d, dweight, dbias);
   return hipGetLastError();
 }
 
