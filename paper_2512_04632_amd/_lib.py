@@ -269,247 +269,6 @@ def muon_step_grouped(params: Sequence, grads: Sequence, bufs: Sequence, lr: flo
     _check("tm_muon_step_grouped", st)
 
 
-# ------------------------------------------------------------------ operators
-
-def _dtype_code(t, name: str) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return DTYPE_BF16
-    if t.dtype is torch.float32:
-        return DTYPE_F32
-    raise ValueError(f"{name} must be bfloat16 or float32")
-
-
-def _rows(t, name: str):
-    """t as (tensor, rows, width, row stride): any leading dimensions that lie at one stride
-    (others are copied), the last one contiguous."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dim() < 1:
-        raise ValueError(f"{name} must have at least one dimension")
-    d = t.shape[-1]
-    if t.dim() != 2:
-        t = t.reshape(-1, d) if d else t.reshape(t.shape[:-1].numel(), 0)
-    rows = t.shape[0]
-    ld = t.stride(0)
-    if (d > 1 and t.stride(1) != 1) or (rows > 1 and ld < d):
-        t = t.contiguous()
-        ld = d
-    return t, rows, d, max(ld, d)
-
-
-def _same(t, like, name: str, shape, dtype=None):
-    """Checks a companion tensor: device, shape, and type where one is asked for."""
-    if t.device != like.device:
-        raise ValueError(f"{name} must be on the same device")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if dtype is not None and t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}")
-
-
-def _vector(t, like, name: str, n: int, dtype):
-    _same(t, like, name, (n,), dtype)
-    return t if t.is_contiguous() else t.contiguous()
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _call(fn: str, device, stream, *args) -> None:
-    """An operator's entry point on `device`, its last argument the stream."""
-    import torch
-    f = getattr(lib(), fn)
-    if device.index == torch.cuda.current_device():
-        if stream is None:
-            handle = torch._C._cuda_getCurrentRawStream(device.index)
-        else:
-            handle = stream.cuda_stream
-        st = f(*args, handle)
-    else:
-        with torch.cuda.device(device):
-            if stream is None:
-                stream = torch.cuda.current_stream(device)
-            st = f(*args, stream.cuda_stream)
-    if st != TM_OK:
-        raise TurboMuonError(fn, st, last_error())
-
-
-def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
-    """Layer norm over the last dimension of x (bf16 or fp32, any strides between rows).
-
-    weight and bias are fp32 vectors or None.  Returns (y, mean, rstd): y of x's shape and
-    type, mean and rstd fp32, one per row.
-    """
-    import torch
-    code = _dtype_code(x, "x")
-    rows_of, rows, d, ld = _rows(x, "x")
-    f32 = torch.float32
-    if weight is not None:
-        weight = _vector(weight, x, "weight", d, f32)
-    if bias is not None:
-        bias = _vector(bias, x, "bias", d, f32)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean, rstd = torch.empty((2, rows), dtype=f32, device=x.device).unbind(0)
-    _call("tm_layer_norm", x.device, stream, rows_of.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
-          mean.data_ptr(), rstd.data_ptr(), rows, d, eps, code)
-    return y, mean, rstd
-
-
-def layer_norm_backward(dy, x, mean, rstd, weight=None, param_grads: bool = True, stream=None):
-    """Gradients of layer_norm: (dx, dweight, dbias), the last two fp32, or None without
-    param_grads.  mean and rstd are layer_norm's; dy has x's shape and type."""
-    import torch
-    code = _dtype_code(x, "x")
-    _same(dy, x, "dy", x.shape, x.dtype)
-    x2, rows, d, ldx = _rows(x, "x")
-    dy2, _, _, lddy = _rows(dy, "dy")
-    f32 = torch.float32
-    mean, rstd = _vector(mean, x, "mean", rows, f32), _vector(rstd, x, "rstd", rows, f32)
-    if weight is not None:
-        weight = _vector(weight, x, "weight", d, f32)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dweight = dbias = None
-    if param_grads:
-        dweight, dbias = torch.empty((2, d), dtype=f32, device=x.device).unbind(0)
-    _call("tm_layer_norm_backward", x.device, stream, dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
-          mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), d, _ptr(dweight), _ptr(dbias), rows, d, code)
-    return dx, dweight, dbias
-
-
-def _matrices(w, like, name: str):
-    """Stacked matrices as (tensor, row stride, matrix stride), the last dimension contiguous."""
-    if w.dim() != 3:
-        raise ValueError(f"{name} must be (experts, rows, columns)")
-    if w.device != like.device or w.dtype is not like.dtype:
-        raise ValueError(f"{name} must have x's type and device")
-    e, r, c = w.shape
-    if (c > 1 and w.stride(2) != 1) or (r > 1 and w.stride(1) < c) or \
-            (e > 1 and w.stride(0) < (r - 1) * w.stride(1) + c):
-        w = w.contiguous()
-    return w, max(w.stride(1), c), w.stride(0) if e > 1 else 0
-
-
-def _ends(ends, like):
-    import torch
-    if ends.dim() != 1 or ends.dtype is not torch.int32 or ends.device != like.device:
-        raise ValueError("ends must be an int32 vector on x's device")
-    return ends if ends.is_contiguous() else ends.contiguous()
-
-
-def expert_matmul(x, w, ends, transposed: bool = False, stream=None):
-    """y[i] = x[i] @ w[e] for the rows of each expert e (w[e].T with transposed).
-
-    x is (rows, k), bf16 or fp32, rows sorted by expert; w is (experts, k, n), or (experts, n, k)
-    with transposed; ends is an int32 device vector, ends[e] the number of rows up to expert e's
-    last.  Rows after ends[-1] come out as zeros.  Nothing is synchronised.
-    """
-    import torch
-    code = _dtype_code(x, "x")
-    if x.dim() != 2:
-        raise ValueError("x must be (rows, k)")
-    x, rows, k, ldx = _rows(x, "x")
-    w, ldw, stride_w = _matrices(w, x, "w")
-    experts, n = w.shape[0], w.shape[1 if transposed else 2]
-    if w.shape[2 if transposed else 1] != k:
-        raise ValueError(f"w's matrices of {tuple(w.shape[1:])} do not fit rows of {k}")
-    ends = _ends(ends, x)
-    if ends.shape[0] != experts:
-        raise ValueError("ends must hold one entry per expert")
-    y = torch.empty((rows, n), dtype=x.dtype, device=x.device)
-    _call("tm_expert_matmul", x.device, stream, x.data_ptr(), ldx, w.data_ptr(), ldw, stride_w, ends.data_ptr(),
-          y.data_ptr(), n, rows, experts, k, n, 1 if transposed else 0, code)
-    return y
-
-
-def expert_wgrad(x, dy, ends, dtype=None, stream=None):
-    """dw[e] = x_e.T @ dy_e for the rows of each expert: (experts, k, n), fp32 unless dtype says
-    bf16 (for bf16 rows).  Experts without rows get zeros."""
-    import torch
-    code = _dtype_code(x, "x")
-    if x.dim() != 2 or dy.dim() != 2:
-        raise ValueError("x and dy must be (rows, k) and (rows, n)")
-    _same(dy, x, "dy", (x.shape[0], dy.shape[1]), x.dtype)
-    x, rows, k, ldx = _rows(x, "x")
-    dy, _, n, lddy = _rows(dy, "dy")
-    ends = _ends(ends, x)
-    experts = ends.shape[0]
-    dw = torch.empty((experts, k, n), dtype=dtype or torch.float32, device=x.device)
-    _call("tm_expert_wgrad", x.device, stream, x.data_ptr(), ldx, dy.data_ptr(), lddy, ends.data_ptr(), dw.data_ptr(),
-          n, k * n if experts > 1 else 0, rows, experts, k, n, code, _dtype_code(dw, "dtype"))
-    return dw
-
-
-def _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl, temperature,
-                 stream, grad: bool, keep: bool):
-    import torch
-    code = _dtype_code(logits, "logits")
-    if logits.dim() != 2:
-        raise ValueError("logits must be (rows, vocabulary)")
-    logits, rows, vocab, ld = _rows(logits, "logits")
-    f32 = torch.float32
-    targets = _vector(targets, logits, "targets", rows, torch.int64)
-    old_logp = _vector(old_logp, logits, "old_logp", rows, f32)
-    advantages = _vector(advantages, logits, "advantages", rows, f32)
-    weights = _vector(weights, logits, "weights", rows, f32)
-    if ref_logp is not None:
-        ref_logp = _vector(ref_logp, logits, "ref_logp", rows, f32)
-    loss = torch.empty((), dtype=f32, device=logits.device)
-    dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device) if grad else None
-    if keep:
-        logp, lse, slope = torch.empty((3, rows), dtype=f32, device=logits.device).unbind(0)
-    else:
-        logp, lse, slope = torch.empty(rows, dtype=f32, device=logits.device), None, None
-    _call("tm_policy_loss", logits.device, stream, logits.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
-          advantages.data_ptr(), weights.data_ptr(), _ptr(ref_logp), clip_low, clip_high, kl, temperature,
-          loss.data_ptr(), logp.data_ptr(), _ptr(lse), _ptr(slope), _ptr(dlogits), vocab, rows, vocab, code)
-    return loss, logp, lse, slope, dlogits
-
-
-def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low: float = 0.2,
-                clip_high: float = 0.2, kl: float = 0.0, temperature: float = 1.0, stream=None):
-    """Clipped policy loss with a KL term over (rows, vocabulary) logits, bf16 or fp32:
-
-        sum weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (q - log q - 1)),
-        r = exp(logp - old_logp), q = exp(ref_logp - logp)
-
-    with logp the log probability of each row's int64 target at the temperature.  The other
-    vectors are fp32, one entry per row; ref_logp None leaves the KL term out.  Rows of weight 0
-    or with a negative target take no part.  Returns (loss, logp, lse, slope): the last two are
-    what policy_loss_backward takes.
-    """
-    return _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl,
-                        temperature, stream, False, True)[:4]
-
-
-def policy_loss_with_grad(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low: float = 0.2,
-                          clip_high: float = 0.2, kl: float = 0.0, temperature: float = 1.0, stream=None):
-    """policy_loss and its gradient in one pass: (loss, logp, dlogits)."""
-    loss, logp, _, _, dlogits = _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_low,
-                                             clip_high, kl, temperature, stream, True, False)
-    return loss, logp, dlogits
-
-
-def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: float = 1.0, stream=None):
-    """Gradient by the logits from policy_loss's lse and slope, times grad (an fp32 scalar on the
-    device; None: 1)."""
-    import torch
-    code = _dtype_code(logits, "logits")
-    if logits.dim() != 2:
-        raise ValueError("logits must be (rows, vocabulary)")
-    logits, rows, vocab, ld = _rows(logits, "logits")
-    targets = _vector(targets, logits, "targets", rows, torch.int64)
-    lse = _vector(lse, logits, "lse", rows, torch.float32)
-    slope = _vector(slope, logits, "slope", rows, torch.float32)
-    if grad is not None:
-        _same(grad, logits, "grad", (), torch.float32)
-    dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-    _call("tm_policy_loss_backward", logits.device, stream, logits.data_ptr(), ld, targets.data_ptr(),
-          lse.data_ptr(), slope.data_ptr(), _ptr(grad), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
-    return dlogits
-
-
 def schedule_tail(schedule: Sequence, iters: int) -> list:
     """The rows of a coefficient schedule that a call with `iters` iterations runs
     (tm_schedule_tail: the last `iters` rows)."""
@@ -549,3 +308,18 @@ def timing_read(phase: str):
     n = ctypes.c_int64(0)
     _check("tm_timing_read", lib().tm_timing_read(PHASES[phase], ctypes.byref(ms), ctypes.byref(n)))
     return ms.value, n.value
+
+
+# The operators around the optimizer live in _operators (which needs torch from its first line
+# on); here they are found by name.
+_OPERATORS = ("layer_norm", "layer_norm_backward", "expert_matmul", "expert_wgrad", "policy_loss",
+              "policy_loss_with_grad", "policy_loss_backward")
+
+
+def __getattr__(name: str):
+    if name not in _OPERATORS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import _operators
+    for op in _OPERATORS:
+        globals()[op] = getattr(_operators, op)
+    return globals()[name]

@@ -55,6 +55,7 @@ def build(verbose: bool = False) -> str:
             (os.path.join(CSRC, "tm_loss.hip"), [], "loss.o"),
             (os.path.join(CSRC, "tm_expert.hip"), [], "expert.o"),
             (os.path.join(CSRC, "tm_expert_tiles.hip"), [], "expert_tiles.o"),
+            (os.path.join(CSRC, "tm_expert_staged.hip"), [], "expert_staged.o"),
             (os.path.join(CSRC, "tm_ops.cpp"), [], "ops.o"),
             (os.path.join(CSRC, "tm_api.cpp"), [], "api.o"),
         ]

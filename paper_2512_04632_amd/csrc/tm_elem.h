@@ -80,17 +80,42 @@ __device__ inline void load_vec(const char* row, int first, int n, float fill, f
   }
 }
 
-// The same as stored, zeros past the end: what a row that is read ahead waits in.
-template <class T>
-__device__ inline u32x4_t load_raw(const char* row, int first, int n) {
+// Elements first .. first + W - 1 of a row of n as stored, for a row that is read
+// ahead: a load whose value nothing waits for.  What comes back past the row's
+// end is for `settle` to put right when the row's turn comes.
+//   TAIL = false  n is a multiple of W: a vector is whole or wholly past the end
+//                 (then the row's last one is read again).
+//   TAIL          a vector that would end past the row is read from the row's
+//                 last W elements; rows of less than W are read one by one.
+template <class T, bool TAIL>
+__device__ inline u32x4_t load_ahead(const char* row, int first, int n) {
+  if constexpr (!TAIL) return T::load(row + int64_t(min(first, n - T::W)) * T::kBytes);
   u32x4_t q = {0u, 0u, 0u, 0u};
-  if (first + T::W <= n) {
-    q = T::load(row + int64_t(first) * T::kBytes);
-  } else {
-#pragma unroll
-    for (int i = 0; i < T::W; ++i)
-      if (first + i < n) T::put1(q, i, row + int64_t(first + i) * T::kBytes);
+  if (n >= T::W) {
+    if (first < n) q = T::load(row + int64_t(min(first, n - T::W)) * T::kBytes);
+    return q;
   }
+#pragma unroll
+  for (int i = 0; i < T::W; ++i)
+    if (first + i < n) T::put1(q, i, row + int64_t(first + i) * T::kBytes);
+  return q;
+}
+
+// The vector that load_ahead read, elements in their places and zeros past the end.
+template <class T, bool TAIL>
+__device__ inline u32x4_t settle(u32x4_t q, int first, int n) {
+  if constexpr (!TAIL) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = first < n ? q[i] : 0u;
+    return q;
+  }
+  const int by = first + T::W - n;   // elements past the end
+  if (by <= 0 || n < T::W) return q;
+  const int bits = min(by, T::W) * (8 * T::kBytes);   // down by this many of 128
+  if (bits & 16) q = u32x4_t{q[0] >> 16 | q[1] << 16, q[1] >> 16 | q[2] << 16, q[2] >> 16 | q[3] << 16, q[3] >> 16};
+  if (bits & 32) q = u32x4_t{q[1], q[2], q[3], 0u};
+  if (bits & 64) q = u32x4_t{q[2], q[3], 0u, 0u};
+  if (bits & 128) q = u32x4_t{0u, 0u, 0u, 0u};
   return q;
 }
 

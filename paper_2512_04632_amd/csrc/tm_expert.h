@@ -1,11 +1,20 @@
 // What the expert products' kernels share: the rows of each expert, found on
-// the device.
+// the device, the order of the tiles, operand reads and the output stage.
+//
+// The group sizes are only known on the device: a launch covers the most tiles
+// that any sizes can need, rows / T + experts + 1 rows of tiles, and each
+// workgroup finds its expert from `ends`; the ones left over end at once.
+// Rows after the last expert's belong to a group of their own without a
+// product and come out as zeros; so do the matrices of experts without rows.
 #pragma once
 
 #include "tm_ops.h"
+#include "tm_tile.h"
 
 namespace tmk {
 namespace expert {
+
+using namespace tile;
 
 // A run of rows [first, last) of one expert (experts: the rows of none).
 struct Group {
@@ -49,6 +58,103 @@ __device__ inline bool find_tile(const ExpertArgs& A, int tile, Group& out) {
     before += __shfl(sum, 63);
   }
   return false;
+}
+
+// Rows of T-row tiles that any group sizes can need.
+inline uint64_t row_tiles(const ExpertArgs& A, int T) { return uint64_t(A.rows) / T + uint64_t(A.experts) + 1; }
+inline uint64_t col_tiles(const ExpertArgs& A, int T) { return (uint64_t(A.n) + T - 1) / T; }
+inline uint64_t wgrad_tiles(const ExpertArgs& A, int T) {
+  return uint64_t(A.experts) * ((uint64_t(A.k) + T - 1) / T) * col_tiles(A, T);
+}
+
+// A workgroup's tile and its slice z of the summed index.
+struct Slice {
+  int id, z, slices;
+  // Slice of K values, in whole stages of `unit`: first value and number.
+  __device__ void range(int K, int unit, int& k0, int& n) const {
+    const int len = ((K + slices - 1) / slices + unit - 1) / unit * unit;
+    k0 = min(z * len, K);
+    n = min(len, K - k0);
+  }
+};
+__device__ inline Slice slice_of(const ExpertArgs& A, int block, int blocks) {
+  const int per = blocks / A.slices;
+  const int z = A.slices > 1 ? block / per : 0;
+  return Slice{xcd_remap(block - z * per, per), z, A.slices};
+}
+
+// Place of logical tile `id` in a grid of nI x nJ tiles, in groups of four rows
+// of tiles: tiles that run together share operand panels.
+struct Place {
+  int I, J;
+};
+__device__ inline Place place_of(int id, int nI, int nJ) {
+  constexpr int GM = 4;
+  const int grp = id / (GM * nJ), first = grp * GM, size = min(nI - first, GM);
+  const int rem = id - grp * GM * nJ;
+  return Place{first + rem % size, rem / size};
+}
+
+// Row-major a operand: the wave's block f of 16 columns is chunk wm FM + f of
+// the stage's rows; chunk ^ swizzle = ((wm FM) ^ swizzle) ^ f, since f < FM.
+template <int T, int BK>
+__device__ inline void load_frags_a_rm(Frags<T>& fr, const char* sa, int s, int wm) {
+  constexpr int FM = Tile<T>::FM;
+  const int lane = threadIdx.x & 63;
+  const int lr = lane & 15, g = lane >> 4;
+  const int rl = 8 * g + (lr >> 2);
+  const char* base = sa + (32 * s + rl) * (2 * T) + 8 * (lr & 3);
+  const int chunk = (wm * FM) ^ swz_y<T>(rl);
+#pragma unroll
+  for (int f = 0; f < FM; ++f) {
+    const char* p = base + 32 * (chunk ^ f);
+    s16x4_t v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4_t*)(lds_addr(p + h * 4 * (2 * T))));
+    fr.a[f] = __builtin_bit_cast(uint4, v);
+  }
+}
+
+template <int T, int BK, bool ARM, bool BRM>
+__device__ inline void load_pair(Frags<T>& fr, const char* sa, const char* sb, int s, int wm, int wn) {
+  if constexpr (ARM) load_frags_a_rm<T, BK>(fr, sa, s, wm);
+  else load_frags_a<T, BK>(fr, sa, s, wm);
+  load_frags_b<T, BRM, BK>(fr, sb, s, wn);
+}
+
+// Bytes of a row of the output stage: 16 more than a tile's row, so that the
+// 16 rows that a wave writes at a time start in different banks.
+template <int T>
+constexpr int kStageRow = 2 * T + 16;
+
+// Row and first of the four columns that a lane holds of block (fm, fn).
+template <int T>
+__device__ inline int out_row(int fm) {
+  const int wave = threadIdx.x >> 6;
+  return (wave / Tile<T>::WGN) * Tile<T>::TWM + 16 * fm + int(threadIdx.x & 15);
+}
+template <int T, bool BRM>
+__device__ inline int out_col(int fn) {
+  const int wn = int(threadIdx.x >> 6) % Tile<T>::WGN;
+  return (BRM ? 16 * (fn * Tile<T>::WGN + wn) : wn * Tile<T>::TWN + 16 * fn) + 4 * (int(threadIdx.x & 63) >> 4);
+}
+
+// The tile's bf16 values in LDS, rows of kStageRow bytes; ends with a barrier.
+template <int T, class FCol>
+__device__ inline void stage_bf16(const AccT<T>& acc, char* smem, FCol col) {
+#pragma unroll
+  for (int fm = 0; fm < Tile<T>::FM; ++fm)
+#pragma unroll
+    for (int fn = 0; fn < Tile<T>::FN; ++fn) {
+      uint32_t o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = f2bf(acc[fm][fn][u]);
+      *reinterpret_cast<uint2*>(smem + out_row<T>(fm) * kStageRow<T> + col(fn) * 2) =
+          make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+    }
+  __syncthreads();
 }
 
 }  // namespace expert

@@ -1,234 +1,148 @@
-// Products of ragged groups of rows with one matrix per expert, for gfx950.
-// Rows are sorted by expert; expert e owns rows ends[e - 1] .. ends[e] - 1.
+// Products of ragged groups of rows with one matrix per expert, for gfx950: how
+// a call is run, and the sum of slices where the summed index is split.
 //
 //   matmul   out[i, :] = a[i, :] W[e(i)]        (W: k x n, or n x k transposed)
 //   wgrad    out[e] = a_e^T b_e                 (k x n, the rows are summed over)
 //
-// The group sizes are only known on the device: a launch covers the most tiles
-// that any sizes can need, ceil(rows / T) + experts + 1 row tiles, and each
-// workgroup finds its expert from `ends`; the ones left over end at once.
-// Rows after the last expert's belong to a group of their own without a
-// product and come out as zeros; so do the matrices of experts without rows.
+// bf16 operands with 16-byte rows: tm_expert_tiles.hip; the others and fp32:
+// tm_expert_staged.hip.
 #include <algorithm>
 
 #include "tm_elem.h"
-#include "tm_expert.h"
+#include "tm_ops.h"
 
 namespace tmk {
 namespace expert {
 
-using elem::Bf16;
-using elem::F32;
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-// ---------------------------------------------------------------- any size and alignment
-// 64 x 64 tiles by four waves in a 2 x 2 grid, both operands staged through
-// registers into LDS as rows of BK values of the summed index, element by
-// element with bounds checks.  fp32 multiplies with v_mfma_f32_16x16x4_f32,
-// bf16 with v_mfma_f32_16x16x32_bf16.
-template <class T>
-struct Any;
-template <>
-struct Any<Bf16> {
-  typedef uint16_t E;
-  static constexpr int BK = 32, PAD = 8;
-  __device__ static E raw(const char* p) { return *reinterpret_cast<const E*>(p); }
-  __device__ static void step(f32x4_t (&acc)[2][2], const E* a, const E* b, int lr, int g) {
-    bf16x8_t fa[2], fb[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      fa[i] = *reinterpret_cast<const bf16x8_t*>(a + (16 * i + lr) * (BK + PAD) + 8 * g);
-      fb[i] = *reinterpret_cast<const bf16x8_t*>(b + (16 * i + lr) * (BK + PAD) + 8 * g);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-  }
-};
-template <>
-struct Any<F32> {
-  typedef float E;
-  static constexpr int BK = 16, PAD = 4;
-  __device__ static E raw(const char* p) { return *reinterpret_cast<const E*>(p); }
-  __device__ static void step(f32x4_t (&acc)[2][2], const E* a, const E* b, int lr, int g) {
-#pragma unroll
-    for (int s = 0; s < BK / 4; ++s) {
-      float fa[2], fb[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = a[(16 * i + lr) * (BK + PAD) + 4 * s + g];
-        fb[i] = b[(16 * i + lr) * (BK + PAD) + 4 * s + g];
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
-    }
-  }
-};
-
-constexpr int kAnyTile = 64;
-
-// One operand of the tile: R rows of the tile and K values of the summed
-// index are there.  KC: the summed index runs along the stored row; otherwise
-// the tile's rows do, and the stage is stored transposed.
-template <class T, bool KC>
-struct AnySide {
-  typedef typename Any<T>::E E;
-  static constexpr int BK = Any<T>::BK, LD = BK + Any<T>::PAD, N = kAnyTile * BK / 256;
-  const char* base;
-  int64_t ld;
-  int R, K;
-  E v[N];
-  __device__ void place(int i, int& r, int& k) const {
-    const int at = i * 256 + threadIdx.x;
-    if constexpr (KC) {
-      r = at / BK;
-      k = at % BK;
-    } else {
-      r = at % kAnyTile;
-      k = at / kAnyTile;
-    }
-  }
-  __device__ void load(int k0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int r, k;
-      place(i, r, k);
-      const bool in = r < R && k0 + k < K;
-      const int64_t at = KC ? r * ld + k0 + k : (k0 + k) * ld + r;
-      v[i] = in ? Any<T>::raw(base + at * int64_t(sizeof(E))) : E(0);
-    }
-  }
-  __device__ void store(E* lds) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int r, k;
-      place(i, r, k);
-      lds[r * LD + k] = v[i];
-    }
-  }
-};
-
-template <class T, bool AKC, bool BKC>
-__device__ inline void any_product(f32x4_t (&acc)[2][2], AnySide<T, AKC>& sa, AnySide<T, BKC>& sb, int K) {
-  typedef typename Any<T>::E E;
-  constexpr int BK = Any<T>::BK, LD = BK + Any<T>::PAD;
-  __shared__ __attribute__((aligned(16))) E la[kAnyTile * LD], lb[kAnyTile * LD];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const E* wa = la + (wave >> 1) * 32 * LD;
-  const E* wb = lb + (wave & 1) * 32 * LD;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  if (K <= 0) return;
-  sa.load(0);
-  sb.load(0);
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    __syncthreads();
-    sa.store(la);
-    sb.store(lb);
-    __syncthreads();
-    if (k0 + BK < K) {
-      sa.load(k0 + BK);
-      sb.load(k0 + BK);
-    }
-    Any<T>::step(acc, wa, wb, lane & 15, lane >> 4);
-  }
-}
-
+// out = sum of the slices' results, in their order, each thread a vector: rows
+// of n, `per` of them a matrix and the matrices `stride` elements apart.
 template <class TO>
-__device__ inline void any_store(const f32x4_t (&acc)[2][2], char* out, int64_t ld, int rows, int cols) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slices, char* out, int64_t ldo, int64_t per,
+                                                    int64_t stride, int64_t rows, int n) {
+  constexpr int W = elem::F32::W;
+  const int vecs = (n + W - 1) / W;
+  const int64_t slice = rows * n;
+  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t r = at / vecs;
+  if (r >= rows) return;
+  const int c = int(at - r * vecs) * W;
+  float s[W] = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < slices; ++z) {
+    float v[W];
+    elem::load_vec<elem::F32>(reinterpret_cast<const char*>(part + z * slice + r * n), c, n, 0.f, v);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < W; ++i) s[i] += v[i];
+  }
+  char* to = out + (r / per * stride + r % per * ldo + c) * TO::kBytes;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int r = (wave >> 1) * 32 + 16 * i + 4 * (lane >> 4) + u, c = (wave & 1) * 32 + 16 * j + (lane & 15);
-        if (r < rows && c < cols) TO::store1(out + (r * ld + c) * TO::kBytes, acc[i][j][u]);
-      }
+  for (int i = 0; i < W; ++i)
+    if (c + i < n) TO::store1(to + i * TO::kBytes, s[i]);
 }
 
-template <class T, bool TRANS>
-__global__ __launch_bounds__(256) void k_expert_any(const ExpertArgs A) {
-  const int tiles_n = (A.n + kAnyTile - 1) / kAnyTile;
-  Group g;
-  if (!find_tile<kAnyTile>(A, int(blockIdx.x / uint32_t(tiles_n)), g)) return;
-  const int c0 = int(blockIdx.x % uint32_t(tiles_n)) * kAnyTile;
-  const int K = g.e < A.experts ? A.k : 0;
-  const int cols = min(kAnyTile, A.n - c0), rows = g.last - g.first;
-  AnySide<T, true> sa{A.a + g.first * A.lda * T::kBytes, A.lda, rows, K, {}};
-  AnySide<T, TRANS> sb{A.b + (K > 0 ? g.e * A.stride_b + (TRANS ? c0 * A.ldb : int64_t(c0)) : 0) * T::kBytes,
-                       A.ldb, cols, K, {}};
-  f32x4_t acc[2][2];
-  any_product<T, true, TRANS>(acc, sa, sb, K);
-  any_store<T>(acc, A.out + (g.first * A.ldo + c0) * T::kBytes, A.ldo, rows, cols);
-}
-
-template <class T, class TO>
-__global__ __launch_bounds__(256) void k_wgrad_any(const ExpertArgs A) {
-  const uint32_t tiles_n = (A.n + kAnyTile - 1) / kAnyTile, tiles_k = (A.k + kAnyTile - 1) / kAnyTile;
-  const uint32_t per = tiles_n * tiles_k;
-  const int e = int(blockIdx.x / per), tile = int(blockIdx.x % per);
-  const int r0 = tile / int(tiles_n) * kAnyTile, c0 = tile % int(tiles_n) * kAnyTile;
-  const Group g = group_of(A, e);
-  const int K = g.last - g.first, rows = min(kAnyTile, A.k - r0), cols = min(kAnyTile, A.n - c0);
-  AnySide<T, false> sa{A.a + (g.first * A.lda + r0) * T::kBytes, A.lda, rows, K, {}};
-  AnySide<T, false> sb{A.b + (g.first * A.ldb + c0) * T::kBytes, A.ldb, cols, K, {}};
-  f32x4_t acc[2][2];
-  any_product<T, false, false>(acc, sa, sb, K);
-  any_store<TO>(acc, A.out + (e * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
-}
-
-inline bool too_many(uint64_t blocks) { return blocks >= (uint64_t(1) << 31); }
-
-template <class T>
-hipError_t matmul_any(const ExpertArgs& A, bool transposed, hipStream_t st) {
-  const uint64_t blocks = (uint64_t(A.rows + kAnyTile - 1) / kAnyTile + uint64_t(A.experts) + 1) *
-                          (uint64_t(A.n + kAnyTile - 1) / kAnyTile);
-  if (too_many(blocks)) return hipErrorInvalidConfiguration;
-  if (transposed) hipLaunchKernelGGL((k_expert_any<T, true>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
-  else hipLaunchKernelGGL((k_expert_any<T, false>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
+hipError_t sum_slices(const char* ws, int slices, bool out_f32, char* out, int64_t ldo, int64_t per, int64_t stride,
+                      int64_t rows, int n, hipStream_t st) {
+  const float* part = reinterpret_cast<const float*>(ws);
+  const uint64_t blocks = (uint64_t(rows) * ((uint64_t(n) + 3) / 4) + 255) / 256;
+  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  const dim3 grid{uint32_t(blocks)};
+  if (out_f32) hipLaunchKernelGGL((k_sum_slices<elem::F32>), grid, dim3(256), 0, st, part, slices, out, ldo, per, stride, rows, n);
+  else hipLaunchKernelGGL((k_sum_slices<elem::Bf16>), grid, dim3(256), 0, st, part, slices, out, ldo, per, stride, rows, n);
   return hipGetLastError();
 }
 
-template <class T, class TO>
-hipError_t wgrad_any(const ExpertArgs& A, hipStream_t st) {
-  const uint64_t blocks = uint64_t(A.experts) * (uint64_t(A.n + kAnyTile - 1) / kAnyTile) *
-                          (uint64_t(A.k + kAnyTile - 1) / kAnyTile);
-  if (too_many(blocks)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((k_wgrad_any<T, TO>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
-  return hipGetLastError();
+// Whether the tiles on direct loads take an operand or result: rows of whole
+// 16-byte pieces, and a stride that keeps a tile's byte offsets below 2^32.
+bool whole(const char* p, int64_t ld, int width) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld < (int64_t(1) << 22);
+}
+
+uint64_t up(uint64_t v, uint64_t d) { return (v + d - 1) / d; }
+
+// Slices of a summed index of K values for a launch of `tiles` tiles: about
+// `want` workgroups, none with fewer than `least` values.
+int slices_for(uint64_t tiles, uint64_t K, uint64_t want, uint64_t least) {
+  return int(std::max<uint64_t>(1, std::min<uint64_t>({want / std::max<uint64_t>(tiles, 1), K / least, 64})));
 }
 
 }  // namespace expert
 
-// Whether the tiles of tm_expert_tiles.hip take an operand or result: rows of
-// whole 16-byte pieces, and a stride that keeps a tile's byte offsets below 2^32.
-static bool whole(const char* p, int64_t ld, int width) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld < (int64_t(1) << 22);
+using namespace expert;
+
+// Rows: groups of up to 24 rows on average are bound by the reading of their
+// matrices and take the staged tiles of 16 or 32 rows, whatever the type and
+// alignment (63 rows over 53 experts of 192 x 6976, bf16: 24 us on 16-row tiles,
+// 57 on the 64 tile of direct loads; 80 rows over 5 experts of 7960 x 1970, fp32:
+// 108 us on 32 rows, 144 on 16, 184 on 64: the larger groups of an uneven call
+// should not need two tiles).  fp32 and odd operands stay with 32 rows up to 64
+// (105 rows over 2 experts of 4869 x 5632, odd: 47 us, 51 on the 64 tile).
+// Direct loads take the 256 tile from about one and a half tiles per compute
+// unit on (16384 rows, 8 experts of 4096 x 14336: 1.50 ms, 2.23 on 128, 2.97 on
+// 64; 24 rows, 8 experts of 768 x 2048: 19 us, 9 on 64), staged ones the 128 tile
+// from two (with 256 or 1024 in place of 512 the calls on either side lose a few
+// per cent).
+//
+// Slices of no less than eight stages, 256 values of fp32 and 512 of bf16 (7 rows,
+// 2 experts of 4608 x 64, fp32: 14.5 us, 17.5 from 512 on, 16.6 from 128 on, 72
+// unsplit; 24 rows, 8 experts of 768 x 2048, bf16: 9 us, 12 when split from 256 on).
+ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
+  ExpertPlan P{};
+  P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) && A.stride_b % 8 == 0 &&
+                      whole(A.out, A.ldo, A.n));
+  const uint64_t groups = uint64_t(std::min(A.experts, A.rows));
+  auto tiles = [&](uint64_t TM, uint64_t TN) { return (uint64_t(A.rows) / TM + groups) * up(A.n, TN); };
+  const uint64_t mean = uint64_t(A.rows) / groups;
+  if (!P.staged && mean > 24) {
+    P.tile = tiles(256, 256) >= 384 ? 256 : 64;
+    P.slices = P.tile == 64 ? slices_for(tiles(64, 64), A.k, 512, 512) : 1;
+  } else {
+    P.staged = true;
+    P.tile = mean <= 8 ? 16 : mean <= 64 ? 32 : tiles(128, 128) >= 512 ? 128 : 64;
+    P.slices = P.tile == 128 ? 1 : slices_for(tiles(P.tile, 64), A.k, 1024, f32 ? 256 : 512);
+  }
+  if (P.slices > 1) P.bytes = uint64_t(P.slices) * uint64_t(A.rows) * uint64_t(A.n) * 4u;
+  return P;
 }
 
-hipError_t launch_expert_matmul(const ExpertArgs& A, bool f32, bool transposed, hipStream_t st) {
-  if (f32) return expert::matmul_any<elem::F32>(A, transposed, st);
-  const bool fits = whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) && A.stride_b % 8 == 0 &&
-                    whole(A.out, A.ldo, A.n);
-  return fits ? launch_expert_matmul_tiles(A, transposed, st) : expert::matmul_any<elem::Bf16>(A, transposed, st);
+// Weight gradients: the same lines for the number of tiles; the summed index is
+// a group's rows (24211 rows, one expert, 896 x 128, fp32: 71 us in 36 slices).
+ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
+  ExpertPlan P{};
+  P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
+  auto tiles = [&](uint64_t T) { return uint64_t(A.experts) * up(A.k, T) * up(A.n, T); };
+  const uint64_t mean = uint64_t(A.rows) / uint64_t(A.experts);
+  P.tile = P.staged ? (tiles(128) >= 512 ? 128 : 64) : tiles(256) >= 384 ? 256 : 64;
+  P.slices = P.tile == 64 ? slices_for(tiles(64), mean, P.staged ? 1024 : 512, f32 ? 256 : 512) : 1;
+  if (P.slices > 1) P.bytes = uint64_t(P.slices) * uint64_t(A.experts) * uint64_t(A.k) * uint64_t(A.n) * 4u;
+  return P;
 }
 
-hipError_t launch_expert_wgrad(const ExpertArgs& A, bool f32, bool out_f32, hipStream_t st) {
-  if (f32) return expert::wgrad_any<elem::F32, elem::F32>(A, st);
-  if (whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n))
-    return launch_expert_wgrad_tiles(A, out_f32, st);
-  return out_f32 ? expert::wgrad_any<elem::Bf16, elem::F32>(A, st) : expert::wgrad_any<elem::Bf16, elem::Bf16>(A, st);
+hipError_t launch_expert_matmul(const ExpertArgs& call, const ExpertPlan& P, bool f32, bool transposed, char* ws,
+                                hipStream_t st) {
+  ExpertArgs A = call;
+  A.slices = P.slices;
+  if (P.slices > 1) {
+    A.out = ws;
+    A.ldo = A.n;
+    A.slice_out = int64_t(A.rows) * A.n;
+  }
+  const hipError_t e = P.staged ? launch_rows_staged(A, P, f32, transposed, st) : launch_rows_tiles(A, P, transposed, st);
+  if (e != hipSuccess || P.slices == 1) return e;
+  return sum_slices(ws, P.slices, f32, call.out, call.ldo, A.rows, 0, A.rows, A.n, st);
+}
+
+hipError_t launch_expert_wgrad(const ExpertArgs& call, const ExpertPlan& P, bool f32, bool out_f32, char* ws,
+                               hipStream_t st) {
+  ExpertArgs A = call;
+  A.slices = P.slices;
+  if (P.slices > 1) {
+    A.out = ws;
+    A.ldo = A.n;
+    A.stride_b = int64_t(A.k) * A.n;
+    A.slice_out = A.experts * A.stride_b;
+  }
+  const hipError_t e = P.staged ? launch_wgrad_staged(A, P, f32, out_f32, st) : launch_wgrad_tiles(A, P, out_f32, st);
+  if (e != hipSuccess || P.slices == 1) return e;
+  return sum_slices(ws, P.slices, out_f32, call.out, call.ldo, A.k, call.stride_b, int64_t(A.experts) * A.k, A.n, st);
 }
 
 }  // namespace tmk

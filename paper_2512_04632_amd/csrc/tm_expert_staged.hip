@@ -1,0 +1,424 @@
+// Expert products through registers: operands of any alignment and stride,
+// fp32, and groups of a few rows.  Tiles of TM x TN by four waves in a WM x WN
+// grid.
+//
+// A stage is 128 bytes of the summed index (64 bf16 or 32 fp32 values) of both
+// operands.  Its 16-byte chunks go global -> registers -> LDS, at any address
+// (the memory path takes 16-byte loads at an element's alignment).  Rows and
+// columns past the tile's end are read from the last row or the first chunk
+// that is there and dropped when the tile is stored; a stage that reaches the
+// summed index's end, or the last seven rows of a matrix (where 16 bytes could
+// end outside), is loaded with a check of every chunk, and what is past the
+// summed index comes out as zeros.  While a stage is multiplied from one LDS
+// buffer, the next D wait in registers, and the first of them is written to the
+// other buffer afterwards: one barrier a stage.
+//
+// Layouts in LDS: an operand whose summed index is contiguous as rows of 128
+// bytes, chunks XORed by (row / 2) % 8; a row-major one as rows of the tile's
+// columns, for bf16 32-byte chunks XORed by swz_y and read with the transposing
+// instruction, for fp32 64-byte blocks XORed by (row / 4) % 4 and read 4 bytes
+// a lane.  None of these reads has bank conflicts.  fp32 multiplies with
+// v_mfma_f32_16x16x4_f32, four at a time: lane group g of step j takes summed
+// value 16 s + 4 g + j of both operands, so that a contiguous operand is read
+// 16 bytes a lane.
+//
+// fp32 is bound by the matrix cores on large tiles (a 128 x 128 stage is 2048
+// clocks of them against some 300 of LDS reads), so rows that only fill a tile
+// cost as much as real ones: groups of a few rows take tiles of 16 or 32 rows,
+// which are bound by the reading of the matrices.
+#include "tm_elem.h"
+#include "tm_expert.h"
+#include "tm_tile.h"
+
+namespace tmk {
+namespace expert {
+
+using namespace tile;
+using elem::Bf16;
+using elem::F32;
+using elem::u32x4_t;
+
+constexpr int kStageBytes = 128;   // of the summed index, per row or column of a tile
+
+// One operand of a tile.  KC: its rows are the tile's, the summed index runs
+// along them; otherwise (row-major) its rows are the summed index.
+struct Source {
+  const char* p;   // first element of the tile's part
+  int64_t ld;
+  int limit;       // the tile's rows (row-major: columns) that are there
+  int left;        // rows from p's to the matrix's last
+};
+
+// The 16 bytes at p, of which the first n elements are wanted and the others
+// come out as zeros.  `inside`: all 16 bytes belong to the matrix.
+template <class T>
+__device__ inline u32x4_t load_chunk(const char* p, int n, bool inside) {
+  u32x4_t q = {0u, 0u, 0u, 0u};
+  if (n <= 0) return q;
+  if (n >= T::W || inside) {
+    q = T::load(p);
+    if (n < T::W) {
+      const int bytes = n * T::kBytes;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        q[j] &= bytes >= 4 * j + 4 ? 0xffffffffu : bytes > 4 * j ? 0xffffu : 0u;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < T::W; ++i)
+      if (i < n) T::put1(q, i, p + i * T::kBytes);
+  }
+  return q;
+}
+
+// One operand's way into LDS.  TS: the tile's rows (row-major: columns).
+template <class T, int TS, bool KC>
+struct Stager {
+  static constexpr int BK = kStageBytes / T::kBytes, CHUNKS = TS * kStageBytes / 16, Q = (CHUNKS + 255) / 256;
+  static constexpr int PER = KC ? 8 : TS * T::kBytes / 16;   // chunks of a stored row
+  const char* p[Q];
+  int64_t step;
+  int limit, left, K, whole;   // whole: values of the summed index that need no check
+
+  __device__ static int id(int i) { return i * 256 + int(threadIdx.x); }
+  __device__ static int row(int i) { return id(i) / PER; }
+  __device__ static int chunk(int i) { return id(i) % PER; }
+  __device__ static bool mine(int i) { return CHUNKS % 256 == 0 || id(i) < CHUNKS; }
+
+  __device__ void start(const Source& s, int summed) {
+    limit = s.limit;
+    left = s.left;
+    K = summed;
+    whole = KC ? K : min(K, left - 7);
+    step = KC ? kStageBytes : BK * s.ld * T::kBytes;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const int64_t r = KC ? min(row(i), limit - 1) : row(i);
+      const int c = KC || chunk(i) * T::W < limit ? chunk(i) : 0;
+      p[i] = s.p + (r * s.ld + c * T::W) * T::kBytes;
+    }
+  }
+  // Stage at k0, in steps of BK.
+  __device__ void load(int k0, u32x4_t (&v)[Q]) {
+    if (k0 + BK <= whole) {
+#pragma unroll
+      for (int i = 0; i < Q; ++i)
+        if (mine(i)) v[i] = T::load(p[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        if (!mine(i)) continue;
+        // seven rows before the last one, 16 bytes from an element of a row end within the matrix
+        if constexpr (KC)
+          v[i] = load_chunk<T>(p[i], K - k0 - chunk(i) * T::W, min(row(i), limit - 1) + 7 < left);
+        else
+          v[i] = load_chunk<T>(p[i], k0 + row(i) < K ? limit - chunk(i) * T::W : 0, k0 + row(i) + 7 < left);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < Q; ++i) p[i] += step;
+  }
+  __device__ void store(char* lds, const u32x4_t (&v)[Q]) const {
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      if (!mine(i)) continue;
+      const int r = row(i), c = chunk(i);
+      int at;
+      if constexpr (KC) at = r * kStageBytes + 16 * (c ^ ((r / 2) % 8));
+      else if constexpr (T::kBytes == 2) at = r * 2 * TS + 32 * ((c >> 1) ^ swz_y<TS>(r)) + 16 * (c & 1);
+      else at = r * 4 * TS + 64 * ((c >> 2) ^ ((r >> 2) & 3)) + 16 * (c & 3);
+      *reinterpret_cast<u32x4_t*>(lds + at) = v[i];
+    }
+  }
+};
+
+// Operands of slice s of a stage, rows or columns 16 (w F + f) + lane % 16 of a
+// tile side of TS (g: lane / 16).  bf16: 8 values 32 s + 8 g .. + 7.
+template <int TS, bool KC, int F>
+__device__ inline void load_slice(Bf16, uint4 (&v)[F], const char* st, int s, int w) {
+  const int lr = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  if constexpr (KC) {
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      const int r = (w * F + f) * 16 + lr;
+      v[f] = *reinterpret_cast<const uint4*>(st + r * kStageBytes + 16 * ((4 * s + g) ^ ((r / 2) % 8)));
+    }
+  } else {
+    const int rl = 8 * g + (lr >> 2);
+    const char* base = st + (32 * s + rl) * (2 * TS) + 8 * (lr & 3);
+    const int chunk = (w * F) ^ swz_y<TS>(rl);
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      const char* p = base + 32 * (chunk ^ f);
+      s16x4_t h[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4_t*)(lds_addr(p + u * 4 * (2 * TS))));
+      v[f] = __builtin_bit_cast(uint4, h);
+    }
+  }
+}
+// fp32: 4 values 16 s + 4 g .. + 3.
+template <int TS, bool KC, int F>
+__device__ inline void load_slice(F32, f32x4_t (&v)[F], const char* st, int s, int w) {
+  const int lr = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int f = 0; f < F; ++f) {
+    if constexpr (KC) {
+      const int r = (w * F + f) * 16 + lr;
+      v[f] = *reinterpret_cast<const f32x4_t*>(st + r * kStageBytes + 16 * ((4 * s + g) ^ ((r / 2) % 8)));
+    } else {
+      const char* p = st + (16 * s + 4 * g) * 4 * TS + 64 * ((w * F + f) ^ g) + 4 * lr;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[f][j] = *reinterpret_cast<const float*>(p + j * 4 * TS);
+    }
+  }
+}
+
+// The operands are fed the other way round: each lane holds four consecutive columns of a row.
+template <int FM, int FN>
+__device__ inline void mma_slice(Bf16, f32x4_t (&acc)[FM][FN], const uint4 (&a)[FM], const uint4 (&b)[FN]) {
+#pragma unroll
+  for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+    for (int fn = 0; fn < FN; ++fn)
+      acc[fm][fn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b[fn]),
+                                                            __builtin_bit_cast(bf16x8_t, a[fm]), acc[fm][fn], 0, 0, 0);
+}
+template <int FM, int FN>
+__device__ inline void mma_slice(F32, f32x4_t (&acc)[FM][FN], const f32x4_t (&a)[FM], const f32x4_t (&b)[FN]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+      for (int fn = 0; fn < FN; ++fn)
+        acc[fm][fn] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[fn][j], a[fm][j], acc[fm][fn], 0, 0, 0);
+}
+
+template <class T>
+struct SliceOf;
+template <>
+struct SliceOf<Bf16> { typedef uint4 V; };
+template <>
+struct SliceOf<F32> { typedef f32x4_t V; };
+
+// A tile's shape: FM x FN blocks of 16 x 16 a wave; D stages wait in registers
+// (a load takes longer than a stage of a small tile).
+template <int TM_, int TN_, int WM_, int D_>
+struct Shape {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = 4 / WM_, D = D_;
+  static constexpr int FM = TM / 16 / WM, FN = TN / 16 / WN;
+  static constexpr int A_BYTES = TM * kStageBytes, STAGE = (TM + TN) * kStageBytes;
+  static constexpr int ROW = 2 * TN + 16;   // of the bf16 output stage
+  static constexpr int LDS = 2 * STAGE > TM * ROW ? 2 * STAGE : TM * ROW;
+  static_assert(FM >= 1 && FN >= 1, "a block for every wave");
+};
+
+// acc = the tile's product over K values.
+template <class T, class S, bool AKC, bool BKC>
+__device__ inline void product_staged(f32x4_t (&acc)[S::FM][S::FN], char* smem, const Source& a, const Source& b, int K) {
+  using SA = Stager<T, S::TM, AKC>;
+  using SB = Stager<T, S::TN, BKC>;
+  constexpr int BK = SA::BK, D = S::D;
+  const int wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
+#pragma unroll
+  for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (K <= 0) return;
+  SA sa;
+  SB sb;
+  u32x4_t va[D][SA::Q], vb[D][SB::Q];
+  sa.start(a, K);
+  sb.start(b, K);
+  const int nk = (K + BK - 1) / BK;
+  sa.load(0, va[0]);
+  sb.load(0, vb[0]);
+  sa.store(smem, va[0]);
+  sb.store(smem + S::A_BYTES, vb[0]);
+#pragma unroll
+  for (int u = 0; u < D; ++u)
+    if (u + 1 < nk) {
+      sa.load((u + 1) * BK, va[u]);
+      sb.load((u + 1) * BK, vb[u]);
+    }
+  __syncthreads();
+  for (int k0 = 0; k0 < nk; k0 += D)
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      const int kt = k0 + u;
+      if (kt >= nk) break;
+      const char* st = smem + (kt & 1) * S::STAGE;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        typename SliceOf<T>::V fa[S::FM], fb[S::FN];
+        load_slice<S::TM, AKC, S::FM>(T{}, fa, st, s, wm);
+        load_slice<S::TN, BKC, S::FN>(T{}, fb, st + S::A_BYTES, s, wn);
+        mma_slice<S::FM, S::FN>(T{}, acc, fa, fb);
+      }
+      if (kt + 1 < nk) {
+        char* nx = smem + ((kt + 1) & 1) * S::STAGE;   // last read before the previous barrier
+        sa.store(nx, va[u]);
+        sb.store(nx + S::A_BYTES, vb[u]);
+        if (kt + 1 + D < nk) {
+          sa.load((kt + 1 + D) * BK, va[u]);
+          sb.load((kt + 1 + D) * BK, vb[u]);
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// Row and first of the four columns that a lane holds of block (fm, fn).
+template <class S>
+__device__ inline int staged_row(int fm) {
+  return (int(threadIdx.x >> 6) / S::WN * S::FM + fm) * 16 + int(threadIdx.x & 15);
+}
+template <class S>
+__device__ inline int staged_col(int fn) {
+  return (int(threadIdx.x >> 6) % S::WN * S::FN + fn) * 16 + 4 * (int(threadIdx.x & 63) >> 4);
+}
+
+// bf16 through LDS (free after the product's last barrier): 16 bytes a lane along the rows.
+template <class S>
+__device__ inline void store_tile(Bf16, const f32x4_t (&acc)[S::FM][S::FN], char* smem, char* out, int64_t ld, int rows,
+                                  int cols) {
+#pragma unroll
+  for (int fm = 0; fm < S::FM; ++fm)
+#pragma unroll
+    for (int fn = 0; fn < S::FN; ++fn) {
+      uint32_t o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = f2bf(acc[fm][fn][u]);
+      *reinterpret_cast<uint2*>(smem + staged_row<S>(fm) * S::ROW + staged_col<S>(fn) * 2) =
+          make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+    }
+  __syncthreads();
+  constexpr int LPR = S::TN / 8;   // lanes per row
+  const int c = int(threadIdx.x % LPR) * 8;
+  for (int r = threadIdx.x / LPR; r < rows; r += 256 / LPR) {
+    const char* from = smem + r * S::ROW + c * 2;
+    char* to = out + (r * ld + c) * 2;
+    if (c + 8 <= cols) {
+      Bf16::store(to, *reinterpret_cast<const u32x4_t*>(from));
+    } else {
+      for (int i = 0; i < cols - c; ++i)
+        reinterpret_cast<uint16_t*>(to)[i] = reinterpret_cast<const uint16_t*>(from)[i];
+    }
+  }
+}
+
+template <class S>
+__device__ inline void store_tile(F32, const f32x4_t (&acc)[S::FM][S::FN], char*, char* out, int64_t ld, int rows, int cols) {
+#pragma unroll
+  for (int fm = 0; fm < S::FM; ++fm) {
+    const int r = staged_row<S>(fm);
+    if (r >= rows) continue;
+#pragma unroll
+    for (int fn = 0; fn < S::FN; ++fn) {
+      const float v[4] = {acc[fm][fn][0], acc[fm][fn][1], acc[fm][fn][2], acc[fm][fn][3]};
+      elem::store_vec<F32>(out + r * ld * 4, staged_col<S>(fn), cols, v);
+    }
+  }
+}
+
+// TO: type of the result, F32 for slices of the summed index.
+template <class T, class TO, class S, bool TRANS>
+__global__ __launch_bounds__(256) void k_rows_staged(const ExpertArgs A, int row_tiles) {
+  __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+  const int nJ = (A.n + S::TN - 1) / S::TN;
+  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
+  const Place at = place_of(sl.id, row_tiles, nJ);
+  Group g;
+  if (!find_tile<S::TM>(A, at.I, g)) return;
+  const int c0 = at.J * S::TN, rows = g.last - g.first, cols = min(S::TN, A.n - c0);
+  int k0 = 0, K = 0;
+  if (g.e < A.experts) sl.range(A.k, kStageBytes / T::kBytes, k0, K);
+  const Source a{A.a + (g.first * A.lda + k0) * T::kBytes, A.lda, rows, A.rows - g.first};
+  const char* w = A.b + (K > 0 ? g.e * A.stride_b : 0) * T::kBytes;
+  const Source b = TRANS ? Source{w + (c0 * A.ldb + k0) * T::kBytes, A.ldb, cols, A.n - c0}
+                         : Source{w + (k0 * A.ldb + c0) * T::kBytes, A.ldb, cols, A.k - k0};
+  f32x4_t acc[S::FM][S::FN];
+  product_staged<T, S, true, TRANS>(acc, smem, a, b, K);
+  store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + g.first * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
+}
+
+template <class T, class TO, class S>
+__global__ __launch_bounds__(256) void k_wgrad_staged(const ExpertArgs A) {
+  __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+  const int nI = (A.k + S::TM - 1) / S::TM, nJ = (A.n + S::TN - 1) / S::TN;
+  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
+  const int e = sl.id / (nI * nJ);
+  const Place at = place_of(sl.id - e * nI * nJ, nI, nJ);
+  const Group g = group_of(A, e);
+  int k0, K;
+  sl.range(g.last - g.first, kStageBytes / T::kBytes, k0, K);
+  const int first = g.first + k0;
+  const int r0 = at.I * S::TM, c0 = at.J * S::TN, rows = min(S::TM, A.k - r0), cols = min(S::TN, A.n - c0);
+  const Source a{A.a + (first * A.lda + r0) * T::kBytes, A.lda, rows, A.rows - first};
+  const Source b{A.b + (first * A.ldb + c0) * T::kBytes, A.ldb, cols, A.rows - first};
+  f32x4_t acc[S::FM][S::FN];
+  product_staged<T, S, false, false>(acc, smem, a, b, K);
+  store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + e * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo,
+                rows, cols);
+}
+
+template <class T, class TO, class S>
+hipError_t rows_staged(const ExpertArgs& A, bool transposed, hipStream_t st) {
+  const uint64_t tiles = row_tiles(A, S::TM);
+  const uint64_t blocks = tiles * col_tiles(A, S::TN) * uint64_t(A.slices);
+  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  const dim3 grid{uint32_t(blocks)};
+  if (transposed) hipLaunchKernelGGL((k_rows_staged<T, TO, S, true>), grid, dim3(256), 0, st, A, int(tiles));
+  else hipLaunchKernelGGL((k_rows_staged<T, TO, S, false>), grid, dim3(256), 0, st, A, int(tiles));
+  return hipGetLastError();
+}
+
+template <class T, class TO, class S>
+hipError_t wgrad_staged(const ExpertArgs& A, hipStream_t st) {
+  const uint64_t blocks = uint64_t(A.experts) * ((uint64_t(A.k) + S::TM - 1) / S::TM) * col_tiles(A, S::TN) * uint64_t(A.slices);
+  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((k_wgrad_staged<T, TO, S>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
+  return hipGetLastError();
+}
+
+using Tile16 = Shape<16, 64, 1, 3>;
+using Tile32 = Shape<32, 64, 2, 3>;
+using Tile64 = Shape<64, 64, 2, 3>;
+using Tile128 = Shape<128, 128, 2, 1>;
+
+template <class T, class TO>
+hipError_t rows_tile(const ExpertArgs& A, int tile, bool transposed, hipStream_t st) {
+  switch (tile) {
+    case 16: return rows_staged<T, TO, Tile16>(A, transposed, st);
+    case 32: return rows_staged<T, TO, Tile32>(A, transposed, st);
+    case 64: return rows_staged<T, TO, Tile64>(A, transposed, st);
+  }
+  return rows_staged<T, TO, Tile128>(A, transposed, st);
+}
+
+template <class T, class TO>
+hipError_t wgrad_tile(const ExpertArgs& A, int tile, hipStream_t st) {
+  return tile == 64 ? wgrad_staged<T, TO, Tile64>(A, st) : wgrad_staged<T, TO, Tile128>(A, st);
+}
+
+}  // namespace expert
+
+using elem::Bf16;
+using elem::F32;
+
+hipError_t launch_rows_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool transposed, hipStream_t st) {
+  if (f32) return expert::rows_tile<F32, F32>(A, P.tile, transposed, st);
+  return P.slices > 1 ? expert::rows_tile<Bf16, F32>(A, P.tile, transposed, st)
+                      : expert::rows_tile<Bf16, Bf16>(A, P.tile, transposed, st);
+}
+
+hipError_t launch_wgrad_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool out_f32, hipStream_t st) {
+  if (f32) return expert::wgrad_tile<F32, F32>(A, P.tile, st);
+  return out_f32 || P.slices > 1 ? expert::wgrad_tile<Bf16, F32>(A, P.tile, st)
+                                 : expert::wgrad_tile<Bf16, Bf16>(A, P.tile, st);
+}
+
+}  // namespace tmk

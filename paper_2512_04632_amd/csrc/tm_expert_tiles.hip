@@ -1,6 +1,6 @@
 // Expert products of bf16 rows on the matrix cores: square tiles of 256 or
 // 64 fed by direct global -> LDS loads, for operands whose rows are 16-byte
-// aligned (the others: tm_expert.hip).
+// aligned (the others: tm_expert_staged.hip).
 //
 //   rows    out tile = a rows (summed index contiguous) x W (k x n: row-major,
 //           or n x k transposed: summed index contiguous)
@@ -70,35 +70,6 @@ struct Operand {
   int64_t ld;
   int limit;   // rows (row-major operand: columns) of the tile that are there
 };
-
-// Row-major a operand: the wave's block f of 16 columns is chunk wm FM + f of
-// the stage's rows; chunk ^ swizzle = ((wm FM) ^ swizzle) ^ f, since f < FM.
-template <int T, int BK>
-__device__ inline void load_frags_a_rm(Frags<T>& fr, const char* sa, int s, int wm) {
-  constexpr int FM = Tile<T>::FM;
-  const int lane = threadIdx.x & 63;
-  const int lr = lane & 15, g = lane >> 4;
-  const int rl = 8 * g + (lr >> 2);
-  const char* base = sa + (32 * s + rl) * (2 * T) + 8 * (lr & 3);
-  const int chunk = (wm * FM) ^ swz_y<T>(rl);
-#pragma unroll
-  for (int f = 0; f < FM; ++f) {
-    const char* p = base + 32 * (chunk ^ f);
-    s16x4_t v[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4_t*)(lds_addr(p + h * 4 * (2 * T))));
-    fr.a[f] = __builtin_bit_cast(uint4, v);
-  }
-}
-
-template <int T, int BK, bool ARM, bool BRM>
-__device__ inline void load_pair(Frags<T>& fr, const char* sa, const char* sb, int s, int wm, int wn) {
-  if constexpr (ARM) load_frags_a_rm<T, BK>(fr, sa, s, wm);
-  else load_frags_a<T, BK>(fr, sa, s, wm);
-  load_frags_b<T, BRM, BK>(fr, sb, s, wn);
-}
 
 // Operands of slice s of a stage with `valid` values of the summed index: the
 // others become zero.  A lane holds values 32 s + 8 (lane / 16) .. + 7.
@@ -254,40 +225,13 @@ __device__ inline void product(AccT<T>& acc, char* smem, const Operand& a, const
   else product_ring<T, BK, ARM, BRM>(acc, smem, a, b, K);
 }
 
-// Bytes of a row of the output stage: 16 more than a tile's row, so that the
-// 16 rows that a wave writes at a time start in different banks.
-template <int T>
-constexpr int kStageRow = 2 * T + 16;
-
 template <int T, int BK>
 constexpr int lds_bytes() { return std::max(Ring<T, BK>::LDS, T * kStageRow<T>); }
-
-// Row and first of the four columns that a lane holds of block (fm, fn).
-template <int T>
-__device__ inline int out_row(int fm) {
-  const int wave = threadIdx.x >> 6;
-  return (wave / Tile<T>::WGN) * Tile<T>::TWM + 16 * fm + int(threadIdx.x & 15);
-}
-template <int T, bool BRM>
-__device__ inline int out_col(int fn) {
-  const int wn = int(threadIdx.x >> 6) % Tile<T>::WGN;
-  return (BRM ? 16 * (fn * Tile<T>::WGN + wn) : wn * Tile<T>::TWN + 16 * fn) + 4 * (int(threadIdx.x & 63) >> 4);
-}
 
 // bf16 through LDS: whole rows of the tile, 16 bytes a lane.
 template <int T, bool BRM>
 __device__ inline void store_bf16(const AccT<T>& acc, char* smem, uint16_t* out, int64_t ld, int rows, int cols) {
-#pragma unroll
-  for (int fm = 0; fm < Tile<T>::FM; ++fm)
-#pragma unroll
-    for (int fn = 0; fn < Tile<T>::FN; ++fn) {
-      uint32_t o[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) o[u] = f2bf(acc[fm][fn][u]);
-      *reinterpret_cast<uint2*>(smem + out_row<T>(fm) * kStageRow<T> + out_col<T, BRM>(fn) * 2) =
-          make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
-    }
-  __syncthreads();
+  stage_bf16<T>(acc, smem, [](int fn) { return out_col<T, BRM>(fn); });
   constexpr int LPR = T / 8;   // lanes per row
   const int c = int(threadIdx.x % LPR) * 8;
   if (c >= cols) return;
@@ -310,95 +254,84 @@ __device__ inline void store_f32(const AccT<T>& acc, float* out, int64_t ld, int
   }
 }
 
-// Place of logical tile `id` in a grid of nI x nJ tiles, in groups of four rows
-// of tiles: tiles that run together share operand panels.
-struct Place {
-  int I, J;
-};
-__device__ inline Place place_of(int id, int nI, int nJ) {
-  constexpr int GM = 4;
-  const int grp = id / (GM * nJ), first = grp * GM, size = min(nI - first, GM);
-  const int rem = id - grp * GM * nJ;
-  return Place{first + rem % size, rem / size};
-}
-
-template <int T, int BK, bool TRANS>
+// OUT32: fp32 results, the slices of a summed index that is split.
+template <int T, int BK, bool TRANS, bool OUT32>
 __global__ __launch_bounds__(Tile<T>::NT) void k_expert_rows(const ExpertArgs A, int row_tiles) {
   __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<T, BK>()];
   const int nJ = (A.n + T - 1) / T;
-  const Place at = place_of(xcd_remap(int(blockIdx.x), int(gridDim.x)), row_tiles, nJ);
+  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
+  const Place at = place_of(sl.id, row_tiles, nJ);
   Group g;
   if (!find_tile<T>(A, at.I, g)) return;
   const int e = __builtin_amdgcn_readfirstlane(g.e), first = __builtin_amdgcn_readfirstlane(g.first);
   const int rows = __builtin_amdgcn_readfirstlane(g.last) - first;
   const int c0 = at.J * T, cols = min(T, A.n - c0);
-  const uint16_t* x = reinterpret_cast<const uint16_t*>(A.a) + first * A.lda;
+  int k0 = 0, K = 0;
+  if (e < A.experts) sl.range(A.k, 64, k0, K);
+  const uint16_t* x = reinterpret_cast<const uint16_t*>(A.a) + first * A.lda + k0;
   const uint16_t* w = reinterpret_cast<const uint16_t*>(A.b);
-  if (e < A.experts) w += e * A.stride_b + (TRANS ? c0 * A.ldb : int64_t(c0));
+  if (K > 0) w += e * A.stride_b + (TRANS ? c0 * A.ldb + k0 : k0 * A.ldb + c0);
   AccT<T> acc;
-  product<T, BK, false, !TRANS>(acc, smem, Operand{x, A.lda, rows}, Operand{w, A.ldb, cols},
-                                e < A.experts ? A.k : 0);
-  store_bf16<T, !TRANS>(acc, smem, reinterpret_cast<uint16_t*>(A.out) + first * A.ldo + c0, A.ldo, rows, cols);
+  product<T, BK, false, !TRANS>(acc, smem, Operand{x, A.lda, rows}, Operand{w, A.ldb, cols}, K);
+  const int64_t out = sl.z * A.slice_out + first * A.ldo + c0;
+  if constexpr (OUT32)
+    store_f32<T, !TRANS>(acc, reinterpret_cast<float*>(A.out) + out, A.ldo, rows, cols);
+  else
+    store_bf16<T, !TRANS>(acc, smem, reinterpret_cast<uint16_t*>(A.out) + out, A.ldo, rows, cols);
 }
 
 template <int T, int BK, bool OUT32>
 __global__ __launch_bounds__(Tile<T>::NT) void k_expert_wgrad(const ExpertArgs A) {
   __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<T, BK>()];
   const int nI = (A.k + T - 1) / T, nJ = (A.n + T - 1) / T;
-  const int id = xcd_remap(int(blockIdx.x), int(gridDim.x));
-  const int e = id / (nI * nJ);
-  const Place at = place_of(id - e * nI * nJ, nI, nJ);
+  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
+  const int e = sl.id / (nI * nJ);
+  const Place at = place_of(sl.id - e * nI * nJ, nI, nJ);
   const Group g = group_of(A, e);
-  const int first = __builtin_amdgcn_readfirstlane(g.first), K = __builtin_amdgcn_readfirstlane(g.last) - first;
+  int k0, K;
+  sl.range(__builtin_amdgcn_readfirstlane(g.last - g.first), 64, k0, K);
+  const int first = __builtin_amdgcn_readfirstlane(g.first) + k0;
   const int r0 = at.I * T, c0 = at.J * T, rows = min(T, A.k - r0), cols = min(T, A.n - c0);
   const uint16_t* x = reinterpret_cast<const uint16_t*>(A.a) + first * A.lda + r0;
   const uint16_t* dy = reinterpret_cast<const uint16_t*>(A.b) + first * A.ldb + c0;
   AccT<T> acc;
   product<T, BK, true, true>(acc, smem, Operand{x, A.lda, rows}, Operand{dy, A.ldb, cols}, K);
-  const int64_t out = e * A.stride_b + r0 * A.ldo + c0;
+  const int64_t out = sl.z * A.slice_out + e * A.stride_b + r0 * A.ldo + c0;
   if constexpr (OUT32)
     store_f32<T, true>(acc, reinterpret_cast<float*>(A.out) + out, A.ldo, rows, cols);
   else
     store_bf16<T, true>(acc, smem, reinterpret_cast<uint16_t*>(A.out) + out, A.ldo, rows, cols);
 }
 
-template <int T, int BK>
+template <int T, int BK, bool OUT32>
 hipError_t rows_t(const ExpertArgs& A, bool transposed, hipStream_t st) {
-  const uint64_t row_tiles = uint64_t(A.rows + T - 1) / T + uint64_t(A.experts) + 1;
-  const uint64_t blocks = row_tiles * (uint64_t(A.n + T - 1) / T);
+  const uint64_t tiles = row_tiles(A, T);
+  const uint64_t blocks = tiles * col_tiles(A, T) * uint64_t(A.slices);
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
   const dim3 grid{uint32_t(blocks)}, block(Tile<T>::NT);
-  if (transposed) hipLaunchKernelGGL((k_expert_rows<T, BK, true>), grid, block, 0, st, A, int(row_tiles));
-  else hipLaunchKernelGGL((k_expert_rows<T, BK, false>), grid, block, 0, st, A, int(row_tiles));
+  if (transposed) hipLaunchKernelGGL((k_expert_rows<T, BK, true, OUT32>), grid, block, 0, st, A, int(tiles));
+  else hipLaunchKernelGGL((k_expert_rows<T, BK, false, OUT32>), grid, block, 0, st, A, int(tiles));
   return hipGetLastError();
 }
 
-template <int T, int BK>
-hipError_t wgrad_t(const ExpertArgs& A, bool out_f32, hipStream_t st) {
-  const uint64_t blocks = uint64_t(A.experts) * (uint64_t(A.k + T - 1) / T) * (uint64_t(A.n + T - 1) / T);
+template <int T, int BK, bool OUT32>
+hipError_t wgrad_t(const ExpertArgs& A, hipStream_t st) {
+  const uint64_t blocks = wgrad_tiles(A, T) * uint64_t(A.slices);
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
-  const dim3 grid{uint32_t(blocks)}, block(Tile<T>::NT);
-  if (out_f32) hipLaunchKernelGGL((k_expert_wgrad<T, BK, true>), grid, block, 0, st, A);
-  else hipLaunchKernelGGL((k_expert_wgrad<T, BK, false>), grid, block, 0, st, A);
+  hipLaunchKernelGGL((k_expert_wgrad<T, BK, OUT32>), dim3(uint32_t(blocks)), dim3(Tile<T>::NT), 0, st, A);
   return hipGetLastError();
 }
 
 }  // namespace expert
 
-// Tile by the number of 256 tiles: above about one and a half per compute unit
-// they win (16384 rows, 8 experts of 4096 x 14336: 1.50 ms, 2.45 on 128 tiles,
-// 2.97 on 64), below it the 64 tile's many workgroups do (24 rows, 8 experts of
-// 768 x 2048: 9 us against 19).
-static bool large(uint64_t tiles) { return tiles >= 384; }
-
-hipError_t launch_expert_matmul_tiles(const ExpertArgs& A, bool transposed, hipStream_t st) {
-  const uint64_t tiles = (uint64_t(A.rows) / 256 + uint64_t(A.experts)) * ((uint64_t(A.n) + 255) / 256);
-  return large(tiles) ? expert::rows_t<256, 64>(A, transposed, st) : expert::rows_t<64, 64>(A, transposed, st);
+hipError_t launch_rows_tiles(const ExpertArgs& A, const ExpertPlan& P, bool transposed, hipStream_t st) {
+  if (P.tile == 256) return expert::rows_t<256, 64, false>(A, transposed, st);
+  return P.slices > 1 ? expert::rows_t<64, 64, true>(A, transposed, st) : expert::rows_t<64, 64, false>(A, transposed, st);
 }
 
-hipError_t launch_expert_wgrad_tiles(const ExpertArgs& A, bool out_f32, hipStream_t st) {
-  const uint64_t tiles = uint64_t(A.experts) * ((uint64_t(A.k) + 255) / 256) * ((uint64_t(A.n) + 255) / 256);
-  return large(tiles) ? expert::wgrad_t<256, 64>(A, out_f32, st) : expert::wgrad_t<64, 64>(A, out_f32, st);
+hipError_t launch_wgrad_tiles(const ExpertArgs& A, const ExpertPlan& P, bool out_f32, hipStream_t st) {
+  if (P.tile == 256) return out_f32 ? expert::wgrad_t<256, 64, true>(A, st) : expert::wgrad_t<256, 64, false>(A, st);
+  return out_f32 || P.slices > 1 ? expert::wgrad_t<64, 64, true>(A, st) : expert::wgrad_t<64, 64, false>(A, st);
 }
 
 }  // namespace tmk

@@ -131,26 +131,168 @@ __device__ inline void write_row(const LossArgs& A, int64_t r, const Row& o) {
   A.row_loss[r] = o.loss;
 }
 
-// Gradient of vocabulary entries first .. first + W - 1: p = exp2((l - m) c) inv,
-// out = f ([v = y] - p).
+// Gradient of a vector of logits, the target `target` entries on from its first:
+// p = exp2((l - m) c) inv, out = f ([v = y] - p).
 template <class T>
-__device__ inline void gradient_vec(float* v, int first, int64_t y, float m, float c, float inv, float f) {
+__device__ inline void gradient_vec(float* v, int target, float m, float c, float inv, float f) {
 #pragma unroll
   for (int i = 0; i < T::W; ++i) {
     const float p = exp2_fast((v[i] - m) * c) * inv;
-    v[i] = f * ((first + i == y ? 1.f : 0.f) - p);
+    v[i] = f * ((i == target ? 1.f : 0.f) - p);
   }
 }
 
+// The row's target, or a place that no entry has: a vocabulary ends before 2^30.
+__device__ inline int target_of(const LossArgs& A, int64_t r) {
+  const int64_t y = A.targets[r];
+  return y < A.vocab ? int(y) : INT32_MAX;
+}
+
 template <class T, int NT>
-__device__ inline void zero_row(char* row, int n) {
+__device__ inline void zero_row(char* row, int n, int t) {
   float z[T::W];
 #pragma unroll
   for (int i = 0; i < T::W; ++i) z[i] = 0.f;
-  for (int c = threadIdx.x * T::W; c < n; c += NT * T::W) store_vec<T>(row, c, n, z);
+  for (int c = t * T::W; c < n; c += NT * T::W) store_vec<T>(row, c, n, z);
 }
 
-// One workgroup per row.
+// -inf in the elements of a vector that lie past the row's end.
+template <class T>
+__device__ inline u32x4_t fill_past(u32x4_t q, int first, int n) {
+#pragma unroll
+  for (int i = 0; i < T::W; ++i) {
+    if (first + i < n) continue;
+    if constexpr (T::kBytes == 2) q[i / 2] = i % 2 ? (q[i / 2] & 0xffffu) | 0xff800000u : (q[i / 2] & 0xffff0000u) | 0xff80u;
+    else q[i] = 0xff800000u;
+  }
+  return q;
+}
+
+// The vector as it is, behind a fence: without it the compiler unpacks a held
+// row of bf16 once and keeps the fp32 values, twice the registers.
+__device__ inline u32x4_t afresh(u32x4_t q) {
+  asm volatile("" : "+v"(q));
+  return q;
+}
+
+// Between the vectors of a long held row: unpacked values of several at once
+// have no registers.
+template <int K>
+__device__ inline void keep_order() {
+  if constexpr (K >= 8) __builtin_amdgcn_sched_barrier(0);
+}
+
+// NT threads per row (64: four rows a workgroup), which hold the whole row in
+// registers, K vectors each: it is read once, its maximum is known before the
+// first exponential is taken, and the gradient is formed from the registers.
+template <class T, int NT, int K, bool GRAD>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_loss_held(const LossArgs A) {
+  constexpr int RB = NT < 256 ? 256 / NT : 1, W = T::W, NW = NT / 64;
+  __shared__ Soft slots[NT > 64 ? NW : 1];
+  const int t = threadIdx.x % NT, n = A.vocab;
+  const int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT;
+  if (r >= A.rows) return;
+  char* d = GRAD ? A.dlogits + r * A.ldd * T::kBytes : nullptr;
+  if (!active(A, r)) {
+    if (t == 0) write_row(A, r, Row{0.f, 0.f, 0.f, 0.f});
+    if constexpr (GRAD) zero_row<T, NT>(d, n, t);
+    return;
+  }
+  const char* l = A.logits + r * A.ld * T::kBytes;
+  const float c = A.inv_temp * kLog2e;
+  u32x4_t q[K];
+#pragma unroll
+  for (int j = 0; j < K; ++j) q[j] = load_ahead<T, true>(l, (j * NT + t) * W, n);
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const int first = (j * NT + t) * W;
+    if (first + W > n) q[j] = fill_past<T>(settle<T, true>(q[j], first, n), first, n);
+  }
+  Soft s = nothing();
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    float v[W];
+    T::unpack(afresh(q[j]), v);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      s.m = fmaxf(s.m, v[i]);
+      nan |= v[i] != v[i];
+    }
+    keep_order<K>();
+  }
+  // while every value is -inf the terms are taken as exp(-inf - 0) = 0
+  const float at = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    float v[W];
+    T::unpack(afresh(q[j]), v);
+#pragma unroll
+    for (int i = 0; i < W; ++i) s.s += exp2_fast((v[i] - at) * c);
+    keep_order<K>();
+  }
+  if (nan) s.s = NAN;
+  s = wave_join(s, c);
+  Row row;
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = slots[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) s = join(s, slots[w], c);
+  }
+  row = finish<T>(A, r, s);   // every thread: what it reads is in a cache, and nothing waits for another
+  if constexpr (NT > 64) {
+    // the target's logit has been read by everyone before any of the row is overwritten
+    if constexpr (GRAD) __syncthreads();
+  }
+  if (t == 0) write_row(A, r, row);
+  if constexpr (GRAD) {
+    const float f = row.slope * A.inv_temp, inv = 1.f / s.s;
+    const int y = target_of(A, r);
+    if (f == 0.f) {
+      zero_row<T, NT>(d, n, t);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int first = (j * NT + t) * W;
+      if (first >= n) continue;
+      float v[W];
+      T::unpack(afresh(q[j]), v);
+      gradient_vec<T>(v, y - first, s.m, c, inv, f);
+      store_vec<T>(d, first, n, v);
+      keep_order<K>();
+    }
+  }
+}
+
+// f(values, first entry) for each vector of entries first .. last - 1 of a row
+// that falls to this thread of NT, -inf past the end; four loads at a time.
+template <class T, int NT, class F>
+__device__ inline void each_group(const char* l, int first, int last, F f) {
+  constexpr int G = 4, STEP = NT * T::W;
+  int at = first + int(threadIdx.x) * T::W;
+  for (; at + (G - 1) * STEP + T::W <= last; at += G * STEP) {
+    u32x4_t q[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) q[g] = T::load(l + int64_t(at + g * STEP) * T::kBytes);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float v[T::W];
+      T::unpack(q[g], v);
+      f(v, at + g * STEP);
+    }
+  }
+  for (; at < last; at += STEP) {
+    float v[T::W];
+    load_vec<T>(l, at, last, -INFINITY, v);
+    f(v, at);
+  }
+}
+
+// Longer rows: one workgroup per row, which reads it twice (the second time
+// mostly from the memory-side cache).
 template <class T, int NT, bool GRAD>
 __global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
   __shared__ Soft slots[NT / 64];
@@ -159,17 +301,13 @@ __global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
   const int n = A.vocab;
   if (!active(A, r)) {
     if (threadIdx.x == 0) write_row(A, r, Row{0.f, 0.f, 0.f, 0.f});
-    if constexpr (GRAD) zero_row<T, NT>(A.dlogits + r * A.ldd * T::kBytes, n);
+    if constexpr (GRAD) zero_row<T, NT>(A.dlogits + r * A.ldd * T::kBytes, n, threadIdx.x);
     return;
   }
   const char* l = A.logits + r * A.ld * T::kBytes;
   const float c = A.inv_temp * kLog2e;
   Soft s = nothing();
-  for (int f = threadIdx.x * T::W; f < n; f += NT * T::W) {
-    float v[T::W];
-    load_vec<T>(l, f, n, -INFINITY, v);
-    add_terms<T::W>(s, v, c);
-  }
+  each_group<T, NT>(l, 0, n, [&](float* v, int) { add_terms<T::W>(s, v, c); });
   s = block_join<NT>(s, c, slots);
   if (threadIdx.x == 0) {
     row = finish<T>(A, r, s);
@@ -179,17 +317,15 @@ __global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
     __syncthreads();
     char* d = A.dlogits + r * A.ldd * T::kBytes;
     const float f = row.slope * A.inv_temp, inv = 1.f / s.s;
-    const int64_t y = A.targets[r];
+    const int y = target_of(A, r);
     if (f == 0.f) {
-      zero_row<T, NT>(d, n);
+      zero_row<T, NT>(d, n, threadIdx.x);
       return;
     }
-    for (int at = threadIdx.x * T::W; at < n; at += NT * T::W) {
-      float v[T::W];
-      load_vec<T>(l, at, n, 0.f, v);
-      gradient_vec<T>(v, at, y, s.m, c, inv, f);
+    each_group<T, NT>(l, 0, n, [&](float* v, int at) {
+      gradient_vec<T>(v, y - at, s.m, c, inv, f);
       store_vec<T>(d, at, n, v);
-    }
+    });
   }
 }
 
@@ -204,11 +340,7 @@ __global__ __launch_bounds__(256) void k_loss_part(const LossArgs A) {
   const char* l = A.logits + r * A.ld * T::kBytes;
   const float c = A.inv_temp * kLog2e;
   Soft s = nothing();
-  for (int f = first + threadIdx.x * T::W; f < last; f += 256 * T::W) {
-    float v[T::W];
-    load_vec<T>(l, f, last, -INFINITY, v);
-    add_terms<T::W>(s, v, c);
-  }
+  each_group<T, 256>(l, first, last, [&](float* v, int) { add_terms<T::W>(s, v, c); });
   s = block_join<256>(s, c, slots);
   if (threadIdx.x == 0) A.part[blockIdx.x] = make_float2(s.m, s.s);
 }
@@ -271,7 +403,7 @@ __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
   char* d = A.dlogits + r * A.ldd * T::kBytes;
   const float f = slope * A.inv_temp * (A.grad != nullptr ? *A.grad : 1.f);
   const float lse = A.lse[r];
-  const int64_t y = A.targets[r];
+  const int y = target_of(A, r);
   for (int at = first + threadIdx.x * T::W; at < last; at += 256 * T::W) {
     float v[T::W];
     if (slope == 0.f) {
@@ -282,7 +414,7 @@ __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
 #pragma unroll
       for (int i = 0; i < T::W; ++i) {
         const float p = exp2_fast(fmaf(v[i], A.inv_temp, -lse) * kLog2e);
-        v[i] = f * ((at + i == y ? 1.f : 0.f) - p);
+        v[i] = f * ((i == y - at ? 1.f : 0.f) - p);
       }
     }
     store_vec<T>(d, at, last, v);
@@ -291,20 +423,54 @@ __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
 
 constexpr int kJoinRows = 64;   // up to here one workgroup joins and sums every row
 
+template <class T, int NT, int K>
+void launch_held(const LossArgs& A, hipStream_t st) {
+  constexpr int RB = NT < 256 ? 256 / NT : 1;
+  const dim3 grid(uint32_t((A.rows + RB - 1) / RB)), block(NT < 256 ? 256 : NT);
+  if (A.dlogits != nullptr) hipLaunchKernelGGL((k_loss_held<T, NT, K, true>), grid, block, 0, st, A);
+  else hipLaunchKernelGGL((k_loss_held<T, NT, K, false>), grid, block, 0, st, A);
+}
+
+template <class T, int NT>
+void launch_twice(const LossArgs& A, hipStream_t st) {
+  const dim3 grid(uint32_t(A.rows));
+  if (A.dlogits != nullptr) hipLaunchKernelGGL((k_loss_rows<T, NT, true>), grid, dim3(NT), 0, st, A);
+  else hipLaunchKernelGGL((k_loss_rows<T, NT, false>), grid, dim3(NT), 0, st, A);
+}
+
+// Rows held in registers or read twice, and by how many threads; the same with
+// and without the gradient, so that the value has the same bits (4096 rows unless
+// said otherwise).
+//   Held by a wave: up to 256 vectors (10140 x 1731 bf16 with gradient: 25 us, 36
+//   when read twice).
+//   Held by a workgroup: fp32 from 16384 to 32768 entries (32001: 196 us with
+//   gradient, 230 when read twice).  Below, what the gradient gains the value alone
+//   loses (15000: 100 against 118 us, 67 against 41), and bf16 rows, which are
+//   unpacked anew in every pass, are better read twice (20000: 160 against 75).
+//   Read twice: 256 threads, so that many rows overlap, as long as the rows under
+//   way stay in the memory-side cache until their second reading: 512 threads from
+//   48 KB a row and 1024 from 160 KB (with gradient, 50257 bf16: 251, 223 and 276 us
+//   with 256, 512 and 1024 threads; 8192 x 131072: 1185, 1047, 881).
+template <class T>
+void launch_rows(const LossArgs& A, hipStream_t st) {
+  const int vecs = (A.vocab + T::W - 1) / T::W;
+  if (vecs <= 64 * 2) return launch_held<T, 64, 2>(A, st);
+  if (vecs <= 64 * 4) return launch_held<T, 64, 4>(A, st);
+  if constexpr (T::kBytes == 4) {
+    if (vecs > 1024 * 4 && vecs <= 1024 * 8) return launch_held<T, 1024, 8>(A, st);
+  }
+  const int64_t bytes = int64_t(A.vocab) * T::kBytes;
+  if (bytes <= 48 * 1024) return launch_twice<T, 256>(A, st);
+  if (bytes <= 160 * 1024) return launch_twice<T, 512>(A, st);
+  launch_twice<T, 1024>(A, st);
+}
+
 template <class T>
 hipError_t forward_t(const LossArgs& A, hipStream_t st) {
   if (A.rows == 0) {
     // the sum of no rows
   } else if (A.chunks == 1) {
-    const bool wide = int64_t(A.vocab) * T::kBytes > 32768;
-    const dim3 grid(uint32_t(A.rows)), block(wide ? 1024 : 256);
-    if (A.dlogits != nullptr) {
-      if (wide) hipLaunchKernelGGL((k_loss_rows<T, 1024, true>), grid, block, 0, st, A);
-      else hipLaunchKernelGGL((k_loss_rows<T, 256, true>), grid, block, 0, st, A);
-    } else {
-      if (wide) hipLaunchKernelGGL((k_loss_rows<T, 1024, false>), grid, block, 0, st, A);
-      else hipLaunchKernelGGL((k_loss_rows<T, 256, false>), grid, block, 0, st, A);
-    }
+    launch_rows<T>(A, st);
   } else {
     hipLaunchKernelGGL((k_loss_part<T>), dim3(uint32_t(A.rows) * A.chunks), dim3(256), 0, st, A);
     if (A.rows <= kJoinRows)

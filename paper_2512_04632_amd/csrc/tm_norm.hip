@@ -66,13 +66,14 @@ __device__ inline void load_cols(const float* p, float fill, int t, int d, float
 }
 
 // This thread's vectors of a row, as stored.
-template <int NT, int V, class T>
+template <int NT, int V, class T, bool TAIL>
 __device__ inline void load_row(const char* row, int t, int d, u32x4_t (&q)[V]) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) q[j] = load_raw<T>(row, (j * NT + t) * T::W, d);
+  for (int j = 0; j < V; ++j) q[j] = load_ahead<T, TAIL>(row, (j * NT + t) * T::W, d);
 }
 
-template <class T, int NT, int E>
+// TAIL: rows that end inside a 16-byte vector.
+template <class T, int NT, int E, bool TAIL>
 __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) {
   constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
   __shared__ float slots[2][NW];
@@ -84,17 +85,17 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) 
   const int64_t step = int64_t(gridDim.x) * RB;
   int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT;
   u32x4_t q[V];
-  if (r < A.rows) load_row<NT, V, T>(A.x + r * A.ldx * T::kBytes, t, d, q);
+  if (r < A.rows) load_row<NT, V, T, TAIL>(A.x + r * A.ldx * T::kBytes, t, d, q);
   for (; r < A.rows; r += step) {
     float v[E], s[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      T::unpack(q[j], v + j * W);
+      T::unpack(settle<T, TAIL>(q[j], (j * NT + t) * W, d), v + j * W);
 #pragma unroll
       for (int i = 0; i < W; ++i) s[0] += v[j * W + i];
     }
     // the next row is on its way while this one is summed
-    if (r + step < A.rows) load_row<NT, V, T>(A.x + (r + step) * A.ldx * T::kBytes, t, d, q);
+    if (r + step < A.rows) load_row<NT, V, T, TAIL>(A.x + (r + step) * A.ldx * T::kBytes, t, d, q);
     row_sum<NT>(s, slots[0]);
     const float mean = s[0] / n;
     s[0] = 0.f;
@@ -123,9 +124,16 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) 
   }
 }
 
+// Rows that wait in registers: one, or three of 16 bytes a thread (5999 x 1998
+// bf16: 29 us, 47 with one); two of 32 bytes cost more in occupancy than they bring
+// (16384 x 4096 bf16: 88 us, 84 with one).  1024 threads have no registers for any.
 template <class T, int NT, int E>
+constexpr int rows_ahead() { return NT == 1024 ? 0 : NT <= 256 && E * T::kBytes <= 16 ? 3 : 1; }
+
+template <class T, int NT, int E, bool TAIL>
 __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const NormArgs A) {
   constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
+  constexpr int AHEAD = rows_ahead<T, NT, E>(), D = AHEAD > 0 ? AHEAD : 1;
   __shared__ float slots[2][2 * NW];
   const int t = threadIdx.x % NT, d = A.d;
   const float n = float(d);
@@ -135,53 +143,71 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
   for (int i = 0; i < E; ++i) aw[i] = ab[i] = 0.f;
   const int64_t step = int64_t(gridDim.x) * RB;
   int64_t r = int64_t(blockIdx.x) * RB + threadIdx.x / NT;
-  u32x4_t qx[V], qy[V];
-  float mean = 0.f, rstd = 0.f;
-  auto read = [&](int64_t at) __attribute__((always_inline)) {
-    load_row<NT, V, T>(A.x + at * A.ldx * T::kBytes, t, d, qx);
-    load_row<NT, V, T>(A.dy + at * A.lddy * T::kBytes, t, d, qy);
-    mean = A.mean[at];
-    rstd = A.rstd[at];
+  u32x4_t qx[D][V], qy[D][V];
+  float mean[D], rstd[D];
+  auto read = [&](int u, int64_t at) __attribute__((always_inline)) {
+    load_row<NT, V, T, TAIL>(A.x + at * A.ldx * T::kBytes, t, d, qx[u]);
+    load_row<NT, V, T, TAIL>(A.dy + at * A.lddy * T::kBytes, t, d, qy[u]);
+    mean[u] = A.mean[at];
+    rstd[u] = A.rstd[at];
   };
-  constexpr bool kAhead = NT < 1024;   // 1024 threads have no registers for a second row
-  if (kAhead && r < A.rows) read(r);
+  if constexpr (AHEAD > 0) {
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+      if (r + u * step < A.rows) read(u, r + u * step);
+  }
   int turn = 0;
-  for (; r < A.rows; r += step) {
-    if (!kAhead) read(r);
-    float h[E], g[E], s[2] = {0.f, 0.f};
-    const float scale = rstd;
+  while (r < A.rows) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * NT + t) * W;
-      T::unpack(qx[j], h + j * W);
-      T::unpack(qy[j], g + j * W);
+    for (int u = 0; u < D; ++u) {
+      if (r >= A.rows) break;
+      if constexpr (AHEAD == 0) read(u, r);
+      float h[E], g[E], s[2] = {0.f, 0.f};
+      const float m = mean[u], scale = rstd[u];
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const int e = j * W + i;
-        h[e] = c + i < d ? (h[e] - mean) * rstd : 0.f;
-        aw[e] += g[e] * h[e];
-        ab[e] += g[e];
-        g[e] *= w[e];
-        s[0] += g[e];
-        s[1] += g[e] * h[e];
+      for (int j = 0; j < V; ++j) {
+        const int c = (j * NT + t) * W;
+        T::unpack(settle<T, TAIL>(qx[u][j], c, d), h + j * W);
+        T::unpack(settle<T, TAIL>(qy[u][j], c, d), g + j * W);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const int e = j * W + i;
+          h[e] = c + i < d ? (h[e] - m) * scale : 0.f;
+          aw[e] += g[e] * h[e];
+          ab[e] += g[e];
+          g[e] *= w[e];
+          s[0] += g[e];
+          s[1] += g[e] * h[e];
+        }
       }
-    }
-    if (kAhead && r + step < A.rows) read(r + step);   // on its way while this row is summed
-    row_sum<NT>(s, slots[turn]);
-    turn ^= 1;
-    const float m0 = s[0] / n, m1 = s[1] / n;
-    char* dx = A.out + r * A.ldo * T::kBytes;
+      if (AHEAD > 0 && r + D * step < A.rows) read(u, r + D * step);
+      row_sum<NT>(s, slots[turn]);
+      turn ^= 1;
+      const float m0 = s[0] / n, m1 = s[1] / n;
+      char* dx = A.out + r * A.ldo * T::kBytes;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      float o[W];
+      for (int j = 0; j < V; ++j) {
+        float o[W];
 #pragma unroll
-      for (int i = 0; i < W; ++i) o[i] = scale * (g[j * W + i] - m0 - h[j * W + i] * m1);
-      store_vec<T>(dx, (j * NT + t) * W, d, o);
+        for (int i = 0; i < W; ++i) o[i] = scale * (g[j * W + i] - m0 - h[j * W + i] * m1);
+        store_vec<T>(dx, (j * NT + t) * W, d, o);
+      }
+      r += step;
     }
   }
-  if (A.part == nullptr) return;
-  float* part = A.part + int64_t(blockIdx.x) * 2 * d;
-  if constexpr (RB > 1) {   // the block's rows first, one after the other
+  // the sums of the block's rows: to its line of partial sums, or as the result
+  float *to_w = A.dweight, *to_b = A.dbias;
+  if (A.part != nullptr) {
+    to_w = A.part + int64_t(blockIdx.x) * 2 * d;
+    to_b = to_w + d;
+  }
+  if (to_w == nullptr && to_b == nullptr) return;
+  auto put = [&](int c, float sw, float sb) {
+    if (c >= d) return;
+    if (to_w != nullptr) to_w[c] = sw;
+    if (to_b != nullptr) to_b[c] = sb;
+  };
+  if constexpr (RB > 1) {   // the waves' rows first, one after the other
     __shared__ float sums[2 * NT * E];
     for (int q = 0; q < RB; ++q) {
       if (int(threadIdx.x) / NT == q)
@@ -193,19 +219,10 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
         }
       __syncthreads();
     }
-    for (int c = threadIdx.x; c < d; c += block_threads<NT>()) {
-      part[c] = sums[c];
-      part[d + c] = sums[NT * E + c];
-    }
+    for (int c = threadIdx.x; c < d; c += block_threads<NT>()) put(c, sums[c], sums[NT * E + c]);
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (e / W * NT + t) * W + e % W;
-      if (c < d) {
-        part[c] = aw[e];
-        part[d + c] = ab[e];
-      }
-    }
+    for (int e = 0; e < E; ++e) put((e / W * NT + t) * W + e % W, aw[e], ab[e]);
   }
 }
 
@@ -348,13 +365,16 @@ template <class T, int NT, int E>
 hipError_t forward(const NormArgs& A, hipStream_t st) {
   constexpr int RB = block_threads<NT>() / NT;
   const int blocks = int(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, kMostBlocks));
-  hipLaunchKernelGGL((k_norm<T, NT, E>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
+  if (A.d % T::W == 0) hipLaunchKernelGGL((k_norm<T, NT, E, false>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
+  else hipLaunchKernelGGL((k_norm<T, NT, E, true>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
   return hipGetLastError();
 }
 
 template <class T, int NT, int E>
 hipError_t backward(const NormArgs& A, int blocks, hipStream_t st) {
-  hipLaunchKernelGGL((k_norm_backward<T, NT, E>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
+  const dim3 grid(blocks), block(block_threads<NT>());
+  if (A.d % T::W == 0) hipLaunchKernelGGL((k_norm_backward<T, NT, E, false>), grid, block, 0, st, A);
+  else hipLaunchKernelGGL((k_norm_backward<T, NT, E, true>), grid, block, 0, st, A);
   return hipGetLastError();
 }
 
@@ -398,6 +418,8 @@ hipError_t launch_norm(const NormArgs& A, bool f32, hipStream_t st) {
 
 int norm_blocks(int64_t rows, int64_t d) {
   const int rb = d <= 1024 ? 4 : 1;
+  // a few rows are summed by one workgroup, without the second launch
+  if (d <= kNormMaxFused && rows > 0 && rows <= 4 * rb) return 1;
   const int most = d > kNormMaxFused ? 64 : d > 4096 ? 256 : 512;
   return int(std::min<int64_t>((rows + rb - 1) / rb, most));
 }

@@ -146,8 +146,10 @@ tm_status layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64
   A.ldo = lddx;
   A.rows = int32_t(rows);
   A.d = int32_t(d);
-  const bool params = dweight != nullptr || dbias != nullptr;
+  A.dweight = dweight;
+  A.dbias = dbias;
   const int blocks = tmk::norm_blocks(rows, d);
+  const bool params = (dweight != nullptr || dbias != nullptr) && (blocks != 1 || d > tmk::kNormMaxFused);
   const size_t bytes = params ? size_t(blocks) * 2u * size_t(d) * 4u : 0u;
   return run_op(TM_PHASE_LAYER_NORM_BACKWARD, bytes, stream, [&](char* ws, hipStream_t st) {
     A.part = params ? reinterpret_cast<float*>(ws) : nullptr;
@@ -190,9 +192,10 @@ tm_status expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, 
   A.experts = int32_t(experts);
   A.k = int32_t(k);
   A.n = int32_t(n);
-  return run_op(TM_PHASE_EXPERT_MATMUL, 0, stream, [&](char*, hipStream_t st) {
-    return tmk::launch_expert_matmul(A, dtype == TM_DTYPE_F32, transposed != 0, st);
-  });
+  const bool f32 = dtype == TM_DTYPE_F32, trans = transposed != 0;
+  const tmk::ExpertPlan P = tmk::plan_expert_matmul(A, f32, trans);
+  return run_op(TM_PHASE_EXPERT_MATMUL, size_t(P.bytes), stream,
+                [&](char* ws, hipStream_t st) { return tmk::launch_expert_matmul(A, P, f32, trans, ws, st); });
 }
 
 tm_status expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* ends, void* dw,
@@ -224,9 +227,10 @@ tm_status expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy,
   A.experts = int32_t(experts);
   A.k = int32_t(k);
   A.n = int32_t(n);
-  return run_op(TM_PHASE_EXPERT_WGRAD, 0, stream, [&](char*, hipStream_t st) {
-    return tmk::launch_expert_wgrad(A, dtype == TM_DTYPE_F32, out_dtype == TM_DTYPE_F32, st);
-  });
+  const bool f32 = dtype == TM_DTYPE_F32, out_f32 = out_dtype == TM_DTYPE_F32;
+  const tmk::ExpertPlan P = tmk::plan_expert_wgrad(A, f32);
+  return run_op(TM_PHASE_EXPERT_WGRAD, size_t(P.bytes), stream,
+                [&](char* ws, hipStream_t st) { return tmk::launch_expert_wgrad(A, P, f32, out_f32, ws, st); });
 }
 
 tm_status check_temperature(float t) {

@@ -20,7 +20,8 @@ struct NormArgs {
   const float* bias;    // nullptr: zeros
   float* mean;          // forward: written; backward: read
   float* rstd;
-  float* part;          // backward: column sums of each block, [blocks][2][d]; nullptr: none wanted
+  float* part;          // backward: column sums of each block, [blocks][2][d]; nullptr: one block, or none wanted
+  float *dweight, *dbias;   // where a single block puts them
   int64_t ldx, lddy, ldo;
   int32_t rows, d;
   float eps;
@@ -46,12 +47,28 @@ struct ExpertArgs {
   int64_t lda, ldb, ldo;
   int64_t stride_b;     // elements from one expert's matrix to the next (b, or out of a weight gradient)
   int32_t rows, experts, k, n;
+  int32_t slices;       // of the summed index, each with a result of its own:
+  int64_t slice_out;    // elements from one slice's result to the next
 };
 
-hipError_t launch_expert_matmul(const ExpertArgs& A, bool f32, bool transposed, hipStream_t st);
-hipError_t launch_expert_matmul_tiles(const ExpertArgs& A, bool transposed, hipStream_t st);
-hipError_t launch_expert_wgrad_tiles(const ExpertArgs& A, bool out_f32, hipStream_t st);
-hipError_t launch_expert_wgrad(const ExpertArgs& A, bool f32, bool out_f32, hipStream_t st);
+// How a call is run: by which tiles, and over how many slices of the summed index.
+struct ExpertPlan {
+  bool staged;          // through registers: fp32, operands that are not 16-byte aligned, groups of a few rows
+  int tile, slices;
+  uint64_t bytes;       // workspace: the slices' results
+};
+
+ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed);
+ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32);
+hipError_t launch_expert_matmul(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool transposed, char* ws,
+                                hipStream_t st);
+hipError_t launch_expert_wgrad(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool out_f32, char* ws,
+                               hipStream_t st);
+// The launches that these are made of.
+hipError_t launch_rows_tiles(const ExpertArgs& A, const ExpertPlan& P, bool transposed, hipStream_t st);
+hipError_t launch_wgrad_tiles(const ExpertArgs& A, const ExpertPlan& P, bool out_f32, hipStream_t st);
+hipError_t launch_rows_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool transposed, hipStream_t st);
+hipError_t launch_wgrad_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool out_f32, hipStream_t st);
 
 // ---------------------------------------------------------------- policy loss
 struct LossArgs {

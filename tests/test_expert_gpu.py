@@ -66,6 +66,10 @@ CASES = [
     ([300, 1, 0, 255, 257], 200, 264), ([1] * 70 + [0] * 60 + [5] * 10, 72, 40), ([700], 515, 777),
     ([31, 33], 1000, 24), ([129, 127], 24, 1000), ([400, 0, 112], 768, 520), ([2, 3, 1, 2], 1024, 2048),
     ([9, 15, 0, 8, 40], 264, 520), ([1000, 24], 320, 384), ([513, 600], 576, 1032),
+    # few tiles, a long summed index
+    ([24, 9], 4096, 64), ([5, 0, 40], 3001, 50), ([6000], 64, 48), ([5000, 100, 3333], 33, 65),
+    # many tiles
+    ([900, 1200, 50, 0, 700], 1001, 1537), ([900, 1200, 50, 0, 700], 1024, 3200),
 ]
 
 
