@@ -68,51 +68,73 @@ int slices_for(uint64_t tiles, uint64_t K, uint64_t want, uint64_t least) {
 
 using namespace expert;
 
-// Rows: groups of up to 24 rows on average are bound by the reading of their
-// matrices and take the staged tiles of 16 or 32 rows, whatever the type and
-// alignment (63 rows over 53 experts of 192 x 6976, bf16: 24 us on 16-row tiles,
-// 57 on the 64 tile of direct loads; 80 rows over 5 experts of 7960 x 1970, fp32:
-// 108 us on 32 rows, 144 on 16, 184 on 64: the larger groups of an uneven call
-// should not need two tiles).  fp32 and odd operands stay with 32 rows up to 64
-// (105 rows over 2 experts of 4869 x 5632, odd: 47 us, 51 on the 64 tile).
-// Direct loads take the 256 tile from about one and a half tiles per compute
-// unit on (16384 rows, 8 experts of 4096 x 14336: 1.50 ms, 2.23 on 128, 2.97 on
-// 64; 24 rows, 8 experts of 768 x 2048: 19 us, 9 on 64), staged ones the 128 tile
-// from two (with 256 or 1024 in place of 512 the calls on either side lose a few
-// per cent).
+// Tile and slices of a call by its number of tiles of each size and the length
+// of its summed index (times in us, measured on both sides of each line).
 //
-// Slices of no less than eight stages, 256 values of fp32 and 512 of bf16 (7 rows,
-// 2 experts of 4608 x 64, fp32: 14.5 us, 17.5 from 512 on, 16.6 from 128 on, 72
-// unsplit; 24 rows, 8 experts of 768 x 2048, bf16: 9 us, 12 when split from 256 on).
-ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
+// Direct loads: the 256 tile from 256 tiles on (16384 rows of 1024 x 1024, 260
+// tiles: 35, 44 on 128, 58 on 64; 16384 rows over 16 experts of 512 x 512, 160: 21
+// against 16); the 128 tile from 256 on (4096 rows over 8 of 1024 x 1024, 320: 18, 22
+// on 64; 2048 over 4 of 2048 x 768, 120: 29 against 17), weight gradients from 384
+// on (512 of them: 19, 22 on 64; 256: 24 against 20).
+// Staged bf16 is further from the matrix cores, and the 128 tile pays from 192 on
+// (2048 rows of 2048 x 2048, 272: 39, 51 on 64; 120: 38 against 25), a long summed
+// index also in two slices (4096 rows of 4096 x 1024, 264: 65, 72 in one) or from 64
+// tiles on (gradient of 1024 x 1024 over 16384 rows: 62 in eight, 91 on 64).
+// Staged fp32 runs at the same rate on both; the small tile balances better.
+// The 64 tile: slices up to about two workgroups per compute unit (1024 rows of
+// 8192 x 1024, direct loads, 272 tiles: 44, 34 and 40 in 1, 2 and 4), fp32 three
+// (24211 rows, gradient of 896 x 128: 64, 67 and 75 with 512, 768 and 1536; 17221
+// rows over 19 of 1280 x 64: 51, 44 and 45), each of eight stages at least (7 rows over 2
+// of 4608 x 64, fp32: 14.5, 17.5 from sixteen on, 16.6 from four on, 72 unsplit).
+ExpertPlan plan_tiles(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K) {
+  const uint64_t t64 = tiles[0], t128 = tiles[1], t256 = tiles[2];
   ExpertPlan P{};
-  P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) && A.stride_b % 8 == 0 &&
-                      whole(A.out, A.ldo, A.n));
-  const uint64_t groups = uint64_t(std::min(A.experts, A.rows));
-  auto tiles = [&](uint64_t TM, uint64_t TN) { return (uint64_t(A.rows) / TM + groups) * up(A.n, TN); };
-  const uint64_t mean = uint64_t(A.rows) / groups;
-  if (!P.staged && mean > 24) {
-    P.tile = tiles(256, 256) >= 384 ? 256 : 64;
-    P.slices = P.tile == 64 ? slices_for(tiles(64, 64), A.k, 512, 512) : 1;
-  } else {
-    P.staged = true;
-    P.tile = mean <= 8 ? 16 : mean <= 64 ? 32 : tiles(128, 128) >= 512 ? 128 : 64;
-    P.slices = P.tile == 128 ? 1 : slices_for(tiles(P.tile, 64), A.k, 1024, f32 ? 256 : 512);
+  P.staged = staged;
+  P.tile = 64;
+  P.slices = 1;
+  if (!staged) {
+    if (t256 >= 256) P.tile = 256;
+    else if (t128 >= (wgrad ? 384u : 256u)) P.tile = 128;
+  } else if (f32) {
+    if (t128 >= 512) P.tile = 128;
+  } else if (t128 >= 192 || (t128 >= 64 && K >= 8192)) {
+    P.tile = 128;
+    if (K >= 4096) P.slices = slices_for(t128, K, 544, 512);
   }
-  if (P.slices > 1) P.bytes = uint64_t(P.slices) * uint64_t(A.rows) * uint64_t(A.n) * 4u;
+  if (P.tile == 64) P.slices = f32 ? slices_for(t64, K, 768, 256) : slices_for(t64, K, 544, 512);
   return P;
 }
 
-// Weight gradients: the same lines for the number of tiles; the summed index is
-// a group's rows (24211 rows, one expert, 896 x 128, fp32: 71 us in 36 slices).
+// Groups of up to 24 rows on average are bound by the reading of their matrices
+// and take the staged tiles of 16 or 32 rows, whatever the type and alignment (63
+// rows over 53 experts of 192 x 6976, bf16: 26 on 16 rows, 57 on the 64 tile of
+// direct loads; 80 rows over 5 of 7960 x 1970, fp32: 95 on 32 rows, 184 on 64: the
+// larger groups of an uneven call should not need two tiles).  fp32 and odd
+// operands stay with 32 rows up to 64 (105 rows over 2 of 4869 x 5632, odd: 47, 51 on
+// the 64 tile).
+ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
+  const bool staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) &&
+                               A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
+  const uint64_t groups = uint64_t(std::min(A.experts, A.rows)), mean = uint64_t(A.rows) / groups;
+  auto tiles = [&](uint64_t TM, uint64_t TN) { return (uint64_t(A.rows) / TM + groups) * up(A.n, TN); };
+  ExpertPlan P;
+  if (mean <= (staged ? 64u : 24u)) {
+    P.staged = true;
+    P.tile = mean <= 8 ? 16 : 32;
+    P.slices = slices_for(tiles(P.tile, 64), A.k, 1024, f32 ? 256 : 512);
+  } else {
+    P = plan_tiles(staged, f32, false, {tiles(64, 64), tiles(128, 128), tiles(256, 256)}, A.k);
+  }
+  P.bytes = P.slices > 1 ? uint64_t(P.slices) * uint64_t(A.rows) * uint64_t(A.n) * 4u : 0u;
+  return P;
+}
+
 ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
-  ExpertPlan P{};
-  P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
+  const bool staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 &&
+                               whole(A.out, A.ldo, A.n));
   auto tiles = [&](uint64_t T) { return uint64_t(A.experts) * up(A.k, T) * up(A.n, T); };
-  const uint64_t mean = uint64_t(A.rows) / uint64_t(A.experts);
-  P.tile = P.staged ? (tiles(128) >= 512 ? 128 : 64) : tiles(256) >= 384 ? 256 : 64;
-  P.slices = P.tile == 64 ? slices_for(tiles(64), mean, P.staged ? 1024 : 512, f32 ? 256 : 512) : 1;
-  if (P.slices > 1) P.bytes = uint64_t(P.slices) * uint64_t(A.experts) * uint64_t(A.k) * uint64_t(A.n) * 4u;
+  ExpertPlan P = plan_tiles(staged, f32, true, {tiles(64), tiles(128), tiles(256)}, uint64_t(A.rows) / uint64_t(A.experts));
+  P.bytes = P.slices > 1 ? uint64_t(P.slices) * uint64_t(A.experts) * uint64_t(A.k) * uint64_t(A.n) * 4u : 0u;
   return P;
 }
 

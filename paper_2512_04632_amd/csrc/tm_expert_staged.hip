@@ -386,7 +386,7 @@ hipError_t wgrad_staged(const ExpertArgs& A, hipStream_t st) {
 
 using Tile16 = Shape<16, 64, 1, 3>;
 using Tile32 = Shape<32, 64, 2, 3>;
-using Tile64 = Shape<64, 64, 2, 3>;
+using Tile64 = Shape<64, 64, 2, 2>;
 using Tile128 = Shape<128, 128, 2, 1>;
 
 template <class T, class TO>

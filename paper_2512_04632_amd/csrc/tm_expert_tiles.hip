@@ -1,5 +1,5 @@
-// Expert products of bf16 rows on the matrix cores: square tiles of 256 or
-// 64 fed by direct global -> LDS loads, for operands whose rows are 16-byte
+// Expert products of bf16 rows on the matrix cores: square tiles of 256, 128
+// or 64 fed by direct global -> LDS loads, for operands whose rows are 16-byte
 // aligned (the others: tm_expert_staged.hip).
 //
 //   rows    out tile = a rows (summed index contiguous) x W (k x n: row-major,
@@ -326,11 +326,13 @@ hipError_t wgrad_t(const ExpertArgs& A, hipStream_t st) {
 
 hipError_t launch_rows_tiles(const ExpertArgs& A, const ExpertPlan& P, bool transposed, hipStream_t st) {
   if (P.tile == 256) return expert::rows_t<256, 64, false>(A, transposed, st);
+  if (P.tile == 128) return expert::rows_t<128, 32, false>(A, transposed, st);
   return P.slices > 1 ? expert::rows_t<64, 64, true>(A, transposed, st) : expert::rows_t<64, 64, false>(A, transposed, st);
 }
 
 hipError_t launch_wgrad_tiles(const ExpertArgs& A, const ExpertPlan& P, bool out_f32, hipStream_t st) {
   if (P.tile == 256) return out_f32 ? expert::wgrad_t<256, 64, true>(A, st) : expert::wgrad_t<256, 64, false>(A, st);
+  if (P.tile == 128) return out_f32 ? expert::wgrad_t<128, 32, true>(A, st) : expert::wgrad_t<128, 32, false>(A, st);
   return out_f32 || P.slices > 1 ? expert::wgrad_t<64, 64, true>(A, st) : expert::wgrad_t<64, 64, false>(A, st);
 }
 
