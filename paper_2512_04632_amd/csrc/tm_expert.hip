@@ -76,11 +76,12 @@ using namespace expert;
 // against 16); the 128 tile from 256 on (4096 rows over 8 of 1024 x 1024, 320: 18, 22
 // on 64; 2048 over 4 of 2048 x 768, 120: 29 against 17), weight gradients from 384
 // on (512 of them: 19, 22 on 64; 256: 24 against 20).
-// Staged bf16 is further from the matrix cores, and the 128 tile pays from 192 on
-// (2048 rows of 2048 x 2048, 272: 39, 51 on 64; 120: 38 against 25), a long summed
-// index also in two slices (4096 rows of 4096 x 1024, 264: 65, 72 in one) or from 64
-// tiles on (gradient of 1024 x 1024 over 16384 rows: 62 in eight, 91 on 64).
-// Staged fp32 runs at the same rate on both; the small tile balances better.
+// Staged bf16: the 128 tile from 192 on (2048 rows of 2048 x 2048, 272: 35, 44 on 64;
+// 2048 over 4 of 2048 x 768, 120: 34 against 25), a long summed index from 64 on, in
+// slices (gradient of 1024 x 1024 over 16384 rows: 61 in eight, 88 on 64).
+// Staged fp32: from 512 on (1043 rows over 10 of 1408 x 3520, 504: 133, 119 on 64; 8216 over
+// 20 of 192 x 1088, 756: 42 against 50), a long summed index as bf16 (the same
+// gradient: 213, 285 on 64).
 // The 64 tile: slices up to about two workgroups per compute unit (1024 rows of
 // 8192 x 1024, direct loads, 272 tiles: 44, 34 and 40 in 1, 2 and 4), fp32 three
 // (24211 rows, gradient of 896 x 128: 64, 67 and 75 with 512, 768 and 1536; 17221
@@ -95,9 +96,7 @@ ExpertPlan plan_tiles(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)
   if (!staged) {
     if (t256 >= 256) P.tile = 256;
     else if (t128 >= (wgrad ? 384u : 256u)) P.tile = 128;
-  } else if (f32) {
-    if (t128 >= 512) P.tile = 128;
-  } else if (t128 >= 192 || (t128 >= 64 && K >= 8192)) {
+  } else if (t128 >= (f32 ? 512u : 192u) || (t128 >= 64 && K >= 8192)) {
     P.tile = 128;
     if (K >= 4096) P.slices = slices_for(t128, K, 544, 512);
   }

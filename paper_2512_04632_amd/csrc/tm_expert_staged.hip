@@ -22,10 +22,21 @@
 // value 16 s + 4 g + j of both operands, so that a contiguous operand is read
 // 16 bytes a lane.
 //
-// fp32 is bound by the matrix cores on large tiles (a 128 x 128 stage is 2048
-// clocks of them against some 300 of LDS reads), so rows that only fill a tile
-// cost as much as real ones: groups of a few rows take tiles of 16 or 32 rows,
-// which are bound by the reading of the matrices.
+// fp32 on the 128 tile goes as three bf16 parts, x = hi + mid + lo, each rounded to
+// nearest from what the ones before it leave: 8 bits each, all 24 of x together.
+// A product is hi hi + hi mid + mid hi + mid mid + hi lo + lo hi in one fp32 accumulator,
+// small terms first; mid lo, lo mid and lo lo, at most 2^-23 of it, are left out.  Six
+// bf16 instructions take 96 clocks where the eight of fp32 for the same 32 values
+// take 256 (16384 rows over 8 experts of 2048 x 2048: 0.80 ms, 172 TFLOP/s, against 1.03 ms
+// of fp32 instructions).  Values that three parts cannot hold (NaN, infinities, and
+// the few that round to one) set a flag, and the tile is done again with fp32
+// instructions; parts below the smallest normal number may vanish (x below about
+// 2^-110 keeps fewer bits).  On the smaller tiles the splitting costs what the
+// instructions save (2048 rows of 1024 x 1024: 45 us, 40 without; 80 rows over 5 experts
+// of 7960 x 1970: 111 against 95), and fp32 multiplies as it is.
+//
+// Rows that only fill a tile cost as much as real ones: groups of a few rows take
+// tiles of 16 or 32 rows, which are bound by the reading of the matrices.
 #include "tm_elem.h"
 #include "tm_expert.h"
 #include "tm_tile.h"
@@ -98,9 +109,12 @@ struct Stager {
       p[i] = s.p + (r * s.ld + c * T::W) * T::kBytes;
     }
   }
-  // Stage at k0, in steps of BK.
+  // Stage at k0, in steps of BK.  FAST: known to need no check (the main loops'
+  // way: with the checked loads' branches beside them, every wait for a stage that
+  // was loaded long ago would be a wait for all loads under way).
+  template <bool FAST>
   __device__ void load(int k0, u32x4_t (&v)[Q]) {
-    if (k0 + BK <= whole) {
+    if (FAST || k0 + BK <= whole) {
 #pragma unroll
       for (int i = 0; i < Q; ++i)
         if (mine(i)) v[i] = T::load(p[i]);
@@ -213,8 +227,35 @@ struct Shape {
   static constexpr int A_BYTES = TM * kStageBytes, STAGE = (TM + TN) * kStageBytes;
   static constexpr int ROW = 2 * TN + 16;   // of the bf16 output stage
   static constexpr int LDS = 2 * STAGE > TM * ROW ? 2 * STAGE : TM * ROW;
+  static constexpr bool kParts = TM >= 128;   // fp32 as three bf16 parts
+  static_assert(3 * 64 * (TM + TN) <= 2 * STAGE, "a stage of their planes takes less than two stages");
+  static constexpr int kWaves = TM >= 128 ? 2 : 3;   // per SIMD, for the register allocation
   static_assert(FM >= 1 && FN >= 1, "a block for every wave");
 };
+
+// begin(fast), then step(kt, kt % D, fast) for each stage kt < nk; fast (a constant)
+// while the stages that they load, at most D for begin and kt + D for a step, are
+// among the first `unchecked` (steps that load one further say one less).  The
+// fast steps follow a beginning of their own: with the other's branches in front of
+// them the compiler would wait for every load under way before each use.
+template <int D, class FB, class F>
+__device__ inline void staged_loop(int nk, int unchecked, FB begin, F step) {
+  int kt = 0;
+  if (unchecked >= 2 * D) {
+    begin(std::true_type{});
+    do {
+#pragma unroll
+      for (int u = 0; u < D; ++u) step(kt + u, u, std::true_type{});
+      kt += D;
+    } while (kt + 2 * D <= unchecked);
+  } else {
+    begin(std::false_type{});
+  }
+  for (; kt < nk; kt += D)
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+      if (kt + u < nk) step(kt + u, u, std::false_type{});
+}
 
 // acc = the tile's product over K values.
 template <class T, class S, bool AKC, bool BKC>
@@ -234,41 +275,169 @@ __device__ inline void product_staged(f32x4_t (&acc)[S::FM][S::FN], char* smem, 
   sa.start(a, K);
   sb.start(b, K);
   const int nk = (K + BK - 1) / BK;
-  sa.load(0, va[0]);
-  sb.load(0, vb[0]);
-  sa.store(smem, va[0]);
-  sb.store(smem + S::A_BYTES, vb[0]);
+  auto begin = [&](auto fast) __attribute__((always_inline)) {
+    constexpr bool FAST = decltype(fast)::value;
+    sa.template load<FAST>(0, va[0]);
+    sb.template load<FAST>(0, vb[0]);
+    sa.store(smem, va[0]);
+    sb.store(smem + S::A_BYTES, vb[0]);
 #pragma unroll
-  for (int u = 0; u < D; ++u)
-    if (u + 1 < nk) {
-      sa.load((u + 1) * BK, va[u]);
-      sb.load((u + 1) * BK, vb[u]);
-    }
-  __syncthreads();
-  for (int k0 = 0; k0 < nk; k0 += D)
-#pragma unroll
-    for (int u = 0; u < D; ++u) {
-      const int kt = k0 + u;
-      if (kt >= nk) break;
-      const char* st = smem + (kt & 1) * S::STAGE;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        typename SliceOf<T>::V fa[S::FM], fb[S::FN];
-        load_slice<S::TM, AKC, S::FM>(T{}, fa, st, s, wm);
-        load_slice<S::TN, BKC, S::FN>(T{}, fb, st + S::A_BYTES, s, wn);
-        mma_slice<S::FM, S::FN>(T{}, acc, fa, fb);
+    for (int u = 0; u < D; ++u)
+      if (FAST || u + 1 < nk) {
+        sa.template load<FAST>((u + 1) * BK, va[u]);
+        sb.template load<FAST>((u + 1) * BK, vb[u]);
       }
-      if (kt + 1 < nk) {
-        char* nx = smem + ((kt + 1) & 1) * S::STAGE;   // last read before the previous barrier
-        sa.store(nx, va[u]);
-        sb.store(nx + S::A_BYTES, vb[u]);
-        if (kt + 1 + D < nk) {
-          sa.load((kt + 1 + D) * BK, va[u]);
-          sb.load((kt + 1 + D) * BK, vb[u]);
-        }
-      }
-      __syncthreads();
+    __syncthreads();
+  };
+  auto step = [&](int kt, int u, auto fast) __attribute__((always_inline)) {
+    constexpr bool FAST = decltype(fast)::value;
+    const char* st = smem + (kt & 1) * S::STAGE;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      typename SliceOf<T>::V fa[S::FM], fb[S::FN];
+      load_slice<S::TM, AKC, S::FM>(T{}, fa, st, s, wm);
+      load_slice<S::TN, BKC, S::FN>(T{}, fb, st + S::A_BYTES, s, wn);
+      mma_slice<S::FM, S::FN>(T{}, acc, fa, fb);
     }
+    if (FAST || kt + 1 < nk) {
+      char* nx = smem + ((kt + 1) & 1) * S::STAGE;   // last read before the previous barrier
+      sa.store(nx, va[u]);
+      sb.store(nx + S::A_BYTES, vb[u]);
+      if (FAST || kt + 1 + D < nk) {
+        sa.template load<FAST>((kt + 1 + D) * BK, va[u]);
+        sb.template load<FAST>((kt + 1 + D) * BK, vb[u]);
+      }
+    }
+    __syncthreads();
+  };
+  staged_loop<D>(nk, min(sa.whole, sb.whole) / BK - 1, begin, step);
+}
+
+// The three parts of four values, each as four bf16 (hi first).  True if one of
+// the values has none: not finite, or past the largest bf16.
+__device__ inline bool split3(u32x4_t q, uint2 (&part)[3]) {
+  float x[4];
+  F32::unpack(q, x);
+  const float most = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+  bool bad = !(most < 3.38e38f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= x[i] != x[i];   // fmaxf passes a NaN over
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = f2bf(x[i]);
+      if (p < 2) x[i] -= __uint_as_float(h[i] << 16);   // exact
+    }
+    part[p] = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+  }
+  return bad;
+}
+
+// A stage of 32 fp32 values as three planes in LDS, TS * 64 bytes each: a
+// contiguous operand as rows of 64 bytes, 16-byte chunks XORed by (row / 4) % 4;
+// a row-major one as rows of the tile's columns, as for bf16.
+template <int TS, bool KC, int Q>
+__device__ inline bool store3(char* lds, const u32x4_t (&v)[Q]) {
+  using St = Stager<F32, TS, KC>;
+  static_assert(TS * kStageBytes % 4096 == 0, "a chunk for every thread");
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < Q; ++i) {
+    const int r = St::row(i), c = St::chunk(i);
+    const int at = KC ? r * 64 + 16 * ((c >> 1) ^ ((r / 4) % 4)) + 8 * (c & 1)
+                      : r * 2 * TS + 32 * ((c >> 2) ^ swz_y<TS>(r)) + 8 * (c & 3);
+    uint2 part[3];
+    bad |= split3(v[i], part);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(lds + p * TS * 64 + at) = part[p];
+  }
+  return bad;
+}
+
+// One plane's operands: 8 values 8 g .. + 7 of row or column 16 (w F + f) + lane % 16.
+template <int TS, bool KC, int F>
+__device__ inline void load_plane(uint4 (&v)[F], const char* st, int w) {
+  if constexpr (KC) {
+    const int lr = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      const int r = (w * F + f) * 16 + lr;
+      v[f] = *reinterpret_cast<const uint4*>(st + r * 64 + 16 * (g ^ ((r / 4) % 4)));
+    }
+  } else {
+    load_slice<TS, false, F>(Bf16{}, v, st, 0, w);
+  }
+}
+
+// fp32 as three parts, in one LDS buffer with two barriers a stage, so that two
+// workgroups share a compute unit.  False if a value has no parts.
+template <class S, bool AKC, bool BKC>
+__device__ inline bool product_parts(f32x4_t (&acc)[S::FM][S::FN], char* smem, const Source& a, const Source& b, int K) {
+  using SA = Stager<F32, S::TM, AKC>;
+  using SB = Stager<F32, S::TN, BKC>;
+  constexpr int BK = SA::BK, D = S::D, PA = S::TM * 64, PB = S::TN * 64;
+  const int wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
+#pragma unroll
+  for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (K <= 0) return true;
+  SA sa;
+  SB sb;
+  u32x4_t va[D][SA::Q], vb[D][SB::Q];
+  sa.start(a, K);
+  sb.start(b, K);
+  const int nk = (K + BK - 1) / BK;
+  bool bad = false;
+  auto store = [&](char* lds, const u32x4_t (&qa)[SA::Q], const u32x4_t (&qb)[SB::Q]) __attribute__((always_inline)) {
+    bad |= store3<S::TM, AKC>(lds, qa);
+    bad |= store3<S::TN, BKC>(lds + 3 * PA, qb);
+  };
+  auto multiply = [&](const char* lds) __attribute__((always_inline)) {
+    uint4 fb[3][S::FN];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) load_plane<S::TN, BKC, S::FN>(fb[p], lds + 3 * PA + p * PB, wn);
+#pragma unroll
+    for (int p = 2; p >= 0; --p) {   // a's parts, small ones first, each with those of b that count
+      uint4 fa[S::FM];
+      load_plane<S::TM, AKC, S::FM>(fa, lds + p * PA, wm);
+#pragma unroll
+      for (int q = 2 - p; q >= 0; --q) mma_slice<S::FM, S::FN>(Bf16{}, acc, fa, fb[q]);
+    }
+  };
+  const int unchecked = min(sa.whole, sb.whole) / BK;
+  auto begin = [&](auto fast) __attribute__((always_inline)) {
+    constexpr bool FAST = decltype(fast)::value;
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+      if (FAST || u < nk) {
+        sa.template load<FAST>(u * BK, va[u]);
+        sb.template load<FAST>(u * BK, vb[u]);
+      }
+  };
+  staged_loop<D>(nk, unchecked, begin, [&](int kt, int u, auto fast) __attribute__((always_inline)) {
+    constexpr bool FAST = decltype(fast)::value;
+    if (kt > 0) __syncthreads();   // the stage before has been read
+    store(smem, va[u], vb[u]);
+    if (FAST || kt + D < nk) {
+      sa.template load<FAST>((kt + D) * BK, va[u]);
+      sb.template load<FAST>((kt + D) * BK, vb[u]);
+    }
+    __syncthreads();
+    multiply(smem);
+  });
+  return !__syncthreads_or(bad);
+}
+
+// The product in the type's way.
+template <class T, class S, bool AKC, bool BKC>
+__device__ inline void product_tile(f32x4_t (&acc)[S::FM][S::FN], char* smem, const Source& a, const Source& b, int K) {
+  if constexpr (T::kBytes == 4 && S::kParts) {
+    if (product_parts<S, AKC, BKC>(acc, smem, a, b, K)) return;
+  }
+  product_staged<T, S, AKC, BKC>(acc, smem, a, b, K);
 }
 
 // Row and first of the four columns that a lane holds of block (fm, fn).
@@ -326,7 +495,7 @@ __device__ inline void store_tile(F32, const f32x4_t (&acc)[S::FM][S::FN], char*
 
 // TO: type of the result, F32 for slices of the summed index.
 template <class T, class TO, class S, bool TRANS>
-__global__ __launch_bounds__(256) void k_rows_staged(const ExpertArgs A, int row_tiles) {
+__global__ __launch_bounds__(256, S::kWaves) void k_rows_staged(const ExpertArgs A, int row_tiles) {
   __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
   const int nJ = (A.n + S::TN - 1) / S::TN;
   const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
@@ -341,12 +510,12 @@ __global__ __launch_bounds__(256) void k_rows_staged(const ExpertArgs A, int row
   const Source b = TRANS ? Source{w + (c0 * A.ldb + k0) * T::kBytes, A.ldb, cols, A.n - c0}
                          : Source{w + (k0 * A.ldb + c0) * T::kBytes, A.ldb, cols, A.k - k0};
   f32x4_t acc[S::FM][S::FN];
-  product_staged<T, S, true, TRANS>(acc, smem, a, b, K);
+  product_tile<T, S, true, TRANS>(acc, smem, a, b, K);
   store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + g.first * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
 }
 
 template <class T, class TO, class S>
-__global__ __launch_bounds__(256) void k_wgrad_staged(const ExpertArgs A) {
+__global__ __launch_bounds__(256, S::kWaves) void k_wgrad_staged(const ExpertArgs A) {
   __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
   const int nI = (A.k + S::TM - 1) / S::TM, nJ = (A.n + S::TN - 1) / S::TN;
   const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
@@ -360,7 +529,7 @@ __global__ __launch_bounds__(256) void k_wgrad_staged(const ExpertArgs A) {
   const Source a{A.a + (first * A.lda + r0) * T::kBytes, A.lda, rows, A.rows - first};
   const Source b{A.b + (first * A.ldb + c0) * T::kBytes, A.ldb, cols, A.rows - first};
   f32x4_t acc[S::FM][S::FN];
-  product_staged<T, S, false, false>(acc, smem, a, b, K);
+  product_tile<T, S, false, false>(acc, smem, a, b, K);
   store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + e * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo,
                 rows, cols);
 }

@@ -187,6 +187,34 @@ def test_offsets_past_32_bits():
         _close(dw[e], x[rng].double().t() @ dy[rng].double(), x[rng].double().abs().t() @ dy[rng].double().abs(), rows, "f32")
 
 
+def test_fp32_values_that_have_no_bf16_parts():
+    """Values up to the largest fp32 and infinities take the fp32 products: the largest value
+    times one stays, an infinity times a value is that infinity, not NaN; small and large
+    entries in one product keep the accuracy of fp32."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    for rows, k, n in ((200, 96, 130), (700, 40, 1000)):
+        x, w = _randn(g, (rows, k), "f32"), _randn(g, (1, k, n), "f32")
+        x[3] = 0.0
+        x[3, 5] = torch.finfo(torch.float32).max
+        w[0, 5] = 1.0
+        w[0, 7] = 0.5 + w[0, 7].abs()
+        x[100, 7] = float("inf")
+        y = tm.expert_matmul(x, w, _ends([rows]))
+        assert (y[3] == torch.finfo(torch.float32).max).all()
+        assert (y[100] == float("inf")).all()
+        keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+        keep[3] = keep[100] = False
+        want = x[keep].double() @ w[0].double()
+        _close(y[keep], want, x[keep].double().abs() @ w[0].double().abs(), k, "f32")
+        x = _randn(g, (rows, k), "f32") * torch.logspace(-20, 10, k, device="cuda")
+        w = w * torch.logspace(15, -10, k, device="cuda")[None, :, None]
+        want, terms = x.double() @ w[0].double(), x.double().abs() @ w[0].double().abs()
+        _close(tm.expert_matmul(x, w, _ends([rows])), want, terms, k, "f32")
+        dy = _randn(g, (rows, n), "f32", 1e-25)
+        _check_wgrad(x, dy, [rows], "f32", tm.expert_wgrad(x, dy, _ends([rows])))
+
+
 def test_ends_that_make_no_sense_stay_in_bounds():
     """Decreasing or too large ends: the rows that they reach are computed, nothing else is touched."""
     g = torch.Generator(device="cuda")
