@@ -41,27 +41,32 @@ def _rows(t):
 
 def _vector(t, like, name: str, n: int, dtype):
     """A companion vector of n entries on like's device, contiguous."""
-    if t.dim() != 1 or t.shape[0] != n:
-        raise ValueError(f"{name} must have shape ({n},), not {tuple(t.shape)}")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} must be on the same device")
+    if t.dtype is not dtype or t.shape != (n,) or t.device != like.device:
+        raise ValueError(f"{name} must be a {dtype} vector of {n} entries on {like.device}, not a {t.dtype} "
+                         f"tensor of shape {tuple(t.shape)} on {t.device}")
     return t if t.is_contiguous() else t.contiguous()
+
+
+def _empty_like(t):
+    """A contiguous tensor of t's shape and type (for a contiguous t the cheaper call)."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _call(fn: str, index: int, stream, *args) -> None:
     """An operator's entry point on device `index`, the stream its last argument."""
-    f = getattr(_lib.lib(), fn)
-    if index == torch.cuda.current_device():
-        st = f(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    f = getattr(_lib._lib or _lib.lib(), fn)
+    if index == _current_device():
+        st = f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(index):
-            st = f(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+            st = f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
     if st != _lib.TM_OK:
         raise _lib.TurboMuonError(fn, st, _lib.last_error())
 
@@ -78,8 +83,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
         weight = _vector(weight, x, "weight", d, _F32)
     if bias is not None:
         bias = _vector(bias, x, "bias", d, _F32)
-    y = x.new_empty(x.shape)
-    mean, rstd = x.new_empty(rows, dtype=_F32), x.new_empty(rows, dtype=_F32)
+    y = _empty_like(x)
+    mean = x.new_empty(rows, dtype=_F32)
+    rstd = torch.empty_like(mean)
     _call("tm_layer_norm", x.get_device(), stream, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
           mean.data_ptr(), rstd.data_ptr(), rows, d, eps, code)
     return y, mean, rstd
@@ -96,10 +102,11 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, param_grads: bool = True
     mean, rstd = _vector(mean, x, "mean", rows, _F32), _vector(rstd, x, "rstd", rows, _F32)
     if weight is not None:
         weight = _vector(weight, x, "weight", d, _F32)
-    dx = x.new_empty(x.shape)
+    dx = _empty_like(x)
     dweight = dbias = None
     if param_grads:
-        dweight, dbias = x.new_empty(d, dtype=_F32), x.new_empty(d, dtype=_F32)
+        dweight = x.new_empty(d, dtype=_F32)
+        dbias = torch.empty_like(dweight)
     _call("tm_layer_norm_backward", x.get_device(), stream, dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
           mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), d, _ptr(dweight), _ptr(dbias), rows, d, code)
     return dx, dweight, dbias
@@ -181,12 +188,12 @@ def _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_
     if ref_logp is not None:
         ref_logp = _vector(ref_logp, logits, "ref_logp", rows, _F32)
     loss = logits.new_empty((), dtype=_F32)
-    logp = logits.new_empty(rows, dtype=_F32)
+    logp = torch.empty_like(weights)
     lse = slope = dlogits = None
     if grad:
-        dlogits = logits.new_empty((rows, vocab))
+        dlogits = _empty_like(logits)
     if keep:
-        lse, slope = logits.new_empty(rows, dtype=_F32), logits.new_empty(rows, dtype=_F32)
+        lse, slope = torch.empty_like(weights), torch.empty_like(weights)
     _call("tm_policy_loss", logits.get_device(), stream, l2.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), weights.data_ptr(), _ptr(ref_logp), clip_low, clip_high, kl, temperature,
           loss.data_ptr(), logp.data_ptr(), _ptr(lse), _ptr(slope), _ptr(dlogits), vocab, rows, vocab, code)
@@ -229,7 +236,7 @@ def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: fl
     slope = _vector(slope, logits, "slope", rows, _F32)
     if grad is not None and (grad.dim() != 0 or grad.dtype is not _F32 or grad.device != logits.device):
         raise ValueError("grad must be an fp32 scalar on the logits' device")
-    dlogits = logits.new_empty((rows, vocab))
+    dlogits = _empty_like(logits)
     _call("tm_policy_loss_backward", logits.get_device(), stream, l2.data_ptr(), ld, targets.data_ptr(),
           lse.data_ptr(), slope.data_ptr(), _ptr(grad), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
     return dlogits

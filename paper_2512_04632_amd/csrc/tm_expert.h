@@ -2,11 +2,13 @@
 // the device, the order of the tiles, operand reads and the output stage.
 //
 // The group sizes are only known on the device: a launch covers the most tiles
-// that any sizes can need, rows / T + experts + 1 rows of tiles, and each
-// workgroup finds its expert from `ends`; the ones left over end at once.
+// that any sizes can need, and each workgroup finds its expert from `ends`; the
+// ones left over end at once.
 // Rows after the last expert's belong to a group of their own without a
 // product and come out as zeros; so do the matrices of experts without rows.
 #pragma once
+
+#include <algorithm>
 
 #include "tm_ops.h"
 #include "tm_tile.h"
@@ -60,8 +62,13 @@ __device__ inline bool find_tile(const ExpertArgs& A, int tile, Group& out) {
   return false;
 }
 
-// Rows of T-row tiles that any group sizes can need.
-inline uint64_t row_tiles(const ExpertArgs& A, int T) { return uint64_t(A.rows) / T + uint64_t(A.experts) + 1; }
+// Rows of T-row tiles that any group sizes can need: the whole tiles, one more for
+// each group that has rows (the experts' and the one of no expert), and no more
+// than there are rows.
+inline uint64_t row_tiles(const ExpertArgs& A, int T) {
+  const uint64_t rows = uint64_t(A.rows), groups = std::min(uint64_t(A.experts) + 1, rows);
+  return std::min(rows / T + groups, rows);
+}
 inline uint64_t col_tiles(const ExpertArgs& A, int T) { return (uint64_t(A.n) + T - 1) / T; }
 inline uint64_t wgrad_tiles(const ExpertArgs& A, int T) {
   return uint64_t(A.experts) * ((uint64_t(A.k) + T - 1) / T) * col_tiles(A, T);

@@ -241,13 +241,11 @@ struct Shape {
 template <int D, class FB, class F>
 __device__ inline void staged_loop(int nk, int unchecked, FB begin, F step) {
   int kt = 0;
-  if (unchecked >= 2 * D) {
+  if (unchecked >= D) {
     begin(std::true_type{});
-    do {
+    for (; kt + 2 * D <= unchecked; kt += D)
 #pragma unroll
       for (int u = 0; u < D; ++u) step(kt + u, u, std::true_type{});
-      kt += D;
-    } while (kt + 2 * D <= unchecked);
   } else {
     begin(std::false_type{});
   }
