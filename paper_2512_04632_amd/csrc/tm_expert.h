@@ -32,11 +32,10 @@ __device__ inline Group group_of(const ExpertArgs& A, int e) {
   return g;
 }
 
-// Row tile `tile` (of T rows) of the launch: its group cut to the tile's rows.
-// Every lane of a wave calls it; the lanes look at 64 groups at a time.  False
-// past the last tile.
-template <int T>
-__device__ inline bool find_tile(const ExpertArgs& A, int tile, Group& out) {
+// Row tile `tile` (of T rows, counted from group to group) of the launch: its
+// group cut to the tile's rows.  Every lane of a wave calls it; the lanes look at
+// 64 groups at a time.  False past the last tile.
+__device__ inline bool find_tile(const ExpertArgs& A, int T, int tile, Group& out) {
   const int lane = threadIdx.x & 63;
   int before = 0;   // tiles of the groups looked at so far
   for (int base = 0; base <= A.experts; base += 64) {
@@ -70,8 +69,24 @@ inline uint64_t row_tiles(const ExpertArgs& A, int T) {
   return std::min(rows / T + groups, rows);
 }
 inline uint64_t col_tiles(const ExpertArgs& A, int T) { return (uint64_t(A.n) + T - 1) / T; }
-inline uint64_t wgrad_tiles(const ExpertArgs& A, int T) {
-  return uint64_t(A.experts) * ((uint64_t(A.k) + T - 1) / T) * col_tiles(A, T);
+// Blocks of a weight gradient on TM x TN tiles: the experts' matrices, or those of
+// the chunks of their rows.
+inline uint64_t wgrad_blocks(const ExpertArgs& A, int TM, int TN) {
+  return (A.chunk == 0 ? uint64_t(A.experts) : row_tiles(A, A.chunk)) * ((uint64_t(A.k) + TM - 1) / TM) * col_tiles(A, TN);
+}
+
+// Tiles (of T rows) of the groups before e; every lane of a wave calls it.
+__device__ inline int tiles_before(const ExpertArgs& A, int T, int e) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int base = 0; base < e; base += 64)
+    if (base + lane < e) {
+      const Group g = group_of(A, base + lane);
+      sum += (g.last - g.first + T - 1) / T;
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  return sum;
 }
 
 // A workgroup's tile and its slice z of the summed index.
@@ -162,6 +177,28 @@ __device__ inline void stage_bf16(const AccT<T>& acc, char* smem, FCol col) {
           make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
     }
   __syncthreads();
+}
+
+// A weight gradient's tile: rows [first, first + K) of expert e, summed into matrix
+// `out` of the result (or, with chunks, of the workspace).
+struct GradTile {
+  int e, out, tile, first, K;
+};
+// Block `block` of a launch over `tiles` tiles a matrix; false for one that has nothing to do.
+__device__ inline bool grad_tile(const ExpertArgs& A, int block, int blocks, int tiles, GradTile& t) {
+  const int id = xcd_remap(block, blocks);
+  t.out = id / tiles;
+  t.tile = id - t.out * tiles;
+  Group g;
+  if (A.chunk == 0) {
+    g = group_of(A, t.out);
+  } else if (!find_tile(A, A.chunk, t.out, g) || g.e == A.experts) {
+    return false;
+  }
+  t.e = __builtin_amdgcn_readfirstlane(g.e);
+  t.first = __builtin_amdgcn_readfirstlane(g.first);
+  t.K = __builtin_amdgcn_readfirstlane(g.last) - t.first;
+  return true;
 }
 
 }  // namespace expert

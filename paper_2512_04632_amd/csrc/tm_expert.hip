@@ -9,44 +9,69 @@
 #include <algorithm>
 
 #include "tm_elem.h"
-#include "tm_ops.h"
+#include "tm_expert.h"
 
 namespace tmk {
 namespace expert {
 
-// out = sum of the slices' results, in their order, each thread a vector: rows
-// of n, `per` of them a matrix and the matrices `stride` elements apart.
+// Entries c .. c + 3 of a row of n: the sum of `count` results that lie `apart`
+// elements from each other.
 template <class TO>
-__global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slices, char* out, int64_t ldo, int64_t per,
-                                                    int64_t stride, int64_t rows, int n) {
-  constexpr int W = elem::F32::W;
-  const int vecs = (n + W - 1) / W;
-  const int64_t slice = rows * n;
+__device__ inline void sum_vec(const float* part, int64_t apart, int count, char* out, int c, int n) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < count; ++z) {
+    float v[4];
+    elem::load_vec<elem::F32>(reinterpret_cast<const char*>(part + z * apart), c, n, 0.f, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += v[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < n) TO::store1(out + (c + i) * TO::kBytes, s[i]);
+}
+
+// out = sum of the slices' results, in their order, each thread a vector of the
+// rows x n result.
+template <class TO>
+__global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slices, char* out, int64_t ldo, int64_t rows, int n) {
+  const int vecs = (n + 3) / 4;
   const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
   const int64_t r = at / vecs;
   if (r >= rows) return;
-  const int c = int(at - r * vecs) * W;
-  float s[W] = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < slices; ++z) {
-    float v[W];
-    elem::load_vec<elem::F32>(reinterpret_cast<const char*>(part + z * slice + r * n), c, n, 0.f, v);
-#pragma unroll
-    for (int i = 0; i < W; ++i) s[i] += v[i];
-  }
-  char* to = out + (r / per * stride + r % per * ldo + c) * TO::kBytes;
-#pragma unroll
-  for (int i = 0; i < W; ++i)
-    if (c + i < n) TO::store1(to + i * TO::kBytes, s[i]);
+  sum_vec<TO>(part + r * n, rows * n, slices, out + r * ldo * TO::kBytes, int(at - r * vecs) * 4, n);
 }
 
-hipError_t sum_slices(const char* ws, int slices, bool out_f32, char* out, int64_t ldo, int64_t per, int64_t stride,
-                      int64_t rows, int n, hipStream_t st) {
+// out[e] = sum of the matrices of the chunks of e's rows, in their order; zeros for
+// an expert without rows.  `per` blocks a matrix.
+template <class TO>
+__global__ __launch_bounds__(256) void k_sum_chunks(const float* part, const ExpertArgs A, int per) {
+  const int e = int(blockIdx.x / uint32_t(per)), vecs = (A.n + 3) / 4;
+  const Group g = group_of(A, e);
+  const int before = tiles_before(A, A.chunk, e), chunks = (g.last - g.first + A.chunk - 1) / A.chunk;
+  const int64_t at = int64_t(blockIdx.x % uint32_t(per)) * 256 + threadIdx.x, r = at / vecs;
+  if (r >= A.k) return;
+  const int64_t size = int64_t(A.k) * A.n;
+  sum_vec<TO>(part + before * size + r * A.n, size, chunks, A.out + (e * A.stride_b + r * A.ldo) * TO::kBytes,
+              int(at - r * vecs) * 4, A.n);
+}
+
+hipError_t sum_slices(const char* ws, int slices, bool out_f32, char* out, int64_t ldo, int64_t rows, int n, hipStream_t st) {
   const float* part = reinterpret_cast<const float*>(ws);
   const uint64_t blocks = (uint64_t(rows) * ((uint64_t(n) + 3) / 4) + 255) / 256;
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
   const dim3 grid{uint32_t(blocks)};
-  if (out_f32) hipLaunchKernelGGL((k_sum_slices<elem::F32>), grid, dim3(256), 0, st, part, slices, out, ldo, per, stride, rows, n);
-  else hipLaunchKernelGGL((k_sum_slices<elem::Bf16>), grid, dim3(256), 0, st, part, slices, out, ldo, per, stride, rows, n);
+  if (out_f32) hipLaunchKernelGGL((k_sum_slices<elem::F32>), grid, dim3(256), 0, st, part, slices, out, ldo, rows, n);
+  else hipLaunchKernelGGL((k_sum_slices<elem::Bf16>), grid, dim3(256), 0, st, part, slices, out, ldo, rows, n);
+  return hipGetLastError();
+}
+
+hipError_t sum_chunks(const char* ws, const ExpertArgs& A, bool out_f32, hipStream_t st) {
+  const float* part = reinterpret_cast<const float*>(ws);
+  const uint64_t per = (uint64_t(A.k) * ((uint64_t(A.n) + 3) / 4) + 255) / 256, blocks = per * uint64_t(A.experts);
+  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  const dim3 grid{uint32_t(blocks)};
+  if (out_f32) hipLaunchKernelGGL((k_sum_chunks<elem::F32>), grid, dim3(256), 0, st, part, A, int(per));
+  else hipLaunchKernelGGL((k_sum_chunks<elem::Bf16>), grid, dim3(256), 0, st, part, A, int(per));
   return hipGetLastError();
 }
 
@@ -87,22 +112,16 @@ using namespace expert;
 // (24211 rows, gradient of 896 x 128: 64, 67 and 75 with 512, 768 and 1536; 17221
 // rows over 19 of 1280 x 64: 51, 44 and 45), each of eight stages at least (7 rows over 2
 // of 4608 x 64, fp32: 14.5, 17.5 from sixteen on, 16.6 from four on, 72 unsplit).
-ExpertPlan plan_tiles(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K) {
-  const uint64_t t64 = tiles[0], t128 = tiles[1], t256 = tiles[2];
-  ExpertPlan P{};
-  P.staged = staged;
-  P.tile = 64;
-  P.slices = 1;
-  if (!staged) {
-    if (t256 >= 256) P.tile = 256;
-    else if (t128 >= (wgrad ? 384u : 256u)) P.tile = 128;
-  } else if (t128 >= (f32 ? 512u : 192u) || (t128 >= 64 && K >= 8192)) {
-    P.tile = 128;
-    if (K >= 4096) P.slices = slices_for(t128, K, 544, 512);
-  }
-  if (P.tile == 64) P.slices = f32 ? slices_for(t64, K, 768, 256) : slices_for(t64, K, 544, 512);
-  return P;
+int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K) {
+  const uint64_t t128 = tiles[1], t256 = tiles[2];
+  if (!staged) return t256 >= 256 ? 256 : t128 >= (wgrad ? 384u : 256u) ? 128 : 64;
+  return t128 >= (f32 ? 512u : 192u) || (t128 >= 64 && K >= 8192) ? 128 : 64;
 }
+
+// Workgroups that a call with few tiles is split into, and the fewest values of
+// the summed index of each.
+uint64_t wanted(bool f32) { return f32 ? 768 : 544; }
+uint64_t fewest(bool f32) { return f32 ? 256 : 512; }
 
 // Groups of up to 24 rows on average are bound by the reading of their matrices
 // and take the staged tiles of 16 or 32 rows, whatever the type and alignment (63
@@ -116,24 +135,45 @@ ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
                                A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
   const uint64_t groups = uint64_t(std::min(A.experts, A.rows)), mean = uint64_t(A.rows) / groups;
   auto tiles = [&](uint64_t TM, uint64_t TN) { return (uint64_t(A.rows) / TM + groups) * up(A.n, TN); };
-  ExpertPlan P;
+  ExpertPlan P{};
   if (mean <= (staged ? 64u : 24u)) {
     P.staged = true;
     P.tile = mean <= 8 ? 16 : 32;
     P.slices = slices_for(tiles(P.tile, 64), A.k, 1024, f32 ? 256 : 512);
   } else {
-    P = plan_tiles(staged, f32, false, {tiles(64, 64), tiles(128, 128), tiles(256, 256)}, A.k);
+    const uint64_t t[3] = {tiles(64, 64), tiles(128, 128), tiles(256, 256)};
+    P.staged = staged;
+    P.tile = choose_tile(staged, f32, false, t, A.k);
+    P.slices = 1;
+    if (P.tile == 64) P.slices = slices_for(t[0], A.k, wanted(f32), fewest(f32));
+    else if (P.tile == 128 && staged && A.k >= 4096) P.slices = slices_for(t[1], A.k, 544, 512);
   }
   P.bytes = P.slices > 1 ? uint64_t(P.slices) * uint64_t(A.rows) * uint64_t(A.n) * 4u : 0u;
   return P;
 }
 
+// A weight gradient's summed index is a group's rows, and their number is not
+// known here: where there are few tiles, groups are cut into chunks of so many
+// rows that the call has about the wanted number of workgroups whoever owns the
+// rows, and chunks are summed afterwards (24162 rows, unevenly over 11 experts of
+// 73 x 2069, fp32: 128 us; 255 with every group cut into the same number of
+// parts).  Short groups gain less than the sum costs: 10342 rows over 43 experts of
+// 1133 x 103, bf16, are 19 us whole and 31 in chunks.
 ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
-  const bool staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 &&
-                               whole(A.out, A.ldo, A.n));
-  auto tiles = [&](uint64_t T) { return uint64_t(A.experts) * up(A.k, T) * up(A.n, T); };
-  ExpertPlan P = plan_tiles(staged, f32, true, {tiles(64), tiles(128), tiles(256)}, uint64_t(A.rows) / uint64_t(A.experts));
-  P.bytes = P.slices > 1 ? uint64_t(P.slices) * uint64_t(A.experts) * uint64_t(A.k) * uint64_t(A.n) * 4u : 0u;
+  ExpertPlan P{};
+  P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
+  auto tiles = [&](uint64_t T) { return up(A.k, T) * up(A.n, T); };
+  const uint64_t experts = uint64_t(A.experts), rows = uint64_t(A.rows);
+  const uint64_t t[3] = {experts * tiles(64), experts * tiles(128), experts * tiles(256)};
+  P.tile = choose_tile(P.staged, f32, true, t, rows / experts);
+  P.slices = 1;
+  const uint64_t want = P.tile == 64 ? wanted(f32) : 544;
+  if ((P.tile == 64 || (P.tile == 128 && P.staged)) && experts * tiles(P.tile) <= want + want / 2) {
+    const uint64_t chunk = std::max(fewest(f32), up(rows * tiles(P.tile), want * 64) * 64);
+    if (rows >= 2 * chunk && rows / experts >= 2 * fewest(f32)) P.chunk = int(chunk);
+  }
+  if (P.chunk > 0)
+    P.bytes = (rows / uint64_t(P.chunk) + std::min(experts + 1, rows)) * uint64_t(A.k) * uint64_t(A.n) * 4u;
   return P;
 }
 
@@ -148,22 +188,24 @@ hipError_t launch_expert_matmul(const ExpertArgs& call, const ExpertPlan& P, boo
   }
   const hipError_t e = P.staged ? launch_rows_staged(A, P, f32, transposed, st) : launch_rows_tiles(A, P, transposed, st);
   if (e != hipSuccess || P.slices == 1) return e;
-  return sum_slices(ws, P.slices, f32, call.out, call.ldo, A.rows, 0, A.rows, A.n, st);
+  return sum_slices(ws, P.slices, f32, call.out, call.ldo, A.rows, A.n, st);
 }
 
 hipError_t launch_expert_wgrad(const ExpertArgs& call, const ExpertPlan& P, bool f32, bool out_f32, char* ws,
                                hipStream_t st) {
   ExpertArgs A = call;
-  A.slices = P.slices;
-  if (P.slices > 1) {
+  A.chunk = P.chunk;
+  if (P.chunk > 0) {
     A.out = ws;
     A.ldo = A.n;
     A.stride_b = int64_t(A.k) * A.n;
-    A.slice_out = A.experts * A.stride_b;
   }
   const hipError_t e = P.staged ? launch_wgrad_staged(A, P, f32, out_f32, st) : launch_wgrad_tiles(A, P, out_f32, st);
-  if (e != hipSuccess || P.slices == 1) return e;
-  return sum_slices(ws, P.slices, out_f32, call.out, call.ldo, A.k, call.stride_b, int64_t(A.experts) * A.k, A.n, st);
+  if (e != hipSuccess || P.chunk == 0) return e;
+  A.out = call.out;
+  A.ldo = call.ldo;
+  A.stride_b = call.stride_b;
+  return sum_chunks(ws, A, out_f32, st);
 }
 
 }  // namespace tmk

@@ -499,7 +499,7 @@ __global__ __launch_bounds__(256, S::kWaves) void k_rows_staged(const ExpertArgs
   const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
   const Place at = place_of(sl.id, row_tiles, nJ);
   Group g;
-  if (!find_tile<S::TM>(A, at.I, g)) return;
+  if (!find_tile(A, S::TM, at.I, g)) return;
   const int c0 = at.J * S::TN, rows = g.last - g.first, cols = min(S::TN, A.n - c0);
   int k0 = 0, K = 0;
   if (g.e < A.experts) sl.range(A.k, kStageBytes / T::kBytes, k0, K);
@@ -516,20 +516,15 @@ template <class T, class TO, class S>
 __global__ __launch_bounds__(256, S::kWaves) void k_wgrad_staged(const ExpertArgs A) {
   __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
   const int nI = (A.k + S::TM - 1) / S::TM, nJ = (A.n + S::TN - 1) / S::TN;
-  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
-  const int e = sl.id / (nI * nJ);
-  const Place at = place_of(sl.id - e * nI * nJ, nI, nJ);
-  const Group g = group_of(A, e);
-  int k0, K;
-  sl.range(g.last - g.first, kStageBytes / T::kBytes, k0, K);
-  const int first = g.first + k0;
+  GradTile t;
+  if (!grad_tile(A, int(blockIdx.x), int(gridDim.x), nI * nJ, t)) return;
+  const Place at = place_of(t.tile, nI, nJ);
   const int r0 = at.I * S::TM, c0 = at.J * S::TN, rows = min(S::TM, A.k - r0), cols = min(S::TN, A.n - c0);
-  const Source a{A.a + (first * A.lda + r0) * T::kBytes, A.lda, rows, A.rows - first};
-  const Source b{A.b + (first * A.ldb + c0) * T::kBytes, A.ldb, cols, A.rows - first};
+  const Source a{A.a + (t.first * A.lda + r0) * T::kBytes, A.lda, rows, A.rows - t.first};
+  const Source b{A.b + (t.first * A.ldb + c0) * T::kBytes, A.ldb, cols, A.rows - t.first};
   f32x4_t acc[S::FM][S::FN];
-  product_tile<T, S, false, false>(acc, smem, a, b, K);
-  store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + e * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo,
-                rows, cols);
+  product_tile<T, S, false, false>(acc, smem, a, b, t.K);
+  store_tile<S>(TO{}, acc, smem, A.out + (t.out * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
 }
 
 template <class T, class TO, class S>
@@ -545,7 +540,7 @@ hipError_t rows_staged(const ExpertArgs& A, bool transposed, hipStream_t st) {
 
 template <class T, class TO, class S>
 hipError_t wgrad_staged(const ExpertArgs& A, hipStream_t st) {
-  const uint64_t blocks = uint64_t(A.experts) * ((uint64_t(A.k) + S::TM - 1) / S::TM) * col_tiles(A, S::TN) * uint64_t(A.slices);
+  const uint64_t blocks = wgrad_blocks(A, S::TM, S::TN);
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_wgrad_staged<T, TO, S>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
   return hipGetLastError();
@@ -584,7 +579,7 @@ hipError_t launch_rows_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32
 
 hipError_t launch_wgrad_staged(const ExpertArgs& A, const ExpertPlan& P, bool f32, bool out_f32, hipStream_t st) {
   if (f32) return expert::wgrad_tile<F32, F32>(A, P.tile, st);
-  return out_f32 || P.slices > 1 ? expert::wgrad_tile<Bf16, F32>(A, P.tile, st)
+  return out_f32 || P.chunk > 0 ? expert::wgrad_tile<Bf16, F32>(A, P.tile, st)
                                  : expert::wgrad_tile<Bf16, Bf16>(A, P.tile, st);
 }
 

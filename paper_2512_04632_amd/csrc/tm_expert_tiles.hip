@@ -262,7 +262,7 @@ __global__ __launch_bounds__(Tile<T>::NT) void k_expert_rows(const ExpertArgs A,
   const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
   const Place at = place_of(sl.id, row_tiles, nJ);
   Group g;
-  if (!find_tile<T>(A, at.I, g)) return;
+  if (!find_tile(A, T, at.I, g)) return;
   const int e = __builtin_amdgcn_readfirstlane(g.e), first = __builtin_amdgcn_readfirstlane(g.first);
   const int rows = __builtin_amdgcn_readfirstlane(g.last) - first;
   const int c0 = at.J * T, cols = min(T, A.n - c0);
@@ -284,19 +284,15 @@ template <int T, int BK, bool OUT32>
 __global__ __launch_bounds__(Tile<T>::NT) void k_expert_wgrad(const ExpertArgs A) {
   __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<T, BK>()];
   const int nI = (A.k + T - 1) / T, nJ = (A.n + T - 1) / T;
-  const Slice sl = slice_of(A, int(blockIdx.x), int(gridDim.x));
-  const int e = sl.id / (nI * nJ);
-  const Place at = place_of(sl.id - e * nI * nJ, nI, nJ);
-  const Group g = group_of(A, e);
-  int k0, K;
-  sl.range(__builtin_amdgcn_readfirstlane(g.last - g.first), 64, k0, K);
-  const int first = __builtin_amdgcn_readfirstlane(g.first) + k0;
+  GradTile t;
+  if (!grad_tile(A, int(blockIdx.x), int(gridDim.x), nI * nJ, t)) return;
+  const Place at = place_of(t.tile, nI, nJ);
   const int r0 = at.I * T, c0 = at.J * T, rows = min(T, A.k - r0), cols = min(T, A.n - c0);
-  const uint16_t* x = reinterpret_cast<const uint16_t*>(A.a) + first * A.lda + r0;
-  const uint16_t* dy = reinterpret_cast<const uint16_t*>(A.b) + first * A.ldb + c0;
+  const uint16_t* x = reinterpret_cast<const uint16_t*>(A.a) + t.first * A.lda + r0;
+  const uint16_t* dy = reinterpret_cast<const uint16_t*>(A.b) + t.first * A.ldb + c0;
   AccT<T> acc;
-  product<T, BK, true, true>(acc, smem, Operand{x, A.lda, rows}, Operand{dy, A.ldb, cols}, K);
-  const int64_t out = sl.z * A.slice_out + e * A.stride_b + r0 * A.ldo + c0;
+  product<T, BK, true, true>(acc, smem, Operand{x, A.lda, rows}, Operand{dy, A.ldb, cols}, t.K);
+  const int64_t out = t.out * A.stride_b + r0 * A.ldo + c0;
   if constexpr (OUT32)
     store_f32<T, true>(acc, reinterpret_cast<float*>(A.out) + out, A.ldo, rows, cols);
   else
@@ -316,7 +312,7 @@ hipError_t rows_t(const ExpertArgs& A, bool transposed, hipStream_t st) {
 
 template <int T, int BK, bool OUT32>
 hipError_t wgrad_t(const ExpertArgs& A, hipStream_t st) {
-  const uint64_t blocks = wgrad_tiles(A, T) * uint64_t(A.slices);
+  const uint64_t blocks = wgrad_blocks(A, T, T);
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_expert_wgrad<T, BK, OUT32>), dim3(uint32_t(blocks)), dim3(Tile<T>::NT), 0, st, A);
   return hipGetLastError();
@@ -333,7 +329,7 @@ hipError_t launch_rows_tiles(const ExpertArgs& A, const ExpertPlan& P, bool tran
 hipError_t launch_wgrad_tiles(const ExpertArgs& A, const ExpertPlan& P, bool out_f32, hipStream_t st) {
   if (P.tile == 256) return out_f32 ? expert::wgrad_t<256, 64, true>(A, st) : expert::wgrad_t<256, 64, false>(A, st);
   if (P.tile == 128) return out_f32 ? expert::wgrad_t<128, 32, true>(A, st) : expert::wgrad_t<128, 32, false>(A, st);
-  return out_f32 || P.slices > 1 ? expert::wgrad_t<64, 64, true>(A, st) : expert::wgrad_t<64, 64, false>(A, st);
+  return out_f32 || P.chunk > 0 ? expert::wgrad_t<64, 64, true>(A, st) : expert::wgrad_t<64, 64, false>(A, st);
 }
 
 }  // namespace tmk

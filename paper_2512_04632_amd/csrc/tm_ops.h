@@ -47,15 +47,16 @@ struct ExpertArgs {
   int64_t lda, ldb, ldo;
   int64_t stride_b;     // elements from one expert's matrix to the next (b, or out of a weight gradient)
   int32_t rows, experts, k, n;
-  int32_t slices;       // of the summed index, each with a result of its own:
+  int32_t slices;       // matmul: of the summed index, each with a result of its own:
   int64_t slice_out;    // elements from one slice's result to the next
+  int32_t chunk;        // weight gradient: rows of an expert that are summed into one matrix (0: all of them)
 };
 
 // How a call is run: by which tiles, and over how many slices of the summed index.
 struct ExpertPlan {
   bool staged;          // through registers: fp32, operands that are not 16-byte aligned, groups of a few rows
-  int tile, slices;
-  uint64_t bytes;       // workspace: the slices' results
+  int tile, slices, chunk;
+  uint64_t bytes;       // workspace: the slices' or chunks' results
 };
 
 ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed);
