@@ -1,7 +1,9 @@
 """ctypes binding of the operators around the optimizer: argument marshalling only.
 
 Called as attributes of ``_lib``.  Each function checks its tensors' metadata,
-allocates its results, and passes raw device pointers and the current stream;
+allocates its results, and passes raw device pointers and the current stream
+(``stream=`` makes another one current for the call; as everywhere, a tensor made
+on one stream is used on another only after an event or a wait);
 all arithmetic runs in the library's kernels.  A small call is bound by its
 host time, so the common case (contiguous tensors on the current device) takes
 few steps.
@@ -59,16 +61,25 @@ def _ptr(t):
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _call(fn: str, index: int, stream, *args) -> None:
-    """An operator's entry point on device `index`, the stream its last argument."""
+def _call(fn: str, index: int, *args) -> None:
+    """An operator's entry point on device `index`, its current stream the last argument."""
     f = getattr(_lib._lib or _lib.lib(), fn)
     if index == _current_device():
-        st = f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
+        st = f(*args, _current_stream(index))
     else:
         with torch.cuda.device(index):
-            st = f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
+            st = f(*args, _current_stream(index))
     if st != _lib.TM_OK:
         raise _lib.TurboMuonError(fn, st, _lib.last_error())
+
+
+def _on(stream, like, op, *args):
+    """op(*args) with `stream`, one of like's device, current: the copies and the results of the
+    call belong to that stream as the kernels do."""
+    if stream.device != like.device:
+        raise ValueError(f"the stream is one of {stream.device}, the tensors are on {like.device}")
+    with torch.cuda.stream(stream):
+        return op(*args)
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
@@ -77,6 +88,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     weight and bias are fp32 vectors or None.  Returns (y, mean, rstd): y of x's shape and
     type, mean and rstd fp32, one per row.
     """
+    if stream is not None:
+        return _on(stream, x, layer_norm, x, weight, bias, eps)
     code = _code(x, "x")
     x2, rows, d, ld = _rows(x)
     if weight is not None:
@@ -86,7 +99,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     y = _empty_like(x)
     mean = x.new_empty(rows, dtype=_F32)
     rstd = torch.empty_like(mean)
-    _call("tm_layer_norm", x.get_device(), stream, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
+    _call("tm_layer_norm", x.get_device(), x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
           mean.data_ptr(), rstd.data_ptr(), rows, d, eps, code)
     return y, mean, rstd
 
@@ -94,6 +107,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
 def layer_norm_backward(dy, x, mean, rstd, weight=None, param_grads: bool = True, stream=None):
     """Gradients of layer_norm: (dx, dweight, dbias), the last two fp32, or None without
     param_grads.  mean and rstd are layer_norm's; dy has x's shape and type."""
+    if stream is not None:
+        return _on(stream, x, layer_norm_backward, dy, x, mean, rstd, weight, param_grads)
     code = _code(x, "x")
     if dy.shape != x.shape or dy.dtype is not x.dtype or dy.device != x.device:
         raise ValueError("dy must have x's shape, type and device")
@@ -107,7 +122,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, param_grads: bool = True
     if param_grads:
         dweight = x.new_empty(d, dtype=_F32)
         dbias = torch.empty_like(dweight)
-    _call("tm_layer_norm_backward", x.get_device(), stream, dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
+    _call("tm_layer_norm_backward", x.get_device(), dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
           mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), d, _ptr(dweight), _ptr(dbias), rows, d, code)
     return dx, dweight, dbias
 
@@ -138,6 +153,8 @@ def expert_matmul(x, w, ends, transposed: bool = False, stream=None):
     with transposed; ends is an int32 device vector, ends[e] the number of rows up to expert e's
     last.  Rows after ends[-1] come out as zeros.  Nothing is synchronised.
     """
+    if stream is not None:
+        return _on(stream, x, expert_matmul, x, w, ends, transposed)
     code = _code(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be (rows, k)")
@@ -152,7 +169,7 @@ def expert_matmul(x, w, ends, transposed: bool = False, stream=None):
     if ends.shape[0] != experts:
         raise ValueError("ends must hold one entry per expert")
     y = x.new_empty((rows, n))
-    _call("tm_expert_matmul", x.get_device(), stream, x2.data_ptr(), ldx, w.data_ptr(), ldw, stride_w, ends.data_ptr(),
+    _call("tm_expert_matmul", x.get_device(), x2.data_ptr(), ldx, w.data_ptr(), ldw, stride_w, ends.data_ptr(),
           y.data_ptr(), n, rows, experts, k, n, 1 if transposed else 0, code)
     return y
 
@@ -160,6 +177,8 @@ def expert_matmul(x, w, ends, transposed: bool = False, stream=None):
 def expert_wgrad(x, dy, ends, dtype=None, stream=None):
     """dw[e] = x_e.T @ dy_e for the rows of each expert: (experts, k, n), fp32 unless dtype says
     bf16 (for bf16 rows).  Experts without rows get zeros."""
+    if stream is not None:
+        return _on(stream, x, expert_wgrad, x, dy, ends, dtype)
     code = _code(x, "x")
     if x.dim() != 2 or dy.dim() != 2 or dy.shape[0] != x.shape[0]:
         raise ValueError("x and dy must be (rows, k) and (rows, n)")
@@ -170,13 +189,16 @@ def expert_wgrad(x, dy, ends, dtype=None, stream=None):
     ends = _ends(ends, x)
     experts = ends.shape[0]
     dw = x.new_empty((experts, k, n), dtype=dtype or _F32)
-    _call("tm_expert_wgrad", x.get_device(), stream, x2.data_ptr(), ldx, dy2.data_ptr(), lddy, ends.data_ptr(),
+    _call("tm_expert_wgrad", x.get_device(), x2.data_ptr(), ldx, dy2.data_ptr(), lddy, ends.data_ptr(),
           dw.data_ptr(), n, k * n if experts > 1 else 0, rows, experts, k, n, code, _code(dw, "dtype"))
     return dw
 
 
 def _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl, temperature,
                  stream, grad: bool, keep: bool):
+    if stream is not None:
+        return _on(stream, logits, _policy_loss, logits, targets, old_logp, advantages, weights, ref_logp, clip_low,
+                   clip_high, kl, temperature, None, grad, keep)
     code = _code(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be (rows, vocabulary)")
@@ -194,7 +216,7 @@ def _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_
         dlogits = _empty_like(logits)
     if keep:
         lse, slope = torch.empty_like(weights), torch.empty_like(weights)
-    _call("tm_policy_loss", logits.get_device(), stream, l2.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
+    _call("tm_policy_loss", logits.get_device(), l2.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), weights.data_ptr(), _ptr(ref_logp), clip_low, clip_high, kl, temperature,
           loss.data_ptr(), logp.data_ptr(), _ptr(lse), _ptr(slope), _ptr(dlogits), vocab, rows, vocab, code)
     return loss, logp, lse, slope, dlogits
@@ -227,6 +249,8 @@ def policy_loss_with_grad(logits, targets, old_logp, advantages, weights, ref_lo
 def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: float = 1.0, stream=None):
     """Gradient by the logits from policy_loss's lse and slope, times grad (an fp32 scalar on the
     device; None: 1)."""
+    if stream is not None:
+        return _on(stream, logits, policy_loss_backward, logits, targets, lse, slope, grad, temperature)
     code = _code(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be (rows, vocabulary)")
@@ -237,6 +261,6 @@ def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: fl
     if grad is not None and (grad.dim() != 0 or grad.dtype is not _F32 or grad.device != logits.device):
         raise ValueError("grad must be an fp32 scalar on the logits' device")
     dlogits = _empty_like(logits)
-    _call("tm_policy_loss_backward", logits.get_device(), stream, l2.data_ptr(), ld, targets.data_ptr(),
+    _call("tm_policy_loss_backward", logits.get_device(), l2.data_ptr(), ld, targets.data_ptr(),
           lse.data_ptr(), slope.data_ptr(), _ptr(grad), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
     return dlogits

@@ -76,16 +76,16 @@ inline uint64_t wgrad_blocks(const ExpertArgs& A, int TM, int TN) {
 }
 
 // Tiles (of T rows) of the groups before e; every lane of a wave calls it.
-__device__ inline int tiles_before(const ExpertArgs& A, int T, int e) {
+__device__ inline int64_t tiles_before(const ExpertArgs& A, int T, int e) {
   const int lane = threadIdx.x & 63;
-  int sum = 0;
+  int64_t sum = 0;
   for (int base = 0; base < e; base += 64)
     if (base + lane < e) {
       const Group g = group_of(A, base + lane);
       sum += (g.last - g.first + T - 1) / T;
     }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor((long long)sum, o);
   return sum;
 }
 
@@ -182,7 +182,7 @@ __device__ inline void stage_bf16(const AccT<T>& acc, char* smem, FCol col) {
 // A weight gradient's tile: rows [first, first + K) of expert e, summed into matrix
 // `out` of the result (or, with chunks, of the workspace).
 struct GradTile {
-  int e, out, tile, first, K;
+  int out, tile, first, K;
 };
 // Block `block` of a launch over `tiles` tiles a matrix; false for one that has nothing to do.
 __device__ inline bool grad_tile(const ExpertArgs& A, int block, int blocks, int tiles, GradTile& t) {
@@ -195,7 +195,6 @@ __device__ inline bool grad_tile(const ExpertArgs& A, int block, int blocks, int
   } else if (!find_tile(A, A.chunk, t.out, g) || g.e == A.experts) {
     return false;
   }
-  t.e = __builtin_amdgcn_readfirstlane(g.e);
   t.first = __builtin_amdgcn_readfirstlane(g.first);
   t.K = __builtin_amdgcn_readfirstlane(g.last) - t.first;
   return true;

@@ -42,12 +42,14 @@ __global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slice
 }
 
 // out[e] = sum of the matrices of the chunks of e's rows, in their order; zeros for
-// an expert without rows.  `per` blocks a matrix.
+// an expert without rows.  `per` blocks a matrix; `most` matrices are there, which
+// only ends that decrease could pass.
 template <class TO>
-__global__ __launch_bounds__(256) void k_sum_chunks(const float* part, const ExpertArgs A, int per) {
+__global__ __launch_bounds__(256) void k_sum_chunks(const float* part, int64_t most, const ExpertArgs A, int per) {
   const int e = int(blockIdx.x / uint32_t(per)), vecs = (A.n + 3) / 4;
   const Group g = group_of(A, e);
-  const int before = tiles_before(A, A.chunk, e), chunks = (g.last - g.first + A.chunk - 1) / A.chunk;
+  const int64_t before = min(tiles_before(A, A.chunk, e), most);
+  const int chunks = int(min(int64_t((g.last - g.first + A.chunk - 1) / A.chunk), most - before));
   const int64_t at = int64_t(blockIdx.x % uint32_t(per)) * 256 + threadIdx.x, r = at / vecs;
   if (r >= A.k) return;
   const int64_t size = int64_t(A.k) * A.n;
@@ -69,9 +71,10 @@ hipError_t sum_chunks(const char* ws, const ExpertArgs& A, bool out_f32, hipStre
   const float* part = reinterpret_cast<const float*>(ws);
   const uint64_t per = (uint64_t(A.k) * ((uint64_t(A.n) + 3) / 4) + 255) / 256, blocks = per * uint64_t(A.experts);
   if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  const int64_t most = int64_t(row_tiles(A, A.chunk));
   const dim3 grid{uint32_t(blocks)};
-  if (out_f32) hipLaunchKernelGGL((k_sum_chunks<elem::F32>), grid, dim3(256), 0, st, part, A, int(per));
-  else hipLaunchKernelGGL((k_sum_chunks<elem::Bf16>), grid, dim3(256), 0, st, part, A, int(per));
+  if (out_f32) hipLaunchKernelGGL((k_sum_chunks<elem::F32>), grid, dim3(256), 0, st, part, most, A, int(per));
+  else hipLaunchKernelGGL((k_sum_chunks<elem::Bf16>), grid, dim3(256), 0, st, part, most, A, int(per));
   return hipGetLastError();
 }
 
@@ -123,11 +126,17 @@ int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], u
 uint64_t wanted(bool f32) { return f32 ? 768 : 544; }
 uint64_t fewest(bool f32) { return f32 ? 256 : 512; }
 
+// The staged 128 tile: slices from 8192 values on (2048 rows of 8201 x 2048, bf16: 104,
+// 112 in one; fp32 450, 538; of 4098 x 2048, bf16, 60 against 54).
+//
 // Groups of up to 24 rows on average are bound by the reading of their matrices
 // and take the staged tiles of 16 or 32 rows, whatever the type and alignment (63
 // rows over 53 experts of 192 x 6976, bf16: 26 on 16 rows, 57 on the 64 tile of
 // direct loads; 80 rows over 5 of 7960 x 1970, fp32: 95 on 32 rows, 184 on 64: the
-// larger groups of an uneven call should not need two tiles).  fp32 and odd
+// larger groups of an uneven call should not need two tiles); 16 rows up to 8 on average
+// (48 rows over 8 of 2048 x 4096: 35, 37 on 32 rows; 192 over 16: 68 against 64), in slices
+// of 512 values and more (24 rows over 8 of 768 x 2048, bf16 and fp32: 6.5 and 12.3, 9.2 and
+// 16.2 from 256 on).  fp32 and odd
 // operands stay with 32 rows up to 64 (105 rows over 2 of 4869 x 5632, odd: 47, 51 on
 // the 64 tile).
 ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
@@ -139,14 +148,14 @@ ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
   if (mean <= (staged ? 64u : 24u)) {
     P.staged = true;
     P.tile = mean <= 8 ? 16 : 32;
-    P.slices = slices_for(tiles(P.tile, 64), A.k, 1024, f32 ? 256 : 512);
+    P.slices = slices_for(tiles(P.tile, 64), A.k, 1024, 512);
   } else {
     const uint64_t t[3] = {tiles(64, 64), tiles(128, 128), tiles(256, 256)};
     P.staged = staged;
     P.tile = choose_tile(staged, f32, false, t, A.k);
     P.slices = 1;
     if (P.tile == 64) P.slices = slices_for(t[0], A.k, wanted(f32), fewest(f32));
-    else if (P.tile == 128 && staged && A.k >= 4096) P.slices = slices_for(t[1], A.k, 544, 512);
+    else if (P.tile == 128 && staged && A.k >= 8192) P.slices = slices_for(t[1], A.k, 544, 512);
   }
   P.bytes = P.slices > 1 ? uint64_t(P.slices) * uint64_t(A.rows) * uint64_t(A.n) * 4u : 0u;
   return P;
@@ -166,14 +175,13 @@ ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
   const uint64_t experts = uint64_t(A.experts), rows = uint64_t(A.rows);
   const uint64_t t[3] = {experts * tiles(64), experts * tiles(128), experts * tiles(256)};
   P.tile = choose_tile(P.staged, f32, true, t, rows / experts);
-  P.slices = 1;
   const uint64_t want = P.tile == 64 ? wanted(f32) : 544;
   if ((P.tile == 64 || (P.tile == 128 && P.staged)) && experts * tiles(P.tile) <= want + want / 2) {
     const uint64_t chunk = std::max(fewest(f32), up(rows * tiles(P.tile), want * 64) * 64);
     if (rows >= 2 * chunk && rows / experts >= 2 * fewest(f32)) P.chunk = int(chunk);
   }
   if (P.chunk > 0)
-    P.bytes = (rows / uint64_t(P.chunk) + std::min(experts + 1, rows)) * uint64_t(A.k) * uint64_t(A.n) * 4u;
+    P.bytes = row_tiles(A, P.chunk) * uint64_t(A.k) * uint64_t(A.n) * 4u;
   return P;
 }
 

@@ -329,7 +329,7 @@ __global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
   }
 }
 
-// Few rows: a workgroup per chunk of a row.
+// Few rows (loss_chunks): a workgroup per chunk of a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_loss_part(const LossArgs A) {
   __shared__ Soft slots[4];
@@ -345,14 +345,14 @@ __global__ __launch_bounds__(256) void k_loss_part(const LossArgs A) {
   if (threadIdx.x == 0) A.part[blockIdx.x] = make_float2(s.m, s.s);
 }
 
-// One wave per row joins its chunks.  SUM: a single workgroup takes every row
-// and adds the loss up as well.
-template <class T, bool SUM>
+// One wave per row joins its chunks, and the one workgroup adds the loss up as well.
+template <class T>
 __global__ __launch_bounds__(1024) void k_loss_join(const LossArgs A) {
+  __shared__ double sums[16];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float c = A.inv_temp * kLog2e;
   double total = 0.0;
-  for (int64_t r = int64_t(blockIdx.x) * 16 + wave; r < A.rows; r += int64_t(gridDim.x) * 16) {
+  for (int64_t r = wave; r < A.rows; r += 16) {
     Row o{0.f, 0.f, 0.f, 0.f};
     if (active(A, r)) {
       Soft s = nothing();
@@ -366,14 +366,11 @@ __global__ __launch_bounds__(1024) void k_loss_join(const LossArgs A) {
     if (lane == 0) write_row(A, r, o);
     total += double(o.loss);
   }
-  if constexpr (SUM) {
-    __shared__ double sums[16];
-    if (lane == 0) sums[wave] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < 16; ++w) total += sums[w];
-      *A.loss = float(total);
-    }
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 16; ++w) total += sums[w];
+    *A.loss = float(total);
   }
 }
 
@@ -421,8 +418,6 @@ __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
   }
 }
 
-constexpr int kJoinRows = 64;   // up to here one workgroup joins and sums every row
-
 template <class T, int NT, int K>
 void launch_held(const LossArgs& A, hipStream_t st) {
   constexpr int RB = NT < 256 ? 256 / NT : 1;
@@ -467,29 +462,29 @@ void launch_rows(const LossArgs& A, hipStream_t st) {
 
 template <class T>
 hipError_t forward_t(const LossArgs& A, hipStream_t st) {
-  if (A.rows == 0) {
-    // the sum of no rows
-  } else if (A.chunks == 1) {
-    launch_rows<T>(A, st);
-  } else {
-    hipLaunchKernelGGL((k_loss_part<T>), dim3(uint32_t(A.rows) * A.chunks), dim3(256), 0, st, A);
-    if (A.rows <= kJoinRows)
-      hipLaunchKernelGGL((k_loss_join<T, true>), dim3(1), dim3(1024), 0, st, A);
-    else
-      hipLaunchKernelGGL((k_loss_join<T, false>), dim3((A.rows + 15) / 16), dim3(1024), 0, st, A);
-    if (A.dlogits != nullptr)
-      hipLaunchKernelGGL((k_loss_gradient<T>), dim3(uint32_t(A.rows) * A.chunks), dim3(256), 0, st, A);
+  if (A.chunks > 1) {
+    const dim3 grid(uint32_t(A.rows) * A.chunks);
+    hipLaunchKernelGGL((k_loss_part<T>), grid, dim3(256), 0, st, A);
+    hipLaunchKernelGGL((k_loss_join<T>), dim3(1), dim3(1024), 0, st, A);
+    if (A.dlogits != nullptr) hipLaunchKernelGGL((k_loss_gradient<T>), grid, dim3(256), 0, st, A);
+    return hipGetLastError();
   }
-  if (A.chunks == 1 || A.rows > kJoinRows)
-    hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(1024), 0, st, A.row_loss, A.rows, A.loss);
+  if (A.rows > 0) launch_rows<T>(A, st);
+  hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(1024), 0, st, A.row_loss, A.rows, A.loss);
   return hipGetLastError();
 }
 
 }  // namespace loss
 
+// Parts that each row is cut into where there are fewer rows than the card needs
+// workgroups (us of the value and with gradient, bf16, whole against cut: 16 x
+// 50257 9.6, 15.4 and 7.7, 10.6; 16 x 32768 7.9, 11.3 and 7.5, 9.7; 16 x 16384 6.8, 8.9 and 7.4, 9.9;
+// 32 x 131072 14.9, 26.5 and 10.4, 15.5; 32 x 50257 9.5, 15.8 and 9.9, 13.2; 48 x 131072 15.6, 27.4
+// and 15.4, 20.2: the one workgroup that joins the parts then has three rows a wave;
+// 1 x 131072 14.1, 16.8 and 6.7, 8.8 in 64 parts).
 int loss_chunks(int64_t rows, int64_t vocab) {
-  if (rows >= 512 || vocab < 8192) return 1;
-  return int(std::min<int64_t>((1024 + rows - 1) / rows, vocab / 4096));
+  if (rows > 32 || vocab < (rows > 16 ? 65536 : 32768)) return 1;
+  return int(std::min<int64_t>({512 / rows, vocab / 2048, 64}));
 }
 
 hipError_t launch_loss(const LossArgs& A, bool f32, hipStream_t st) {

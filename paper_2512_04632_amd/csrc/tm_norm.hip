@@ -359,12 +359,18 @@ __global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blo
   if (lc == 0 && col < d) out[col] = s;
 }
 
-constexpr int kMostBlocks = 2048;   // 8 workgroups of 256 threads per compute unit
+// Workgroups of the forward pass (times of the whole call in us, bf16, inputs in
+// turn): rows of 512 threads have two a compute unit (8192 x 8192: 46, 50 with
+// 2048 workgroups), of 1024 one (4096 x 16384: 49, 69 with 2048), so that each goes
+// through many rows, the next one on its way; narrower ones eight (16384 x 768: 12.5, 13.5
+// with 512, 14.3 with a row each).
+int forward_blocks(int d) { return d <= 4096 ? 2048 : d <= 8192 ? 512 : 256; }
+constexpr int kWideBlocks = 2048;   // 4096 x 20000: 313, the same with 512 and 16384
 
 template <class T, int NT, int E>
 hipError_t forward(const NormArgs& A, hipStream_t st) {
   constexpr int RB = block_threads<NT>() / NT;
-  const int blocks = int(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, kMostBlocks));
+  const int blocks = int(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, forward_blocks(A.d)));
   if (A.d % T::W == 0) hipLaunchKernelGGL((k_norm<T, NT, E, false>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
   else hipLaunchKernelGGL((k_norm<T, NT, E, true>), dim3(blocks), dim3(block_threads<NT>()), 0, st, A);
   return hipGetLastError();
@@ -378,6 +384,12 @@ hipError_t backward(const NormArgs& A, int blocks, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Threads for a row, and how many elements each holds: as few threads as hold it
+// (us, bf16, forward and backward: 8192 x 512 on 64 threads of 8: 5.6 and 11.6, of 16:
+// 7.9 and 13.6; 8192 x 1024 on 64: 8.3 and 16.1, on 256: 13.4 and 24.3; 8192 x 2048 on 256 of
+// 8: 14.4 and 29.0, of 16: 19.2 and 33.6; 4096 x 4096 on 256: 13.4 and 31.5, on 512: 23.1
+// and 39.0; 4096 x 8192 on 512: 25.6 and 46.8, on 1024: 46.5 and 62.1; 2048 x 16384 on
+// 1024: 33 and 61, not held: 130 and 161).
 template <class T>
 hipError_t forward_t(const NormArgs& A, hipStream_t st) {
   const int d = A.d;
@@ -387,7 +399,7 @@ hipError_t forward_t(const NormArgs& A, hipStream_t st) {
   if (d <= 4096) return forward<T, 256, 16>(A, st);
   if (d <= 8192) return forward<T, 512, 16>(A, st);
   if (d <= kNormMaxFused) return forward<T, 1024, 16>(A, st);
-  hipLaunchKernelGGL((k_norm_wide<T>), dim3(std::min(A.rows, kMostBlocks)), dim3(kWide), 0, st, A);
+  hipLaunchKernelGGL((k_norm_wide<T>), dim3(std::min(A.rows, kWideBlocks)), dim3(kWide), 0, st, A);
   return hipGetLastError();
 }
 
@@ -406,7 +418,7 @@ hipError_t backward_t(const NormArgs& A, int blocks, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_norm_backward_wide<T>), dim3(std::min(A.rows, kMostBlocks)), dim3(kWide), 0, st, A);
+  hipLaunchKernelGGL((k_norm_backward_wide<T>), dim3(std::min(A.rows, kWideBlocks)), dim3(kWide), 0, st, A);
   return hipGetLastError();
 }
 
@@ -416,11 +428,17 @@ hipError_t launch_norm(const NormArgs& A, bool f32, hipStream_t st) {
   return f32 ? norm::forward_t<elem::F32>(A, st) : norm::forward_t<elem::Bf16>(A, st);
 }
 
-int norm_blocks(int64_t rows, int64_t d) {
+// Workgroups of the backward pass: each leaves a line of partial sums.  Two a
+// compute unit, or one where the rows' registers leave room for no more (us, 512
+// against 256 workgroups: 32768 x 2048 bf16 84 and 101; 16384 x 3000 fp32 120 and 109;
+// 8192 x 8192 bf16 98 and 86; 1024 of them: 16384 x 768 bf16 24, 21 with 512); rows that
+// are not held, with their column sums apart: 4096 x 20000 bf16 417, 409 with 128, 442 with 32.
+int norm_blocks(int64_t rows, int64_t d, bool f32) {
   const int rb = d <= 1024 ? 4 : 1;
-  // a few rows are summed by one workgroup, without the second launch
+  // a few rows are summed by one workgroup: as fast (8 x 4096 bf16: 9.0 us both
+  // ways, 13.4 and 9.1 from eight rows a wave on), and one launch less for the host
   if (d <= kNormMaxFused && rows > 0 && rows <= 4 * rb) return 1;
-  const int most = d > kNormMaxFused ? 64 : d > 4096 ? 256 : 512;
+  const int most = d > kNormMaxFused ? 64 : d > (f32 ? 1024 : 4096) ? 256 : 512;
   return int(std::min<int64_t>((rows + rb - 1) / rb, most));
 }
 

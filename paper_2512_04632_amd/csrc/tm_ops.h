@@ -32,7 +32,7 @@ constexpr int kNormMaxFused = 16384;
 
 hipError_t launch_norm(const NormArgs& A, bool f32, hipStream_t st);
 // Blocks (and so column sums in `part`) of a backward launch.
-int norm_blocks(int64_t rows, int64_t d);
+int norm_blocks(int64_t rows, int64_t d, bool f32);
 hipError_t launch_norm_backward(const NormArgs& A, bool f32, int blocks, hipStream_t st);
 // dweight, dbias (either may be nullptr) = sums of `blocks` partial sums.
 hipError_t launch_norm_params(const float* part, int blocks, int d, float* dweight, float* dbias,

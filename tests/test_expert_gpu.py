@@ -233,6 +233,42 @@ def test_ends_that_make_no_sense_stay_in_bounds():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,k,n", [
+    ([0, 7000, 1, 0, 513, 30, 0], 65, 33), ([1024, 1024, 0, 2048], 64, 72),
+    # more experts than a wave has lanes, rows of none at the end
+    ([3000 if e % 9 == 4 else 1200 * (e % 3) for e in range(70)], 8, 9),
+])
+def test_long_groups_in_chunks(counts, k, n, dtype):
+    log(f"case: weight gradient of long uneven groups, {len(counts)} experts {k} x {n} {dtype}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    rows = sum(counts) + 700
+    x, dy = _randn(g, (rows, k), dtype), _randn(g, (rows, n), dtype)
+    x[rows - 700:] = float("nan")
+    ends = _ends(counts)
+    dw = tm.expert_wgrad(x, dy, ends)
+    _check_wgrad(x, dy, counts, "f32", dw)
+    assert torch.equal(dw, tm.expert_wgrad(x, dy, ends))
+    for e, (c, m) in enumerate(zip(counts, dw)):
+        assert c > 0 or not m.any(), e
+    if dtype == "bf16":
+        _check_wgrad(x, dy, counts, "bf16", tm.expert_wgrad(x, dy, ends, dtype=torch.bfloat16))
+
+
+def test_ends_that_make_no_sense_stay_in_bounds_of_the_chunks():
+    """Decreasing ends count rows more than once: more chunks than the call has room for are left out."""
+    log("case: weight gradient in chunks, ends that decrease")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    rows = 4096
+    x = _randn(g, (rows, 64), "bf16")
+    for ends in ([rows, 0, rows], [-5, rows, 90], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1]):
+        dw = tm.expert_wgrad(x, x, torch.tensor(ends, dtype=torch.int32, device="cuda"))
+        _check_wgrad(x, x, [max(0, min(ends[0], rows))], "f32", dw[:1])
+    torch.cuda.synchronize()
+
+
 def test_gradients_against_differences():
     g = torch.Generator(device="cuda")
     g.manual_seed(7)

@@ -72,6 +72,37 @@ def test_explicit_stream():
     assert _same(ref, got)
 
 
+def test_explicit_stream_orders_the_copies_it_needs():
+    """Inputs that are copied first (columns outermost) are copied on the call's stream, not behind the work
+    of the current one."""
+    log("case: operators on a stream given by name, inputs of other strides")
+    s = _all(4)
+    flip = {k: v.t().contiguous().t() for k, v in s.items() if k in ("x", "dy", "logits")}
+    mt = s["m"].transpose(1, 2).contiguous().transpose(1, 2)
+    mean, rstd = tm.layer_norm(s["x"])[1:]
+    lse, slope = tm.policy_loss(s["logits"], s["targets"], s["v"][0] - 9, s["v"][1], s["weights"])[2:]
+
+    def calls(x, dy, m, logits, **kw):
+        return [*tm.layer_norm(x, s["w"], s["b"], **kw), *tm.layer_norm_backward(dy, x, mean, rstd, s["w"], **kw),
+                tm.expert_matmul(x, m, s["ends"], **kw), tm.expert_wgrad(x, dy, s["ends"], **kw),
+                *tm.policy_loss(logits, s["targets"], s["v"][0] - 9, s["v"][1], s["weights"], **kw),
+                *tm.policy_loss_with_grad(logits, s["targets"], s["v"][0] - 9, s["v"][1], s["weights"], **kw),
+                tm.policy_loss_backward(logits, s["targets"], lse, slope, **kw)]
+
+    ref = calls(s["x"], s["dy"], s["m"], s["logits"])
+    busy = torch.randn(4096, 4096, device="cuda")
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy @ busy                               # milliseconds of work ahead on the current stream
+    got = calls(flip["x"], flip["dy"], mt, flip["logits"], stream=st)
+    st.synchronize()
+    with torch.cuda.stream(st):
+        same = _same(got, ref)
+    torch.cuda.synchronize()
+    assert same
+
+
 def test_graph_replays_match_eager():
     log("case: operators in a captured graph")
     s, other = _all(4), _all(5)

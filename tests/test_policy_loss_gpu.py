@@ -279,3 +279,15 @@ def test_no_rows_and_refusals():
         with pytest.raises(tm.TurboMuonError) as e:
             tm.policy_loss(**s, **bad)
         assert e.value.status == tm.TM_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(1, 32768), (4, 40001), (16, 33333), (20, 70001), (32, 131072), (33, 131072)])
+def test_few_long_rows(rows, vocab, dtype):
+    """Rows that are cut into parts: sizes, masks, strides."""
+    log(f"case: policy loss, few long rows {rows} x {vocab} {dtype}")
+    test_value_and_gradient(rows, vocab, dtype)
+    if rows >= 20:
+        test_masked_rows_are_not_read(rows, vocab, dtype)
+    test_masked_vocabulary(max(rows, 4), vocab, dtype)
+    test_strides_and_in_place(rows, vocab, dtype)
