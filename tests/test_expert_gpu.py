@@ -256,6 +256,25 @@ def test_long_groups_in_chunks(counts, k, n, dtype):
         _check_wgrad(x, dy, counts, "bf16", tm.expert_wgrad(x, dy, ends, dtype=torch.bfloat16))
 
 
+@pytest.mark.parametrize("counts,k,n", [([9, 3, 14], 7770, 461), ([100, 130], 6000, 700), ([7000], 900, 1400)])
+def test_long_fp32_sums_keep_their_digits(counts, k, n):
+    """Rounding errors of a sum of K terms in turn grow with sqrt(K): each rounding of the running sum is off by
+    0.41 U of it (rms: evenly within half a unit in the last place, which is U to 2 U of the value), together
+    0.41 U sqrt(K / 2) of the result.  Runs of less than a half of K stay below 0.29 of U sqrt(K / 2)."""
+    log(f"case: long fp32 sums, {sum(counts)} rows, {k} x {n}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    rows, ends = sum(counts), _ends(counts)
+    x, dy, w = _randn(g, (rows, k), "f32"), _randn(g, (rows, n), "f32"), _randn(g, (len(counts), k, n), "f32")
+    if len(counts) > 1:
+        got, K = tm.expert_matmul(x, w, ends), k
+        want = torch.cat([x[a:b].double() @ w[e].double() for e, a, b in _bounds(counts)])
+    else:
+        got, K = tm.expert_wgrad(x, dy, ends)[0], rows
+        want = x.double().t() @ dy.double()
+    assert float((got.double() - want).norm()) <= 0.3 * U * (K / 2) ** 0.5 * float(want.norm())
+
+
 def test_ends_that_make_no_sense_stay_in_bounds_of_the_chunks():
     """Decreasing ends count rows more than once: more chunks than the call has room for are left out."""
     log("case: weight gradient in chunks, ends that decrease")
