@@ -233,8 +233,9 @@ tm_status tm_orthogonalize_noalloc(void* X, int64_t m, int64_t n, int64_t batch,
  * graph capture and timing are as stated above; the calls marked (W) keep
  * partial sums in a workspace of their own per (device, stream), which grows
  * and is captured like the orthogonalizer's.  Every result is the same on
- * every run (no float atomics).  NaN and Inf propagate, but never out of rows
- * that take no part.
+ * every run (no float atomics); the order of a sum, and so the last bits, may
+ * differ with the sizes, strides and alignment of a call.  NaN and Inf
+ * propagate, but never out of rows that take no part.
  */
 #define TM_DTYPE_BF16 0
 #define TM_DTYPE_F32  1
@@ -268,7 +269,7 @@ tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
                                  int dtype, void* stream);
 
 /*
- * tm_expert_matmul - y[i, :] = x[i, :] W[e], e the expert of row i.
+ * tm_expert_matmul (W) - y[i, :] = x[i, :] W[e], e the expert of row i.
  *   x     rows x k;  y  rows x n, of the same type.
  *   w     matrix e starts at w + e stride_w: k x n with row stride ldw, or
  *         n x k where `transposed` (y = x W^T: with the forward pass's w and dy
@@ -279,18 +280,23 @@ tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
  *         stream: no host synchronisation.  Whatever it holds, nothing outside
  *         the matrices is read or written.
  *   k, n  1..TM_MAX_DIM;  experts 1..TM_MAX_EXPERTS.
- * y overlaps nothing that is read.
+ * y overlaps nothing that is read.  Sums are fp32.  fp32 products of many rows
+ * are formed of three bf16 parts of each operand on the matrix cores and are as
+ * exact as a sum of fp32 products (tiles with NaN, Inf or values that round past
+ * the largest bf16 take fp32 products); operands below about 2^-110 keep fewer
+ * bits there.
  */
 tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t stride_w,
                            const int32_t* ends, void* y, int64_t ldy, int64_t rows, int64_t experts,
                            int64_t k, int64_t n, int transposed, int dtype, void* stream);
 
 /*
- * tm_expert_wgrad - dw[e] = x_e^T dy_e over the rows of each expert (k x n;
+ * tm_expert_wgrad (W) - dw[e] = x_e^T dy_e over the rows of each expert (k x n;
  * zeros for an expert without rows).
  *   x, dy      rows x k and rows x n of type `dtype`.
  *   dw         matrix e starts at dw + e stride_dw, row stride lddw; of type
  *              `out_dtype`: fp32, or bf16 where the rows are.
+ * Sums as in tm_expert_matmul.
  */
 tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* ends,
                           void* dw, int64_t lddw, int64_t stride_dw, int64_t rows, int64_t experts,
@@ -315,7 +321,8 @@ tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t ld
  *   dlogits     rows x vocab of the logits' type (it may be the logits), or
  *               NULL: the value alone.
  * Rows that take no part: logp, lse, slope and their gradient are zero, their
- * logits are not read.  A row of nothing but -inf gives NaN.
+ * logits are not read.  A row of nothing but -inf gives NaN.  loss and logp have
+ * the same bits with and without dlogits.
  */
 tm_status tm_policy_loss(const void* logits, int64_t ld, const int64_t* targets, const float* old_logp,
                          const float* advantages, const float* weights, const float* ref_logp,
@@ -327,7 +334,9 @@ tm_status tm_policy_loss(const void* logits, int64_t ld, const int64_t* targets,
  * tm_policy_loss_backward - dlogits from the lse and slope of an earlier
  * tm_policy_loss on the same logits, targets and temperature, times *grad (a
  * device float, NULL for 1).  Rows of slope 0 are not read, their gradient is
- * zero.  dlogits may be the logits.
+ * zero.  dlogits may be the logits.  The probabilities are taken from lse, whose
+ * rounding (2^-24 of it) they carry: with logits of large size, such as a row of
+ * nothing but the lowest value, tm_policy_loss's dlogits are the exact ones.
  */
 tm_status tm_policy_loss_backward(const void* logits, int64_t ld, const int64_t* targets,
                                   const float* lse, const float* slope, const float* grad,

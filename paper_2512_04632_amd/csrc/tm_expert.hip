@@ -31,7 +31,8 @@ __device__ inline void sum_vec(const float* part, int64_t apart, int count, char
 }
 
 // out = sum of the slices' results, in their order, each thread a vector of the
-// rows x n result.
+// rows x n result.  Bound by the reading, from the caches that the slices were
+// written to: 2 us and more.
 template <class TO>
 __global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slices, char* out, int64_t ldo, int64_t rows, int n) {
   const int vecs = (n + 3) / 4;

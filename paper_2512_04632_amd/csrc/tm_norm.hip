@@ -15,6 +15,10 @@
 // grid and write one line of partial sums each, which k_norm_params adds up in
 // a fixed order (no atomics: results are the same on every run).  Statistics
 // and sums are fp32; y and dx are rounded once.
+//
+// Bound by HBM once there are rows enough (16384 x 4096 bf16: forward 53.7 us, 5.0
+// TB/s, what a large copy reaches; backward 83.9 us, 4.8 TB/s) and by the host's
+// 8 us a call below some hundred rows (64 x 768: 4.1 us of kernel).
 #include <algorithm>
 
 #include "tm_elem.h"
@@ -72,7 +76,10 @@ __device__ inline void load_row(const char* row, int t, int d, u32x4_t (&q)[V]) 
   for (int j = 0; j < V; ++j) q[j] = load_ahead<T, TAIL>(row, (j * NT + t) * T::W, d);
 }
 
-// TAIL: rows that end inside a 16-byte vector.
+// Forward.  NT threads a row, E elements each (forward_t); TAIL: rows that end
+// inside a 16-byte vector.  Two sums
+// over the row's threads and the load are a chain that one row leaves idle: the
+// next row is loaded while this one is summed (16384 x 4096 bf16: 47 us of kernel).
 template <class T, int NT, int E, bool TAIL>
 __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) {
   constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
@@ -130,6 +137,11 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm(const NormArgs A) 
 template <class T, int NT, int E>
 constexpr int rows_ahead() { return NT == 1024 ? 0 : NT <= 256 && E * T::kBytes <= 16 ? 3 : 1; }
 
+// Backward: x and dy are read once, dx written once; the columns' sums stay in
+// registers over a workgroup's rows, so few workgroups write few lines of partial
+// sums (norm_blocks).  16384 x 4096 bf16: 80 us of kernel for 403 MB, 5.0 TB/s; 4001 x
+// 1001 fp32 16.8 us, 2.9 TB/s: rows of odd length, four a workgroup, are bound by
+// their chains of loads and sums.
 template <class T, int NT, int E, bool TAIL>
 __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const NormArgs A) {
   constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT / 64;
@@ -228,7 +240,8 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
 
 // Rows wider than a workgroup's registers (kNormMaxFused): one workgroup of
 // 1024 threads per row, which reads the row once for each sum and once for the
-// result (the later passes find it in a cache).
+// result (the later passes find it in a cache).  Bound by the cache's rate: 4096 x
+// 20000 bf16 313 us, 1.05 TB/s of what has to move.
 constexpr int kWide = 1024;
 
 template <class T, class F>
@@ -276,6 +289,7 @@ __global__ __launch_bounds__(kWide) void k_norm_wide(const NormArgs A) {
   }
 }
 
+// The same backwards: 4096 x 20000 bf16 410 us with the column sums.
 template <class T>
 __global__ __launch_bounds__(kWide) void k_norm_backward_wide(const NormArgs A) {
   __shared__ float slots[2][2 * kWide / 64];
@@ -336,7 +350,7 @@ __global__ __launch_bounds__(256) void k_norm_columns(const NormArgs A, int slic
 }
 
 // out[c] = sum of the blocks' partial sums of column c: 32 columns a block, 32
-// threads each.
+// threads each.  Bound by latency: 512 lines of 4096 columns, 16 MB, 4.5 us.
 __global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blocks, int d, float* dweight,
                                                       float* dbias) {
   float* out = blockIdx.y == 0 ? dweight : dbias;
