@@ -116,9 +116,18 @@ using namespace expert;
 // (24211 rows, gradient of 896 x 128: 64, 67 and 75 with 512, 768 and 1536; 17221
 // rows over 19 of 1280 x 64: 51, 44 and 45), each of eight stages at least (7 rows over 2
 // of 4608 x 64, fp32: 14.5, 17.5 from sixteen on, 16.6 from four on, 72 unsplit).
-int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K) {
+//
+// Groups of few rows on average leave most of a large tile empty, and a weight
+// gradient's tile works as long as its group is: the 64 tile up to 64 rows (4096
+// rows over 64 experts of 2048 x 1408, even and uneven groups: 86 and 97, 102 and 105 on 128,
+// 120 and 122 on 256; 80 rows each: 111 and 110, 108 and 109 on 128), the 128 tile below
+// 128 rows (112 each: 118 and 115, 126 and 127 on 256; 160: 142 and 144 against 128 and 130)
+// and for weight gradients up to 256 (128 each: 154 and 164, 156 and 196 on 256; 512 each of
+// 2048 x 2048: 116 and 125 against 94 and 146).
+int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K, uint64_t mean) {
   const uint64_t t128 = tiles[1], t256 = tiles[2];
-  if (!staged) return t256 >= 256 ? 256 : t128 >= (wgrad ? 384u : 256u) ? 128 : 64;
+  if (!staged && !wgrad && mean <= 64) return 64;
+  if (!staged) return t256 >= 256 && mean >= (wgrad ? 257u : 128u) ? 256 : t128 >= (wgrad ? 384u : 256u) ? 128 : 64;
   return t128 >= (f32 ? 512u : 192u) || (t128 >= 64 && K >= 8192) ? 128 : 64;
 }
 
@@ -160,7 +169,7 @@ ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
   } else {
     const uint64_t t[3] = {tiles(64, 64), tiles(128, 128), tiles(256, 256)};
     P.staged = staged;
-    P.tile = choose_tile(staged, f32, false, t, A.k);
+    P.tile = choose_tile(staged, f32, false, t, A.k, mean);
     P.slices = 1;
     if (P.tile == 64) P.slices = slices_for(t[0], A.k, wanted(f32), fewest(f32));
     else if (P.tile == 128 && staged && A.k >= 8192) P.slices = slices_for(t[1], A.k, 544, 512);
@@ -183,7 +192,7 @@ ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
   auto tiles = [&](uint64_t T) { return up(A.k, T) * up(A.n, T); };
   const uint64_t experts = uint64_t(A.experts), rows = uint64_t(A.rows);
   const uint64_t t[3] = {experts * tiles(64), experts * tiles(128), experts * tiles(256)};
-  P.tile = choose_tile(P.staged, f32, true, t, rows / experts);
+  P.tile = choose_tile(P.staged, f32, true, t, rows / experts, rows / experts);
   const uint64_t want = P.tile == 64 ? wanted(f32) : 544;
   if ((P.tile == 64 || (P.tile == 128 && P.staged)) && experts * tiles(P.tile) <= want + want / 2) {
     const uint64_t chunk = std::max(fewest(f32), up(rows * tiles(P.tile), want * 64) * 64);
