@@ -185,8 +185,8 @@ __device__ inline void keep_order() {
 // NT threads per row (64: four rows a workgroup), which hold the whole row in
 // registers, K vectors each: it is read once, its maximum is known before the
 // first exponential is taken, and the gradient is formed from the registers.
-// 10140 x 1731 bf16 with gradient: 25 us, 2.8 TB/s, bound by the exponentials and the
-// unpacking; 4096 x 32001 fp32 with gradient 196 us, 5.4 TB/s.
+// Bound by the exponentials and the unpacking for short rows (10140 x 1731 bf16 with
+// gradient: 25 us), by HBM for long ones (4096 x 32001 fp32 with gradient: 196 us).
 template <class T, int NT, int K, bool GRAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_loss_held(const LossArgs A) {
   constexpr int RB = NT < 256 ? 256 / NT : 1, W = T::W, NW = NT / 64;
@@ -294,9 +294,9 @@ __device__ inline void each_group(const char* l, int first, int last, F f) {
 }
 
 // Longer rows: one workgroup per row, which reads it twice (the second time
-// mostly from the memory-side cache).  Bound by HBM: 8192 x 131072 bf16 with gradient
-// 782 us, 5.5 TB/s of the 4.3 GB that have to move; 4096 x 50257 bf16 with gradient
-// 223 us, 3.7 TB/s.
+// mostly from the memory-side cache).  Bound by HBM: 8192 x 131072 bf16 with gradient,
+// a quarter of the rows without part, 783 us, 4.8 TB/s of what has to move (a large copy
+// reaches 5.0); 4096 x 50257 bf16 with gradient 223 us.
 template <class T, int NT, bool GRAD>
 __global__ __launch_bounds__(NT) void k_loss_rows(const LossArgs A) {
   __shared__ Soft slots[NT / 64];
@@ -397,8 +397,7 @@ __global__ __launch_bounds__(1024) void k_loss_sum(const float* row_loss, int ro
 
 // dlogits from lse and slope, a workgroup per chunk of a row.  Rows of slope
 // 0 are not read.  l / tau - lse is rounded once (fma).  Bound by HBM: 3000 x 32001
-// fp32 124 us, 6.2 TB/s; 8192 x 131072 bf16 539 us, 8.0 TB/s with a part of the logits
-// in the memory-side cache.
+// fp32, a tenth of the rows without part, 125 us, 5.8 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
   const int64_t r = blockIdx.x / A.chunks;
