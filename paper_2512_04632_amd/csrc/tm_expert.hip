@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void k_sum_chunks(const float* part, int64_t m
 hipError_t sum_slices(const char* ws, int slices, bool out_f32, char* out, int64_t ldo, int64_t rows, int n, hipStream_t st) {
   const float* part = reinterpret_cast<const float*>(ws);
   const uint64_t blocks = (uint64_t(rows) * ((uint64_t(n) + 3) / 4) + 255) / 256;
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid{uint32_t(blocks)};
   if (out_f32) hipLaunchKernelGGL((k_sum_slices<elem::F32>), grid, dim3(256), 0, st, part, slices, out, ldo, rows, n);
   else hipLaunchKernelGGL((k_sum_slices<elem::Bf16>), grid, dim3(256), 0, st, part, slices, out, ldo, rows, n);
@@ -71,7 +71,7 @@ hipError_t sum_slices(const char* ws, int slices, bool out_f32, char* out, int64
 hipError_t sum_chunks(const char* ws, const ExpertArgs& A, bool out_f32, hipStream_t st) {
   const float* part = reinterpret_cast<const float*>(ws);
   const uint64_t per = (uint64_t(A.k) * ((uint64_t(A.n) + 3) / 4) + 255) / 256, blocks = per * uint64_t(A.experts);
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, 256)) return hipErrorInvalidConfiguration;
   const int64_t most = int64_t(row_tiles(A, A.chunk));
   const dim3 grid{uint32_t(blocks)};
   if (out_f32) hipLaunchKernelGGL((k_sum_chunks<elem::F32>), grid, dim3(256), 0, st, part, most, A, int(per));

@@ -537,7 +537,7 @@ template <class T, class TO, class S>
 hipError_t rows_staged(const ExpertArgs& A, bool transposed, hipStream_t st) {
   const uint64_t tiles = row_tiles(A, S::TM);
   const uint64_t blocks = tiles * col_tiles(A, S::TN) * uint64_t(A.slices);
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid{uint32_t(blocks)};
   if (transposed) hipLaunchKernelGGL((k_rows_staged<T, TO, S, true>), grid, dim3(256), 0, st, A, int(tiles));
   else hipLaunchKernelGGL((k_rows_staged<T, TO, S, false>), grid, dim3(256), 0, st, A, int(tiles));
@@ -547,7 +547,7 @@ hipError_t rows_staged(const ExpertArgs& A, bool transposed, hipStream_t st) {
 template <class T, class TO, class S>
 hipError_t wgrad_staged(const ExpertArgs& A, hipStream_t st) {
   const uint64_t blocks = wgrad_blocks(A, S::TM, S::TN);
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, 256)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_wgrad_staged<T, TO, S>), dim3(uint32_t(blocks)), dim3(256), 0, st, A);
   return hipGetLastError();
 }

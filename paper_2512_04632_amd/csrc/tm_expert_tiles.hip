@@ -314,7 +314,7 @@ template <int T, int BK, bool OUT32>
 hipError_t rows_t(const ExpertArgs& A, bool transposed, hipStream_t st) {
   const uint64_t tiles = row_tiles(A, T);
   const uint64_t blocks = tiles * col_tiles(A, T) * uint64_t(A.slices);
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, Tile<T>::NT)) return hipErrorInvalidConfiguration;
   const dim3 grid{uint32_t(blocks)}, block(Tile<T>::NT);
   if (transposed) hipLaunchKernelGGL((k_expert_rows<T, BK, true, OUT32>), grid, block, 0, st, A, int(tiles));
   else hipLaunchKernelGGL((k_expert_rows<T, BK, false, OUT32>), grid, block, 0, st, A, int(tiles));
@@ -324,7 +324,7 @@ hipError_t rows_t(const ExpertArgs& A, bool transposed, hipStream_t st) {
 template <int T, int BK, bool OUT32>
 hipError_t wgrad_t(const ExpertArgs& A, hipStream_t st) {
   const uint64_t blocks = wgrad_blocks(A, T, T);
-  if (blocks >= (uint64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (!launchable(blocks, Tile<T>::NT)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_expert_wgrad<T, BK, OUT32>), dim3(uint32_t(blocks)), dim3(Tile<T>::NT), 0, st, A);
   return hipGetLastError();
 }

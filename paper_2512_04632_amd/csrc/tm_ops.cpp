@@ -240,8 +240,9 @@ tm_status check_temperature(float t) {
   return TM_OK;
 }
 
-tm_status check_blocks(int64_t rows, int64_t chunks) {
-  if (rows * chunks >= (int64_t(1) << 31)) return refuse(TM_ERR_UNSUPPORTED, "too many blocks in one launch");
+tm_status check_blocks(int64_t rows, int64_t chunks, uint64_t threads) {
+  if (!tmk::launchable(uint64_t(rows) * uint64_t(chunks), threads))
+    return refuse(TM_ERR_UNSUPPORTED, "too many blocks in one launch");
   return TM_OK;
 }
 
@@ -292,7 +293,9 @@ tm_status policy_loss(const void* logits, int64_t ld, const int64_t* targets, co
   A.kl = kl;
   A.inv_temp = 1.f / temperature;
   const int64_t chunks = empty ? 1 : tmk::loss_chunks(rows, vocab);
-  TM_CHECK(check_blocks(rows, chunks));
+  // threads of a row at most (launch_rows)
+  const int64_t line_bytes = vocab * int64_t(esz);
+  TM_CHECK(check_blocks(rows, chunks, line_bytes <= 4096 ? 64 : line_bytes <= 48 * 1024 ? 256 : 1024));
   A.chunks = int32_t(chunks);
   A.chunk = int32_t(chunk_length(vocab, chunks));
   // workspace: the rows' shares of the loss, lse and slope where the caller
@@ -333,7 +336,7 @@ tm_status policy_loss_backward(const void* logits, int64_t ld, const int64_t* ta
   A.vocab = int32_t(vocab);
   A.inv_temp = 1.f / temperature;
   const int64_t chunks = (vocab * int64_t(esz) + kGradBytes - 1) / kGradBytes;
-  TM_CHECK(check_blocks(rows, chunks));
+  TM_CHECK(check_blocks(rows, chunks, 256));
   A.chunks = int32_t(chunks);
   A.chunk = int32_t(chunk_length(vocab, chunks));
   return run_op(TM_PHASE_POLICY_LOSS_BACKWARD, 0, stream,

@@ -39,6 +39,9 @@ hipError_t launch_norm_params(const float* part, int blocks, int d, float* dweig
                               hipStream_t st);
 
 // ---------------------------------------------------------------- expert products
+// Whether a launch's threads fit the 32 bits that the dispatch packet has for them.
+inline bool launchable(uint64_t blocks, uint64_t threads) { return blocks * threads < (uint64_t(1) << 32); }
+
 struct ExpertArgs {
   const char* a;        // x (rows x k), or x of a weight gradient
   const char* b;        // the experts' matrices, or dy of a weight gradient (rows x n)

@@ -96,3 +96,13 @@ def test_dtype_codes_match_the_header():
     d = {k: int(v) for k, v in re.findall(r"#define\s+(TM_DTYPE_\w+)\s+(\d+)", text)}
     assert d == {"TM_DTYPE_BF16": tm.DTYPE_BF16, "TM_DTYPE_F32": tm.DTYPE_F32}
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+@pytest.mark.parametrize("call,size", [
+    (_loss, dict(rows=1 << 26, vocab=2000, ld=2000)), (_loss, dict(rows=1 << 24, vocab=8000, ld=8000)),
+    (_loss, dict(rows=1 << 22, vocab=100000, ld=100000)), (_loss_back, dict(rows=1 << 24, vocab=64)),
+])
+def test_launches_past_32_bits_of_threads_are_refused(call, size):
+    """A dispatch counts its threads in 32 bits: more would wrap."""
+    assert call(**size) == UNSUPPORTED
+    assert "too many blocks" in tm.last_error()
