@@ -41,10 +41,10 @@ def _rows(t):
     return t, rows, d, ld if ld > d else d
 
 
-def _vector(t, like, name: str, n: int, dtype):
-    """A companion vector of n entries on like's device, contiguous."""
-    if t.dtype is not dtype or t.shape != (n,) or t.device != like.device:
-        raise ValueError(f"{name} must be a {dtype} vector of {n} entries on {like.device}, not a {t.dtype} "
+def _vector(t, index: int, name: str, n: int, dtype):
+    """A companion vector of n entries on device `index`, contiguous."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (n,):
+        raise ValueError(f"{name} must be a {dtype} vector of {n} entries on cuda:{index}, not a {t.dtype} "
                          f"tensor of shape {tuple(t.shape)} on {t.device}")
     return t if t.is_contiguous() else t.contiguous()
 
@@ -90,16 +90,16 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     """
     if stream is not None:
         return _on(stream, x, layer_norm, x, weight, bias, eps)
-    code = _code(x, "x")
+    code, index = _code(x, "x"), x.get_device()
     x2, rows, d, ld = _rows(x)
     if weight is not None:
-        weight = _vector(weight, x, "weight", d, _F32)
+        weight = _vector(weight, index, "weight", d, _F32)
     if bias is not None:
-        bias = _vector(bias, x, "bias", d, _F32)
+        bias = _vector(bias, index, "bias", d, _F32)
     y = _empty_like(x)
-    mean = x.new_empty(rows, dtype=_F32)
+    mean = x.new_empty_strided((rows,), (1,), dtype=_F32)
     rstd = torch.empty_like(mean)
-    _call("tm_layer_norm", x.get_device(), x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
+    _call("tm_layer_norm", index, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), d,
           mean.data_ptr(), rstd.data_ptr(), rows, d, eps, code)
     return y, mean, rstd
 
@@ -109,29 +109,29 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, param_grads: bool = True
     param_grads.  mean and rstd are layer_norm's; dy has x's shape and type."""
     if stream is not None:
         return _on(stream, x, layer_norm_backward, dy, x, mean, rstd, weight, param_grads)
-    code = _code(x, "x")
-    if dy.shape != x.shape or dy.dtype is not x.dtype or dy.device != x.device:
+    code, index = _code(x, "x"), x.get_device()
+    if dy.shape != x.shape or dy.dtype is not x.dtype or dy.get_device() != index:
         raise ValueError("dy must have x's shape, type and device")
     x2, rows, d, ldx = _rows(x)
     dy2, _, _, lddy = _rows(dy)
-    mean, rstd = _vector(mean, x, "mean", rows, _F32), _vector(rstd, x, "rstd", rows, _F32)
+    mean, rstd = _vector(mean, index, "mean", rows, _F32), _vector(rstd, index, "rstd", rows, _F32)
     if weight is not None:
-        weight = _vector(weight, x, "weight", d, _F32)
+        weight = _vector(weight, index, "weight", d, _F32)
     dx = _empty_like(x)
     dweight = dbias = None
     if param_grads:
-        dweight = x.new_empty(d, dtype=_F32)
+        dweight = x.new_empty_strided((d,), (1,), dtype=_F32)
         dbias = torch.empty_like(dweight)
-    _call("tm_layer_norm_backward", x.get_device(), dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
+    _call("tm_layer_norm_backward", index, dy2.data_ptr(), lddy, x2.data_ptr(), ldx, _ptr(weight),
           mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), d, _ptr(dweight), _ptr(dbias), rows, d, code)
     return dx, dweight, dbias
 
 
-def _matrices(w, x):
+def _matrices(w, x, index: int):
     """Stacked matrices as (tensor, row stride, matrix stride), their last dimension contiguous."""
     if w.dim() != 3:
         raise ValueError("w must be (experts, rows, columns)")
-    if w.device != x.device or w.dtype is not x.dtype:
+    if w.get_device() != index or w.dtype is not x.dtype:
         raise ValueError("w must have x's type and device")
     e, r, c = w.shape
     apart, ld, along = w.stride()
@@ -140,8 +140,8 @@ def _matrices(w, x):
     return w, ld if ld > c else c, apart if e > 1 else 0
 
 
-def _ends(ends, x):
-    if ends.dim() != 1 or ends.dtype is not _I32 or ends.device != x.device:
+def _ends(ends, index: int):
+    if ends.dim() != 1 or ends.dtype is not _I32 or ends.get_device() != index:
         raise ValueError("ends must be an int32 vector on x's device")
     return ends if ends.is_contiguous() else ends.contiguous()
 
@@ -155,21 +155,21 @@ def expert_matmul(x, w, ends, transposed: bool = False, stream=None):
     """
     if stream is not None:
         return _on(stream, x, expert_matmul, x, w, ends, transposed)
-    code = _code(x, "x")
+    code, index = _code(x, "x"), x.get_device()
     if x.dim() != 2:
         raise ValueError("x must be (rows, k)")
     x2, rows, k, ldx = _rows(x)
-    w, ldw, stride_w = _matrices(w, x)
+    w, ldw, stride_w = _matrices(w, x, index)
     experts, kw, n = w.shape
     if transposed:
         kw, n = n, kw
     if kw != k:
         raise ValueError(f"w's matrices of {tuple(w.shape[1:])} do not fit rows of {k}")
-    ends = _ends(ends, x)
+    ends = _ends(ends, index)
     if ends.shape[0] != experts:
         raise ValueError("ends must hold one entry per expert")
-    y = x.new_empty((rows, n))
-    _call("tm_expert_matmul", x.get_device(), x2.data_ptr(), ldx, w.data_ptr(), ldw, stride_w, ends.data_ptr(),
+    y = x.new_empty_strided((rows, n), (n, 1))
+    _call("tm_expert_matmul", index, x2.data_ptr(), ldx, w.data_ptr(), ldw, stride_w, ends.data_ptr(),
           y.data_ptr(), n, rows, experts, k, n, 1 if transposed else 0, code)
     return y
 
@@ -179,17 +179,17 @@ def expert_wgrad(x, dy, ends, dtype=None, stream=None):
     bf16 (for bf16 rows).  Experts without rows get zeros."""
     if stream is not None:
         return _on(stream, x, expert_wgrad, x, dy, ends, dtype)
-    code = _code(x, "x")
+    code, index = _code(x, "x"), x.get_device()
     if x.dim() != 2 or dy.dim() != 2 or dy.shape[0] != x.shape[0]:
         raise ValueError("x and dy must be (rows, k) and (rows, n)")
-    if dy.dtype is not x.dtype or dy.device != x.device:
+    if dy.dtype is not x.dtype or dy.get_device() != index:
         raise ValueError("dy must have x's type and device")
     x2, rows, k, ldx = _rows(x)
     dy2, _, n, lddy = _rows(dy)
-    ends = _ends(ends, x)
+    ends = _ends(ends, index)
     experts = ends.shape[0]
-    dw = x.new_empty((experts, k, n), dtype=dtype or _F32)
-    _call("tm_expert_wgrad", x.get_device(), x2.data_ptr(), ldx, dy2.data_ptr(), lddy, ends.data_ptr(),
+    dw = x.new_empty_strided((experts, k, n), (k * n, n, 1), dtype=dtype or _F32)
+    _call("tm_expert_wgrad", index, x2.data_ptr(), ldx, dy2.data_ptr(), lddy, ends.data_ptr(),
           dw.data_ptr(), n, k * n if experts > 1 else 0, rows, experts, k, n, code, _code(dw, "dtype"))
     return dw
 
@@ -199,24 +199,24 @@ def _policy_loss(logits, targets, old_logp, advantages, weights, ref_logp, clip_
     if stream is not None:
         return _on(stream, logits, _policy_loss, logits, targets, old_logp, advantages, weights, ref_logp, clip_low,
                    clip_high, kl, temperature, None, grad, keep)
-    code = _code(logits, "logits")
+    code, index = _code(logits, "logits"), logits.get_device()
     if logits.dim() != 2:
         raise ValueError("logits must be (rows, vocabulary)")
     l2, rows, vocab, ld = _rows(logits)
-    targets = _vector(targets, logits, "targets", rows, _I64)
-    old_logp = _vector(old_logp, logits, "old_logp", rows, _F32)
-    advantages = _vector(advantages, logits, "advantages", rows, _F32)
-    weights = _vector(weights, logits, "weights", rows, _F32)
+    targets = _vector(targets, index, "targets", rows, _I64)
+    old_logp = _vector(old_logp, index, "old_logp", rows, _F32)
+    advantages = _vector(advantages, index, "advantages", rows, _F32)
+    weights = _vector(weights, index, "weights", rows, _F32)
     if ref_logp is not None:
-        ref_logp = _vector(ref_logp, logits, "ref_logp", rows, _F32)
-    loss = logits.new_empty((), dtype=_F32)
+        ref_logp = _vector(ref_logp, index, "ref_logp", rows, _F32)
+    loss = logits.new_empty_strided((), (), dtype=_F32)
     logp = torch.empty_like(weights)
     lse = slope = dlogits = None
     if grad:
         dlogits = _empty_like(logits)
     if keep:
         lse, slope = torch.empty_like(weights), torch.empty_like(weights)
-    _call("tm_policy_loss", logits.get_device(), l2.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
+    _call("tm_policy_loss", index, l2.data_ptr(), ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), weights.data_ptr(), _ptr(ref_logp), clip_low, clip_high, kl, temperature,
           loss.data_ptr(), logp.data_ptr(), _ptr(lse), _ptr(slope), _ptr(dlogits), vocab, rows, vocab, code)
     return loss, logp, lse, slope, dlogits
@@ -251,16 +251,16 @@ def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: fl
     device; None: 1)."""
     if stream is not None:
         return _on(stream, logits, policy_loss_backward, logits, targets, lse, slope, grad, temperature)
-    code = _code(logits, "logits")
+    code, index = _code(logits, "logits"), logits.get_device()
     if logits.dim() != 2:
         raise ValueError("logits must be (rows, vocabulary)")
     l2, rows, vocab, ld = _rows(logits)
-    targets = _vector(targets, logits, "targets", rows, _I64)
-    lse = _vector(lse, logits, "lse", rows, _F32)
-    slope = _vector(slope, logits, "slope", rows, _F32)
-    if grad is not None and (grad.dim() != 0 or grad.dtype is not _F32 or grad.device != logits.device):
+    targets = _vector(targets, index, "targets", rows, _I64)
+    lse = _vector(lse, index, "lse", rows, _F32)
+    slope = _vector(slope, index, "slope", rows, _F32)
+    if grad is not None and (grad.dim() != 0 or grad.dtype is not _F32 or grad.get_device() != index):
         raise ValueError("grad must be an fp32 scalar on the logits' device")
     dlogits = _empty_like(logits)
-    _call("tm_policy_loss_backward", logits.get_device(), l2.data_ptr(), ld, targets.data_ptr(),
+    _call("tm_policy_loss_backward", index, l2.data_ptr(), ld, targets.data_ptr(),
           lse.data_ptr(), slope.data_ptr(), _ptr(grad), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
     return dlogits
