@@ -151,7 +151,8 @@ constexpr uint64_t kLongest = 2816;
 // rows over 53 experts of 192 x 6976, bf16: 26 on 16 rows, 57 on the 64 tile of
 // direct loads; 80 rows over 5 of 7960 x 1970, fp32: 95 on 32 rows, 184 on 64: the
 // larger groups of an uneven call should not need two tiles); 16 rows up to 8 on average
-// (48 rows over 8 of 2048 x 4096: 35, 37 on 32 rows; 192 over 16: 68 against 64), in slices
+// and for a call of no more than 16 (13 rows of 2356 x 6568, fp32: 23, 30 on 32 rows;
+// 48 over 8 of 2048 x 4096: 35, 37; 192 over 16: 68 against 64), in slices
 // of 512 values and more (24 rows over 8 of 768 x 2048, bf16 and fp32: 6.5 and 12.3, 9.2 and
 // 16.2 from 256 on).  fp32 and odd
 // operands stay with 32 rows up to 64 (105 rows over 2 of 4869 x 5632, odd: 47, 51 on
@@ -164,7 +165,7 @@ ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
   ExpertPlan P{};
   if (mean <= (staged ? 64u : 24u)) {
     P.staged = true;
-    P.tile = mean <= 8 ? 16 : 32;
+    P.tile = mean <= 8 || A.rows <= 16 ? 16 : 32;
     P.slices = slices_for(tiles(P.tile, 64), A.k, 1024, 512);
   } else {
     const uint64_t t[3] = {tiles(64, 64), tiles(128, 128), tiles(256, 256)};
@@ -185,7 +186,12 @@ ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
 // rows, and chunks are summed afterwards (24162 rows, unevenly over 11 experts of
 // 73 x 2069, fp32: 128 us; 255 with every group cut into the same number of
 // parts).  Short groups gain less than the sum costs: 10342 rows over 43 experts of
-// 1133 x 103, bf16, are 19 us whole and 31 in chunks.
+// 1133 x 103, bf16, are 19 us whole and 31 in chunks.  With fewer tiles than compute
+// units the longest group alone may be the call's time, and groups of 256 rows on
+// average are cut too (6000 rows unevenly over 20 of 128 x 128: fp32 41 and 15.5, bf16 14.3 and
+// 11.5; evenly 9617 over 24 of 114 x 133: 15.2 and 17.8, 8.1 and 11.7); below 4096 rows the second
+// launch costs more (1200 over 4 of 256 x 512, bf16: 7.8 and 10.6), and so it does on the 128
+// tile (5000 over 12 of 768 x 300, bf16: 19 and 24).
 ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
   ExpertPlan P{};
   P.staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, A.n) && A.stride_b % 8 == 0 && whole(A.out, A.ldo, A.n));
@@ -196,7 +202,9 @@ ExpertPlan plan_expert_wgrad(const ExpertArgs& A, bool f32) {
   const uint64_t want = P.tile == 64 ? wanted(f32) : 544;
   if ((P.tile == 64 || (P.tile == 128 && P.staged)) && experts * tiles(P.tile) <= want + want / 2) {
     const uint64_t chunk = std::max(fewest(f32), up(rows * tiles(P.tile), want * 64) * 64);
-    if (rows >= 2 * chunk && rows / experts >= 2 * fewest(f32)) P.chunk = int(chunk);
+    const uint64_t mean = rows / experts;
+    const bool uneven = P.tile == 64 && experts * tiles(64) <= 256 && mean >= 256 && rows >= 4096;
+    if (rows >= 2 * chunk && (mean >= 2 * fewest(f32) || uneven)) P.chunk = int(chunk);
   }
   if (f32 && P.tile == 64 && rows / experts > kLongest)
     P.chunk = P.chunk > 0 ? std::min(P.chunk, int(kLongest)) : int(kLongest);

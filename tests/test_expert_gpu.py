@@ -236,6 +236,8 @@ def test_ends_that_make_no_sense_stay_in_bounds():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("counts,k,n", [
     ([0, 7000, 1, 0, 513, 30, 0], 65, 33), ([1024, 1024, 0, 2048], 64, 72),
+    # few tiles, groups of 256 rows and more on average
+    ([3000, 40, 900, 0, 513, 30, 200, 1, 260, 700], 70, 65),
     # more experts than a wave has lanes, rows of none at the end
     ([3000 if e % 9 == 4 else 1200 * (e % 3) for e in range(70)], 8, 9),
 ])
