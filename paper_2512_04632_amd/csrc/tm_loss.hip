@@ -367,6 +367,7 @@ __global__ __launch_bounds__(1024) void k_loss_join(const LossArgs A) {
       }
       s = wave_join(s, c);
       o = finish<T>(A, r, s);
+      if (lane == 0) A.stats[r] = make_float2(s.m, 1.f / s.s);
     }
     if (lane == 0) write_row(A, r, o);
     total += double(o.loss);
@@ -395,10 +396,15 @@ __global__ __launch_bounds__(1024) void k_loss_sum(const float* row_loss, int ro
   if (threadIdx.x == 0) *out = float(sums[0]);
 }
 
-// dlogits from lse and slope, a workgroup per chunk of a row.  Rows of slope
-// 0 are not read.  l / tau - lse is rounded once (fma).  Bound by HBM: 3000 x 32001
-// fp32, a tenth of the rows without part, 125 us, 5.8 TB/s.
-template <class T>
+// dlogits of the rows' slopes, a workgroup per chunk of a row.  Rows without a
+// slope are not read.
+//   STATS = true   of rows that k_loss_join has just joined: from their maximum
+//                  and sum, as where one workgroup has the whole row.
+//   STATS = false  from lse, which is all that is left of an earlier call: l / tau -
+//                  lse is rounded once (fma), but carries the rounding of lse.
+//                  Bound by HBM: 3000 x 32001 fp32, a tenth of the rows without
+//                  part, 125 us, 5.8 TB/s.
+template <class T, bool STATS>
 __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
   const int64_t r = blockIdx.x / A.chunks;
   const int q = blockIdx.x - int(r) * A.chunks;
@@ -406,20 +412,32 @@ __global__ __launch_bounds__(256) void k_loss_gradient(const LossArgs A) {
   const float slope = A.slope[r];
   const char* l = A.logits + r * A.ld * T::kBytes;
   char* d = A.dlogits + r * A.ldd * T::kBytes;
-  const float f = slope * A.inv_temp * (A.grad != nullptr ? *A.grad : 1.f);
-  const float lse = A.lse[r];
+  const float f = slope * A.inv_temp * (!STATS && A.grad != nullptr ? *A.grad : 1.f);
+  const bool none = STATS ? f == 0.f : slope == 0.f;
+  const float c = A.inv_temp * kLog2e;
+  float2 stats = make_float2(0.f, 0.f);
+  float lse = 0.f;
+  if constexpr (STATS) {
+    if (!none) stats = A.stats[r];
+  } else {
+    lse = A.lse[r];
+  }
   const int y = target_of(A, r);
   for (int at = first + threadIdx.x * T::W; at < last; at += 256 * T::W) {
     float v[T::W];
-    if (slope == 0.f) {
+    if (none) {
 #pragma unroll
       for (int i = 0; i < T::W; ++i) v[i] = 0.f;
     } else {
       load_vec<T>(l, at, last, 0.f, v);
+      if constexpr (STATS) {
+        gradient_vec<T>(v, y - at, stats.x, c, stats.y, f);
+      } else {
 #pragma unroll
-      for (int i = 0; i < T::W; ++i) {
-        const float p = exp2_fast(fmaf(v[i], A.inv_temp, -lse) * kLog2e);
-        v[i] = f * ((i == y - at ? 1.f : 0.f) - p);
+        for (int i = 0; i < T::W; ++i) {
+          const float p = exp2_fast(fmaf(v[i], A.inv_temp, -lse) * kLog2e);
+          v[i] = f * ((i == y - at ? 1.f : 0.f) - p);
+        }
       }
     }
     store_vec<T>(d, at, last, v);
@@ -474,7 +492,7 @@ hipError_t forward_t(const LossArgs& A, hipStream_t st) {
     const dim3 grid(uint32_t(A.rows) * A.chunks);
     hipLaunchKernelGGL((k_loss_part<T>), grid, dim3(256), 0, st, A);
     hipLaunchKernelGGL((k_loss_join<T>), dim3(1), dim3(1024), 0, st, A);
-    if (A.dlogits != nullptr) hipLaunchKernelGGL((k_loss_gradient<T>), grid, dim3(256), 0, st, A);
+    if (A.dlogits != nullptr) hipLaunchKernelGGL((k_loss_gradient<T, true>), grid, dim3(256), 0, st, A);
     return hipGetLastError();
   }
   if (A.rows > 0) launch_rows<T>(A, st);
@@ -501,8 +519,8 @@ hipError_t launch_loss(const LossArgs& A, bool f32, hipStream_t st) {
 
 hipError_t launch_loss_backward(const LossArgs& A, bool f32, hipStream_t st) {
   const dim3 grid(uint32_t(A.rows) * uint32_t(A.chunks));
-  if (f32) hipLaunchKernelGGL((loss::k_loss_gradient<elem::F32>), grid, dim3(256), 0, st, A);
-  else hipLaunchKernelGGL((loss::k_loss_gradient<elem::Bf16>), grid, dim3(256), 0, st, A);
+  if (f32) hipLaunchKernelGGL((loss::k_loss_gradient<elem::F32, false>), grid, dim3(256), 0, st, A);
+  else hipLaunchKernelGGL((loss::k_loss_gradient<elem::Bf16, false>), grid, dim3(256), 0, st, A);
   return hipGetLastError();
 }
 

@@ -299,14 +299,15 @@ tm_status policy_loss(const void* logits, int64_t ld, const int64_t* targets, co
   A.chunks = int32_t(chunks);
   A.chunk = int32_t(chunk_length(vocab, chunks));
   // workspace: the rows' shares of the loss, lse and slope where the caller
-  // keeps none, the chunks' maxima and sums
+  // keeps none, the chunks' maxima and sums, and those of their rows
   const size_t line = size_t(tmk::align256(uint64_t(rows) * 4u));
-  const size_t bytes = 3u * line + (chunks > 1 ? size_t(rows) * size_t(chunks) * sizeof(float2) : 0u) + 256u;
+  const size_t bytes = 3u * line + (chunks > 1 ? size_t(rows) * size_t(chunks + 1) * sizeof(float2) : 0u) + 256u;
   return run_op(TM_PHASE_POLICY_LOSS, bytes, stream, [&](char* ws, hipStream_t st) {
     A.row_loss = reinterpret_cast<float*>(ws);
     A.lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + line);
     A.slope = slope != nullptr ? slope : reinterpret_cast<float*>(ws + 2u * line);
     A.part = reinterpret_cast<float2*>(ws + 3u * line);
+    A.stats = A.part + rows * chunks;
     return tmk::launch_loss(A, dtype == TM_DTYPE_F32, st);
   });
 }

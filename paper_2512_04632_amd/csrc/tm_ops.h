@@ -84,6 +84,7 @@ struct LossArgs {
   char* dlogits;             // nullptr: no gradient
   float* row_loss;           // workspace: each row's share of the loss
   float2* part;              // workspace: (max, sum of exponentials) of each chunk, [rows][chunks]
+  float2* stats;             // workspace: (max, 1 / sum) of each row that is cut into chunks
   int64_t ld, ldd;
   int32_t rows, vocab;
   int32_t chunks, chunk;     // chunks of a row and their length

@@ -291,3 +291,36 @@ def test_few_long_rows(rows, vocab, dtype):
         test_masked_rows_are_not_read(rows, vocab, dtype)
     test_masked_vocabulary(max(rows, 4), vocab, dtype)
     test_strides_and_in_place(rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(4, 600), (4, 20000), (4, 40001), (16, 32768), (32, 70001), (33, 70001),
+                                        (40, 32001)])
+def test_gradient_of_logits_of_large_size(rows, vocab, dtype):
+    """However the rows are run, the gradient depends on the distances of the logits from their maximum
+    alone: rows of nothing but the type's lowest value, and logits with a common offset of 10^4.
+
+    With Z the largest distance over tau of a row, a probability is off by 2 (D + 16 u) of itself, where D =
+    (V / 2048 + 64 + 8 Z) u (see above), the target's 1 - p by a rounding more; the slope is policy_loss's own."""
+    log(f"case: policy loss, gradient of large logits {rows} x {vocab} {dtype}")
+    s = _inputs(rows, vocab, dtype, seed=12, masked=0.0)
+    s["logits"] = (s["logits"].double() + 1e4).to(DT[dtype])
+    s["logits"][2] = torch.finfo(DT[dtype]).min
+    at = torch.arange(rows, device="cuda")
+    z = s["logits"].double() / TAU
+    z = z - z.amax(1, keepdim=True)   # 64 bits hold no log V beside the lowest value either
+    logp = z[at, s["targets"]] - z.logsumexp(1)
+    s["old_logp"], s["ref_logp"] = (logp - 0.05).float(), (logp + 0.2).float()
+    kw = dict(clip_low=LOW, clip_high=HIGH, kl=KL, temperature=TAU)
+    slope = tm.policy_loss(**s, **kw)[3].double()
+    _, got_logp, grad = tm.policy_loss_with_grad(**s, **kw)
+    assert (slope != 0).all()
+    D = (vocab / 2048 + 64 + 8 * -z.amin(1)) * U
+    _close("logp", got_logp, logp, D + 2 * U * logp.abs())
+    p = z.softmax(1)
+    hit = torch.zeros_like(p)
+    hit[at, s["targets"]] = 1
+    want = (slope / TAU)[:, None] * (hit - p)
+    bound = (slope.abs() / TAU)[:, None] * (2 * p * (D + 16 * U)[:, None] + 4 * U * hit)
+    _close("grad", grad, want, bound + (2.0 ** -8 if dtype == "bf16" else 2 * U) * (want.abs() + bound) + 1e-38)
+    assert (p[2] == 1 / vocab).all()
