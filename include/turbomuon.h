@@ -282,9 +282,9 @@ tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
  *   k, n  1..TM_MAX_DIM;  experts 1..TM_MAX_EXPERTS.
  * y overlaps nothing that is read.  Sums are fp32.  fp32 products of many rows
  * are formed of three bf16 parts of each operand on the matrix cores and are as
- * exact as a sum of fp32 products (tiles with NaN, Inf or values that round past
- * the largest bf16 take fp32 products); operands below about 2^-110 keep fewer
- * bits there.
+ * exact as a sum of fp32 products; tiles with values that three parts do not hold
+ * exactly (NaN, Inf, values that round past the largest bf16, values below about
+ * 2^-110) or with results that are not finite take fp32 products.
  */
 tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t stride_w,
                            const int32_t* ends, void* y, int64_t ldy, int64_t rows, int64_t experts,

@@ -28,10 +28,10 @@
 // small terms first; mid lo, lo mid and lo lo, at most 2^-23 of it, are left out.  Six
 // bf16 instructions take 96 clocks where the eight of fp32 for the same 32 values
 // take 256 (16384 rows over 8 experts of 2048 x 2048: 0.80 ms, 172 TFLOP/s, against 1.03 ms
-// of fp32 instructions).  Values that three parts cannot hold (NaN, infinities, and
-// the few that round to one) set a flag, and the tile is done again with fp32
-// instructions; parts below the smallest normal number may vanish (x below about
-// 2^-110 keeps fewer bits).  On the smaller tiles the splitting costs what the
+// of fp32 instructions).  A tile with a value that three parts do not hold exactly (NaN,
+// infinities, the few that round to one, those below about 2^-110 whose last bits lie below
+// the smallest bf16) or with a result that is not finite is done again with fp32
+// instructions.  On the smaller tiles the splitting costs what the
 // instructions save (2048 rows of 1024 x 1024: 45 us, 40 without; 80 rows over 5 experts
 // of 7960 x 1970: 111 against 95), and fp32 multiplies as it is.
 //
@@ -237,6 +237,16 @@ struct Shape {
   static_assert(FM >= 1 && FN >= 1, "a block for every wave");
 };
 
+// Row and first of the four columns that a lane holds of block (fm, fn).
+template <class S>
+__device__ inline int staged_row(int fm) {
+  return (int(threadIdx.x >> 6) / S::WN * S::FM + fm) * 16 + int(threadIdx.x & 15);
+}
+template <class S>
+__device__ inline int staged_col(int fn) {
+  return (int(threadIdx.x >> 6) % S::WN * S::FN + fn) * 16 + 4 * (int(threadIdx.x & 63) >> 4);
+}
+
 // begin(fast), then step(kt, kt % D, fast) for each stage kt < nk; fast (a constant)
 // while the stages that they load, at most D for begin and kt + D for a step, are
 // among the first `unchecked` (steps that load one further say one less).  The
@@ -315,15 +325,13 @@ __device__ inline void product_staged(f32x4_t (&acc)[S::FM][S::FN], char* smem, 
   staged_loop<D>(nk, min(sa.whole, sb.whole) / BK - 1, begin, step);
 }
 
-// The three parts of four values, each as four bf16 (hi first).  True if one of
-// the values has none: not finite, or past the largest bf16.
-__device__ inline bool split3(u32x4_t q, uint2 (&part)[3]) {
+// The three parts of four values, each as four bf16 (hi first).  The third is what the
+// others leave, `rest` its bits: where the lower 16 of them are not zero, it has bits below
+// the smallest bf16 (2^-133; values from about 2^-110 down) and is no bf16 itself.  An
+// infinity, a NaN or a value that rounds past the largest bf16 has a part that is not finite.
+__device__ inline void split3(u32x4_t q, uint2 (&part)[3], uint32_t (&rest)[4]) {
   float x[4];
   F32::unpack(q, x);
-  const float most = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
-  bool bad = !(most < 3.38e38f);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= x[i] != x[i];   // fmaxf passes a NaN over
 #pragma unroll
   for (int p = 0; p < 3; ++p) {
     uint32_t h[4];
@@ -334,29 +342,47 @@ __device__ inline bool split3(u32x4_t q, uint2 (&part)[3]) {
     }
     part[p] = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
   }
-  return bad;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) rest[i] = __float_as_uint(x[i]);
 }
 
 // A stage of 32 fp32 values as three planes in LDS, TS * 64 bytes each: a
 // contiguous operand as rows of 64 bytes, 16-byte chunks XORed by (row / 4) % 4;
 // a row-major one as rows of the tile's columns, as for bf16.
-template <int TS, bool KC, int Q>
-__device__ inline bool store3(char* lds, const u32x4_t (&v)[Q]) {
+template <int TS, bool KC>
+struct Planes {
   using St = Stager<F32, TS, KC>;
-  static_assert(TS * kStageBytes % 4096 == 0, "a chunk for every thread");
-  bool bad = false;
+  static_assert(TS * kStageBytes % 4096 == 0 && 256 % St::PER == 0, "a chunk for every thread, the same of every row");
+  uint32_t low[2] = {0u, 0u};   // lower bits of the third parts seen: of columns 0 and 1, 2 and 3 of the thread's chunk
+
+  __device__ void store(char* lds, const u32x4_t (&v)[St::Q]) {
 #pragma unroll
-  for (int i = 0; i < Q; ++i) {
-    const int r = St::row(i), c = St::chunk(i);
-    const int at = KC ? r * 64 + 16 * ((c >> 1) ^ ((r / 4) % 4)) + 8 * (c & 1)
-                      : r * 2 * TS + 32 * ((c >> 2) ^ swz_y<TS>(r)) + 8 * (c & 3);
-    uint2 part[3];
-    bad |= split3(v[i], part);
+    for (int i = 0; i < St::Q; ++i) {
+      const int r = St::row(i), c = St::chunk(i);
+      const int at = KC ? r * 64 + 16 * ((c >> 1) ^ ((r / 4) % 4)) + 8 * (c & 1)
+                        : r * 2 * TS + 32 * ((c >> 2) ^ swz_y<TS>(r)) + 8 * (c & 3);
+      uint2 part[3];
+      uint32_t x[4];
+      split3(v[i], part, x);
+      if constexpr (KC) {
+        low[0] |= x[0] | x[1] | x[2] | x[3];
+      } else {
+        low[0] |= __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
+        low[1] |= __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
+      }
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(lds + p * TS * 64 + at) = part[p];
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(lds + p * TS * 64 + at) = part[p];
+    }
   }
-  return bad;
-}
+  // Whether a value lost bits.  What was read beside a row-major operand's last column
+  // (`limit` are there) is not part of it, and must not decide how the tile is done.
+  __device__ bool lost(int limit) const {
+    if constexpr (KC) return (low[0] & 0xffffu) != 0u;
+    const int n = limit - 4 * St::chunk(0);
+    return ((low[0] & 0xffffu) != 0u && n > 0) || ((low[0] >> 16) != 0u && n > 1) ||
+           ((low[1] & 0xffffu) != 0u && n > 2) || ((low[1] >> 16) != 0u && n > 3);
+  }
+};
 
 // One plane's operands: 8 values 8 g .. + 7 of row or column 16 (w F + f) + lane % 16.
 template <int TS, bool KC, int F>
@@ -374,7 +400,10 @@ __device__ inline void load_plane(uint4 (&v)[F], const char* st, int w) {
 }
 
 // fp32 as three parts, in one LDS buffer with two barriers a stage, so that two
-// workgroups share a compute unit.  False if a value has no parts.
+// workgroups share a compute unit.  False if a value has no parts: its third one has
+// lost bits, or a result is not finite (a part was not, or the product of two high parts,
+// each up to 2^-8 above its value, passed the largest fp32 where that of the values does
+// not).
 template <class S, bool AKC, bool BKC>
 __device__ inline bool product_parts(f32x4_t (&acc)[S::FM][S::FN], char* smem, const Source& a, const Source& b, int K) {
   using SA = Stager<F32, S::TM, AKC>;
@@ -392,10 +421,11 @@ __device__ inline bool product_parts(f32x4_t (&acc)[S::FM][S::FN], char* smem, c
   sa.start(a, K);
   sb.start(b, K);
   const int nk = (K + BK - 1) / BK;
-  bool bad = false;
+  Planes<S::TM, AKC> planes_a;
+  Planes<S::TN, BKC> planes_b;
   auto store = [&](char* lds, const u32x4_t (&qa)[SA::Q], const u32x4_t (&qb)[SB::Q]) __attribute__((always_inline)) {
-    bad |= store3<S::TM, AKC>(lds, qa);
-    bad |= store3<S::TN, BKC>(lds + 3 * PA, qb);
+    planes_a.store(lds, qa);
+    planes_b.store(lds + 3 * PA, qb);
   };
   auto multiply = [&](const char* lds) __attribute__((always_inline)) {
     uint4 fb[3][S::FN];
@@ -430,6 +460,14 @@ __device__ inline bool product_parts(f32x4_t (&acc)[S::FM][S::FN], char* smem, c
     __syncthreads();
     multiply(smem);
   });
+  bool bad = planes_a.lost(a.limit) || planes_b.lost(b.limit);
+#pragma unroll
+  for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)   // of contiguous operands every row is one that is there
+        bad |= (AKC || staged_row<S>(i) < a.limit) && (BKC || staged_col<S>(j) + u < b.limit) && !(fabsf(acc[i][j][u]) < INFINITY);
   return !__syncthreads_or(bad);
 }
 
@@ -440,16 +478,6 @@ __device__ inline void product_tile(f32x4_t (&acc)[S::FM][S::FN], char* smem, co
     if (product_parts<S, AKC, BKC>(acc, smem, a, b, K)) return;
   }
   product_staged<T, S, AKC, BKC>(acc, smem, a, b, K);
-}
-
-// Row and first of the four columns that a lane holds of block (fm, fn).
-template <class S>
-__device__ inline int staged_row(int fm) {
-  return (int(threadIdx.x >> 6) / S::WN * S::FM + fm) * 16 + int(threadIdx.x & 15);
-}
-template <class S>
-__device__ inline int staged_col(int fn) {
-  return (int(threadIdx.x >> 6) % S::WN * S::FN + fn) * 16 + 4 * (int(threadIdx.x & 63) >> 4);
 }
 
 // bf16 through LDS (free after the product's last barrier): 16 bytes a lane along the rows.

@@ -345,3 +345,73 @@ def test_refusals():
     assert e.value.status == tm.TM_ERR_UNSUPPORTED
     assert tm.expert_matmul(x[:0], w, _ends([0, 0])).shape == (0, 8)
     assert not tm.expert_wgrad(x[:0], x[:0], _ends([0, 0])).any()
+
+
+# fp32 calls that are large enough for products of bf16 parts: rows, k, n of the rows' products and of the gradient
+PARTS = [(2048, 8, 4096), (8, 2048, 4096)]
+
+
+def _forms(x, w, dy, ends):
+    """The rows' product, the same on transposed matrices, and the weight gradient, with their operands."""
+    yield "rows", lambda: tm.expert_matmul(x, w, ends)
+    yield "transposed", lambda: tm.expert_matmul(dy, w, ends, transposed=True)
+    yield "wgrad", lambda: tm.expert_wgrad(x, dy, ends)
+
+
+@pytest.mark.parametrize("up,down", [(0, 0), (-108, 0), (-122, 60), (-140, 60), (60, -140)])
+def test_fp32_parts_keep_small_values(up, down):
+    """Values whose last bits lie below the smallest bf16 keep the accuracy of fp32, in every form."""
+    log(f"case: fp32 products of values of 2^{up} and 2^{down}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    for rows, k, n in PARTS:
+        x = (_randn(g, (rows, k), "f32").double() * 2.0 ** up).float()
+        w = (_randn(g, (1, k, n), "f32").double() * 2.0 ** down).float()
+        dy = (_randn(g, (rows, n), "f32").double() * 2.0 ** down).float()
+        ends = _ends([rows])
+        if rows > k:
+            _check_rows(x, w, [rows], False, "f32", tm.expert_matmul(x, w, ends))
+            wt = w.transpose(1, 2).contiguous()
+            _check_rows(x, wt, [rows], True, "f32", tm.expert_matmul(x, wt, ends, transposed=True))
+        else:
+            _check_wgrad(x, dy, [rows], "f32", tm.expert_wgrad(x, dy, ends))
+
+
+def test_fp32_parts_of_products_below_the_largest_value():
+    """A product just below the largest fp32, whose high parts multiply to more than it, stays finite; one
+    above it becomes an infinity."""
+    log("case: fp32 products next to the largest value")
+    big = 1.9990 * 2.0 ** 63
+    x, w = torch.full((2048, 1), big, device="cuda"), torch.full((1, 1, 4096), 1.9985 * 2.0 ** 63, device="cuda")
+    w[0, 0, 7] = 2.0 ** 65
+    y = tm.expert_matmul(x, w, _ends([2048]))
+    want = float(x[0, 0].double() * w[0, 0, 0].double())
+    assert (y[:, 7] == float("inf")).all()
+    keep = torch.arange(4096, device="cuda") != 7
+    assert ((y[:, keep].double() - want).abs() <= U * want).all()
+    dw = tm.expert_wgrad(x[:1].expand(1, 2048).contiguous(), w[0, :, keep], _ends([1]))
+    assert ((dw.double() - want).abs() <= U * want).all()
+
+
+@pytest.mark.parametrize("pad", [float("nan"), float("inf"), 1e-41])
+def test_fp32_results_do_not_depend_on_memory_beside_the_operands(pad):
+    log(f"case: fp32 products, {pad} beside the operands")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    for rows, k, n in ((2050, 130, 4093), (131, 2047, 4093)):
+        ends = _ends([rows])
+
+        def inside(*shape):
+            store = torch.zeros(shape[:-2] + (shape[-2] + 2, shape[-1] + 7), device="cuda")
+            view = store[..., 1:-1, 2:-5]
+            view.copy_(_randn(g, shape, "f32"))
+            return store, view
+
+        stores, (x, w, dy) = zip(*(inside(rows, k), inside(1, k, n), inside(rows, n)))
+        ref = [f() for _, f in _forms(x, w, dy, ends)]
+        for store, view in zip(stores, (x, w, dy)):
+            kept = view.clone()
+            store.fill_(pad)
+            view.copy_(kept)
+        for (name, f), want in zip(_forms(x, w, dy, ends), ref):
+            assert torch.equal(f(), want), (name, rows)
