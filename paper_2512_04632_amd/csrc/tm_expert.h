@@ -18,6 +18,9 @@ namespace expert {
 
 using namespace tile;
 
+// Longest run of a sum in fp32 instructions (tm_expert.hip: plan_expert_matmul).
+constexpr uint64_t kLongest = 2816;
+
 // A run of rows [first, last) of one expert (experts: the rows of none).
 struct Group {
   int e, first, last;

@@ -135,7 +135,6 @@ int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], u
 // the summed index of each.
 uint64_t wanted(bool f32) { return f32 ? 768 : 544; }
 uint64_t fewest(bool f32) { return f32 ? 256 : 512; }
-constexpr uint64_t kLongest = 2816;
 
 // The staged 128 tile: slices from 8192 values on (2048 rows of 8201 x 2048, bf16: 104,
 // 112 in one; fp32 450, 538; of 4098 x 2048, bf16, 60 against 54).

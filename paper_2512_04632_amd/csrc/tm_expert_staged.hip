@@ -471,15 +471,6 @@ __device__ inline bool product_parts(f32x4_t (&acc)[S::FM][S::FN], char* smem, c
   return !__syncthreads_or(bad);
 }
 
-// The product in the type's way.
-template <class T, class S, bool AKC, bool BKC>
-__device__ inline void product_tile(f32x4_t (&acc)[S::FM][S::FN], char* smem, const Source& a, const Source& b, int K) {
-  if constexpr (T::kBytes == 4 && S::kParts) {
-    if (product_parts<S, AKC, BKC>(acc, smem, a, b, K)) return;
-  }
-  product_staged<T, S, AKC, BKC>(acc, smem, a, b, K);
-}
-
 // bf16 through LDS (free after the product's last barrier): 16 bytes a lane along the rows.
 template <class S>
 __device__ inline void store_tile(Bf16, const f32x4_t (&acc)[S::FM][S::FN], char* smem, char* out, int64_t ld, int rows,
@@ -509,18 +500,65 @@ __device__ inline void store_tile(Bf16, const f32x4_t (&acc)[S::FM][S::FN], char
   }
 }
 
+// add: to what this thread stored there before.
 template <class S>
-__device__ inline void store_tile(F32, const f32x4_t (&acc)[S::FM][S::FN], char*, char* out, int64_t ld, int rows, int cols) {
+__device__ inline void store_tile(F32, const f32x4_t (&acc)[S::FM][S::FN], char*, char* out, int64_t ld, int rows, int cols,
+                                  bool add = false) {
 #pragma unroll
   for (int fm = 0; fm < S::FM; ++fm) {
     const int r = staged_row<S>(fm);
     if (r >= rows) continue;
 #pragma unroll
     for (int fn = 0; fn < S::FN; ++fn) {
-      const float v[4] = {acc[fm][fn][0], acc[fm][fn][1], acc[fm][fn][2], acc[fm][fn][3]};
+      float v[4] = {acc[fm][fn][0], acc[fm][fn][1], acc[fm][fn][2], acc[fm][fn][3]};
+      if (add) {
+        float before[4];
+        elem::load_vec<F32>(out + r * ld * 4, staged_col<S>(fn), cols, 0.f, before);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] += before[u];
+      }
       elem::store_vec<F32>(out + r * ld * 4, staged_col<S>(fn), cols, v);
     }
   }
+}
+
+// `s` from value `at` of the summed index on.
+template <class T, bool KC>
+__device__ inline Source from(const Source& s, int at) {
+  return Source{s.p + (KC ? int64_t(at) : at * s.ld) * T::kBytes, s.ld, s.limit, KC ? s.left : s.left - at};
+}
+
+// The product in the type's way, and its result to `out`.  RUNS: sums may be longer than
+// kLongest; those of fp32 instructions are then taken in runs of it, each added to what
+// the ones before left in `out` (16 KB of a 64 tile for 1.4 MB of operands).
+template <class T, class TO, class S, bool AKC, bool BKC, bool RUNS>
+__device__ inline void product_tile(char* smem, const Source& a, const Source& b, int K, char* out, int64_t ld, int rows,
+                                    int cols) {
+  f32x4_t acc[S::FM][S::FN];
+  if constexpr (T::kBytes == 4 && S::kParts) {
+    if (product_parts<S, AKC, BKC>(acc, smem, a, b, K)) {
+      store_tile<S>(TO{}, acc, smem, out, ld, rows, cols);
+      return;
+    }
+  }
+  if constexpr (T::kBytes == 4 && RUNS) {
+    static_assert(kLongest % (kStageBytes / 4) == 0, "runs of whole stages");
+    if (K > int(kLongest)) {
+      for (int at = 0; at < K; at += int(kLongest)) {
+        // a zero that the compiler does not know: addresses are formed anew in every run, and
+        // do not take registers beside the product's
+        int64_t zero = 0;
+        asm volatile("" : "+s"(zero));
+        const Source ra{a.p + zero, a.ld + zero, a.limit, a.left}, rb{b.p + zero, b.ld + zero, b.limit, b.left};
+        product_staged<T, S, AKC, BKC>(acc, smem, from<T, AKC>(ra, at), from<T, BKC>(rb, at), min(K - at, int(kLongest)));
+        asm volatile("" : "+s"(zero));
+        store_tile<S>(TO{}, acc, smem, out + zero, ld + zero, rows, cols, at > 0);
+      }
+      return;
+    }
+  }
+  product_staged<T, S, AKC, BKC>(acc, smem, a, b, K);
+  store_tile<S>(TO{}, acc, smem, out, ld, rows, cols);
 }
 
 // The rows' product.  TO: type of the result, F32 for slices of the summed index.
@@ -539,15 +577,18 @@ __global__ __launch_bounds__(256, S::kWaves) void k_rows_staged(const ExpertArgs
   const char* w = A.b + (K > 0 ? g.e * A.stride_b : 0) * T::kBytes;
   const Source b = TRANS ? Source{w + (c0 * A.ldb + k0) * T::kBytes, A.ldb, cols, A.n - c0}
                          : Source{w + (k0 * A.ldb + c0) * T::kBytes, A.ldb, cols, A.k - k0};
-  f32x4_t acc[S::FM][S::FN];
-  product_tile<T, S, true, TRANS>(acc, smem, a, b, K);
-  store_tile<S>(TO{}, acc, smem, A.out + (sl.z * A.slice_out + g.first * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
+  // the smaller tiles' sums are cut into slices (plan_expert_matmul)
+  product_tile<T, TO, S, true, TRANS, S::kParts>(smem, a, b, K, A.out + (sl.z * A.slice_out + g.first * A.ldo + c0) * TO::kBytes,
+                                                 A.ldo, rows, cols);
 }
 
 // The weight gradient: 2048 rows over 4 experts of 2048 x 768, bf16 of odd strides, 21 us,
-// 0.31 PFLOP/s.
+// 0.31 PFLOP/s.  The fp32 64 tile's registers are held to what its five workgroups a compute unit
+// (32 KB of LDS each) leave: the runs of long fp32 sums would take more from every call (4096
+// rows over 16 of 512 x 512, fp32: 27.2 us, 32.1 without the bound; 27080 rows, 10295 of them one
+// expert's, over 63 of 256 x 192: 30.3 evenly, 211 unevenly, 190 in one run).
 template <class T, class TO, class S>
-__global__ __launch_bounds__(256, S::kWaves) void k_wgrad_staged(const ExpertArgs A) {
+__global__ __launch_bounds__(256, T::kBytes == 4 && S::TM == 64 ? 5 : S::kWaves) void k_wgrad_staged(const ExpertArgs A) {
   __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
   const int nI = (A.k + S::TM - 1) / S::TM, nJ = (A.n + S::TN - 1) / S::TN;
   GradTile t;
@@ -556,9 +597,8 @@ __global__ __launch_bounds__(256, S::kWaves) void k_wgrad_staged(const ExpertArg
   const int r0 = at.I * S::TM, c0 = at.J * S::TN, rows = min(S::TM, A.k - r0), cols = min(S::TN, A.n - c0);
   const Source a{A.a + (t.first * A.lda + r0) * T::kBytes, A.lda, rows, A.rows - t.first};
   const Source b{A.b + (t.first * A.ldb + c0) * T::kBytes, A.ldb, cols, A.rows - t.first};
-  f32x4_t acc[S::FM][S::FN];
-  product_tile<T, S, false, false>(acc, smem, a, b, t.K);
-  store_tile<S>(TO{}, acc, smem, A.out + (t.out * A.stride_b + r0 * A.ldo + c0) * TO::kBytes, A.ldo, rows, cols);
+  product_tile<T, TO, S, false, false, true>(smem, a, b, t.K, A.out + (t.out * A.stride_b + r0 * A.ldo + c0) * TO::kBytes,
+                                             A.ldo, rows, cols);
 }
 
 template <class T, class TO, class S>

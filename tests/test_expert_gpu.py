@@ -415,3 +415,43 @@ def test_fp32_results_do_not_depend_on_memory_beside_the_operands(pad):
             view.copy_(kept)
         for (name, f), want in zip(_forms(x, w, dy, ends), ref):
             assert torch.equal(f(), want), (name, rows)
+
+
+def _digits(got, want, K):
+    """The bound of test_long_fp32_sums_keep_their_digits, for sums of more than two of their runs."""
+    off = float((got.double() - want).norm()) / float(want.norm())
+    assert off <= 0.3 * U * (K / 2) ** 0.5, off / (U * (K / 2) ** 0.5)
+
+
+@pytest.mark.parametrize("experts,skew,rows,k,n", [(63, 1.4, 27080, 256, 192), (20, 1.5, 24000, 130, 201),
+                                                   (64, 3.0, 12000, 64, 65), (8, 2.0, 9001, 500, 511)])
+def test_long_fp32_sums_of_uneven_groups_keep_their_digits(experts, skew, rows, k, n):
+    """One group holds far more rows than the groups do on average."""
+    log(f"case: fp32 weight gradient of {rows} rows unevenly over {experts} experts, {k} x {n}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(14)
+    share = [(e + 1.0) ** -skew for e in range(experts)]
+    counts = [int(rows * s / sum(share)) for s in share]
+    counts = counts[1:] + counts[:1]                     # the long one is the last
+    rows = sum(counts)
+    x, dy = _randn(g, (rows, k), "f32"), _randn(g, (rows, n), "f32")
+    dw = tm.expert_wgrad(x, dy, _ends(counts))
+    _check_wgrad(x, dy, counts, "f32", dw)
+    for e, a, b in _bounds(counts):
+        if b - a > 2 * 2816:
+            _digits(dw[e], x[a:b].double().t() @ dy[a:b].double(), b - a)
+    assert max(counts) > 2 * 2816
+
+
+def test_long_fp32_sums_without_parts_keep_their_digits():
+    """Tiles that go back to fp32 products, here for one small value in each row."""
+    log("case: long fp32 sums of values without parts")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(15)
+    rows, K, n = 2048, 9000, 4096
+    x, w = _randn(g, (rows, K), "f32"), _randn(g, (1, K, n), "f32")
+    x[:, 77] = 1.234567e-37
+    want = x.double() @ w[0].double()
+    _digits(tm.expert_matmul(x, w, _ends([rows])), want, K)
+    _digits(tm.expert_matmul(x, w.transpose(1, 2).contiguous(), _ends([rows]), transposed=True), want, K)
+    _digits(tm.expert_wgrad(x.t().contiguous(), w[0], _ends([K]))[0], want, K)
