@@ -324,3 +324,34 @@ def test_gradient_of_logits_of_large_size(rows, vocab, dtype):
     bound = (slope.abs() / TAU)[:, None] * (2 * p * (D + 16 * U)[:, None] + 4 * U * hit)
     _close("grad", grad, want, bound + (2.0 ** -8 if dtype == "bf16" else 2 * U) * (want.abs() + bound) + 1e-38)
     assert (p[2] == 1 / vocab).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(20, 600), (16, 40001)])
+def test_kl_term_of_policies_close_to_each_other(rows, vocab):
+    """q - log q - 1 and 1 - q keep their digits where q is next to 1.
+
+    The gap ref_logp - logp is exact for values this close, taken from the call's own logp.  Below 1 the terms are
+    sums and products of values of one size (alternating ones at most twice their sum): a handful of roundings, and
+    those of the factors kl, weight and of the result, under 16 u in all.  From 1 on the differences are off by
+    the exponential's last bits, 8 u of q + |gap| + 1."""
+    log(f"case: policy loss, KL term of close policies {rows} x {vocab}")
+    s = _inputs(rows, vocab, "f32", seed=16, masked=0.0)
+    s["advantages"].zero_()
+    kw = dict(kl=KL, temperature=TAU)
+    logp = tm.policy_loss(**s, **kw)[1]
+    gaps = torch.tensor([1e-4, -1e-4, 3e-4, -1e-3, 1e-3, 1e-2, -1e-2, 0.1, -0.1, 0.5, -0.5, 0.99, -0.99, 1.2, -1.2, 4.0,
+                         -4.0, 1e-5, 0.0, 2e-2][:rows], device="cuda")
+    s["ref_logp"] = logp + gaps
+    gap = s["ref_logp"].double() - logp.double()
+    m = KL * s["weights"].double()
+    want = m * (torch.special.expm1(gap) - gap)
+    series = gap * gap * (0.5 + gap / 6 + gap ** 2 / 24 + gap ** 3 / 120)   # where 64 bits cancel too
+    want = torch.where(gap.abs() < 1e-2, m * series, want)
+    near = gap.abs() < 1
+    rough = 8 * U * m * (gap.exp() + gap.abs() + 1)
+    slope = tm.policy_loss(**s, **kw)[3]
+    wslope = -m * torch.special.expm1(gap)
+    _close("slope", slope, wslope, torch.where(near, 16 * U * wslope.abs(), rough))
+    loss = torch.stack([tm.policy_loss(**dict(s, weights=torch.where(torch.arange(rows, device="cuda") == r,
+                                                                    s["weights"], 0)), **kw)[0] for r in range(rows)])
+    _close("loss", loss, want, torch.where(near, 16 * U * want, rough))
