@@ -2,9 +2,10 @@
 
 Thin front ends of the entry points in ``_lib`` for training: layer norm,
 products of ragged groups of rows with one matrix per expert, and the clipped
-policy loss with a KL term.  Every arithmetic step runs in the library's
-kernels; this module only keeps what a backward pass reads.  The gradients of
-expert matrices come out stacked, as ``optim.TurboMuon`` takes them.
+policy loss with a KL term.  The arithmetic runs in the library's kernels;
+this module keeps what a backward pass reads and, where expert matrices are of
+another type than the rows, has torch round them.  The gradients of expert
+matrices come out stacked, as ``optim.TurboMuon`` takes them.
 """
 from __future__ import annotations
 
@@ -48,7 +49,11 @@ class _ExpertLinear(torch.autograd.Function):
     def backward(ctx, dy):
         x, wx, ends = ctx.saved_tensors
         dx = _lib.expert_matmul(dy, wx, ends, transposed=True) if ctx.needs_input_grad[0] else None
-        dw = _lib.expert_wgrad(x, dy, ends, dtype=ctx.w_dtype) if ctx.needs_input_grad[1] else None
+        dw = None
+        if ctx.needs_input_grad[1]:
+            # rows' own type or fp32 come from the kernel, any other is its fp32 result rounded
+            direct = ctx.w_dtype if ctx.w_dtype is x.dtype else torch.float32
+            dw = _lib.expert_wgrad(x, dy, ends, dtype=direct).to(ctx.w_dtype)
         return dx, dw, None
 
 
@@ -56,8 +61,9 @@ def expert_linear(x, w, ends):
     """x[i] @ w[e] for the rows of each expert e: x is (rows, k), rows sorted by expert, w is
     (experts, k, n), ends an int32 device vector with the number of rows up to each expert's last.
 
-    w may be fp32 where x is bf16 (the parameters that the optimizer keeps): it is rounded to
-    bf16 for the products, and its gradient comes out in fp32.
+    w may be fp32 where x is bf16 (the parameters that the optimizer keeps): torch rounds it to
+    bf16 for the products, a copy that is kept for the backward pass, and its gradient comes out
+    in fp32.  Any other type of w is taken as x's in the same way, its gradient in its own.
     """
     return _ExpertLinear.apply(x, w, ends)
 

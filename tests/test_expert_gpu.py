@@ -455,3 +455,25 @@ def test_long_fp32_sums_without_parts_keep_their_digits():
     _digits(tm.expert_matmul(x, w, _ends([rows])), want, K)
     _digits(tm.expert_matmul(x, w.transpose(1, 2).contiguous(), _ends([rows]), transposed=True), want, K)
     _digits(tm.expert_wgrad(x.t().contiguous(), w[0], _ends([K]))[0], want, K)
+
+
+@pytest.mark.parametrize("rows,of", [(r, w) for r in ("f32", "bf16") for w in ("bfloat16", "float16", "float32", "float64")])
+def test_matrices_of_another_type(rows, of):
+    """What the forward pass takes, the backward pass gives a gradient for, in the matrices' own type:
+    the product's, rounded once more."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(16)
+    counts, wt = [64, 0, 100], getattr(torch, of)
+    x = _randn(g, (164, 48), rows).requires_grad_()
+    w = (torch.randn((3, 48, 40), generator=g, device="cuda") * 0.1).to(wt).requires_grad_()
+    y = ops.expert_linear(x, w, _ends(counts))
+    _check_rows(x.detach(), w.detach().to(DT[rows]), counts, False, rows, y.detach())
+    y.backward(torch.ones_like(y))
+    assert w.grad.dtype is wt and x.grad.dtype is DT[rows]
+    for e, a, b in _bounds(counts):
+        dy = torch.ones((b - a, 40), dtype=torch.float64, device="cuda")
+        want, terms = x.detach()[a:b].double().t() @ dy, x.detach()[a:b].double().abs().t() @ dy
+        bound = 2 * (b - a) * U * terms
+        eps = {"bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}.get(of, U)
+        assert ((w.grad[e].double() - want).abs() <= bound + eps * (want.abs() + bound) + 2.0 ** -25).all()
+    _check_rows(torch.ones_like(y), w.detach().to(DT[rows]), counts, True, rows, x.grad)
