@@ -234,7 +234,8 @@ tm_status tm_orthogonalize_noalloc(void* X, int64_t m, int64_t n, int64_t batch,
  * partial sums in a workspace of their own per (device, stream), which grows
  * and is captured like the orthogonalizer's.  Every result is the same on
  * every run (no float atomics); the order of a sum, and so the last bits, may
- * differ with the sizes, strides and alignment of a call.  NaN and Inf
+ * differ with the sizes, strides and alignment of a call (fp32 expert products:
+ * and with the values of the rows and columns next to it).  NaN and Inf
  * propagate, but never out of rows that take no part.
  */
 #define TM_DTYPE_BF16 0
@@ -284,7 +285,12 @@ tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
  * are formed of three bf16 parts of each operand on the matrix cores and are as
  * exact as a sum of fp32 products; tiles with values that three parts do not hold
  * exactly (NaN, Inf, values that round past the largest bf16, values below about
- * 2^-110) or with results that are not finite take fp32 products.
+ * 2^-110) or with results that are not finite take fp32 products, at less than
+ * half the speed.
+ * Workspace: a call whose summed index is cut into slices keeps a result in fp32
+ * (rows x n) of each: calls of few tiles, up to 64 slices, and fp32 calls of few
+ * tiles or up to 64 rows an expert, ceil(k / 2816) at least.  That is at most 100 MB
+ * or a twentieth of the matrices.
  */
 tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t stride_w,
                            const int32_t* ends, void* y, int64_t ldy, int64_t rows, int64_t experts,
@@ -296,7 +302,8 @@ tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
  *   x, dy      rows x k and rows x n of type `dtype`.
  *   dw         matrix e starts at dw + e stride_dw, row stride lddw; of type
  *              `out_dtype`: fp32, or bf16 where the rows are.
- * Sums as in tm_expert_matmul.
+ * Sums as in tm_expert_matmul.  Workspace: calls of few tiles keep a matrix in
+ * fp32 (k x n) for every chunk of 256 rows or more that an expert's are cut into.
  */
 tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* ends,
                           void* dw, int64_t lddw, int64_t stride_dw, int64_t rows, int64_t experts,

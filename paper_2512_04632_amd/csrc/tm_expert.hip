@@ -121,7 +121,9 @@ using namespace expert;
 // gradient's tile works as long as its group is: the 64 tile up to 64 rows (4096
 // rows over 64 experts of 2048 x 1408, even and uneven groups: 86 and 97, 102 and 105 on 128,
 // 120 and 122 on 256; 80 rows each: 111 and 110, 108 and 109 on 128), the 128 tile below
-// 128 rows (112 each: 118 and 115, 126 and 127 on 256; 160: 142 and 144 against 128 and 130)
+// 128 rows (the same experts with 120 rows each, 114 and 114, 120 and 116 on 256; 128: 112 and
+// 141, 119 and 119; 144: 135 and 141, 121 and 119; transposed 120: 100 and 121, 98 and 127; 128: 102
+// and 122, 99 and 128; 144: 136 and 138, 100 and 127; 40 of 2048 x 2048 are even to 5% from 136 on)
 // and for weight gradients up to 256 (128 each: 154 and 164, 156 and 196 on 256; 512 each of
 // 2048 x 2048: 116 and 125 against 94 and 146).
 int choose_tile(bool staged, bool f32, bool wgrad, const uint64_t (&tiles)[3], uint64_t K, uint64_t mean) {
@@ -140,10 +142,11 @@ uint64_t fewest(bool f32) { return f32 ? 256 : 512; }
 // 112 in one; fp32 450, 538; of 4098 x 2048, bf16, 60 against 54).
 //
 // An fp32 sum is no longer than kLongest values in one run of the fp32 instructions,
-// whose error grows with the root of the number of roundings (464 rows over 55
-// experts, 461 sums of 7770 each: 1.6e-6 of the result and 163 us whole, 8e-7 and 180
-// us in three; 400 over 10 of 5200 x 5000: 1.3e-6 and 392, 7e-7 and 396 in two).  The
-// 128 tile adds 32 products at a time, and its error is below that.
+// whose error grows with the root of the number of roundings (464 rows over 55 experts of
+// 7770 x 461: 1.1e-6 of the result and 170 us with runs of 5632, 9.1e-7 and 172 of 2816,
+// 6.5e-7 and 177 of 1408; 400 over 10 of 5200 x 5000: 1.3e-6 and 363, 9.1e-7 and 367, 6.5e-7
+// and 367; 2000 over 20 of 7770 x 461: 1.1e-6 and 256, 9.1e-7 and 221, 6.4e-7 and 224): the
+// slices keep as much memory as that many results.  The 128 tile adds 32 products at a time, and its error is below that.
 //
 // Groups of up to 24 rows on average are bound by the reading of their matrices
 // and take the staged tiles of 16 or 32 rows, whatever the type and alignment (63
@@ -152,9 +155,8 @@ uint64_t fewest(bool f32) { return f32 ? 256 : 512; }
 // larger groups of an uneven call should not need two tiles); 16 rows up to 8 on average
 // and for a call of no more than 16 (13 rows of 2356 x 6568, fp32: 23, 30 on 32 rows;
 // 48 over 8 of 2048 x 4096: 35, 37; 192 over 16: 68 against 64), in slices
-// of 512 values and more (24 rows over 8 of 768 x 2048, bf16 and fp32: 6.5 and 12.3, 9.2 and
-// 16.2 from 256 on).  fp32 and odd
-// operands stay with 32 rows up to 64 (105 rows over 2 of 4869 x 5632, odd: 47, 51 on
+// of 512 values and more (24 rows over 8 of 768 x 2048, bf16 and fp32: 8.0 and 11.7, 10.7 and
+// 16.1 from 256 on).  fp32 and odd operands stay with 32 rows up to 64 (105 rows over 2 of 4869 x 5632, odd: 47, 51 on
 // the 64 tile).
 ExpertPlan plan_expert_matmul(const ExpertArgs& A, bool f32, bool transposed) {
   const bool staged = f32 || !(whole(A.a, A.lda, A.k) && whole(A.b, A.ldb, transposed ? A.k : A.n) &&

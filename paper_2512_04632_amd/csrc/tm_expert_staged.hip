@@ -27,19 +27,20 @@
 // A product is hi hi + hi mid + mid hi + mid mid + hi lo + lo hi in one fp32 accumulator,
 // small terms first; mid lo, lo mid and lo lo, at most 2^-23 of it, are left out.  Six
 // bf16 instructions take 96 clocks where the eight of fp32 for the same 32 values
-// take 256 (16384 rows over 8 experts of 2048 x 2048: 0.80 ms, 172 TFLOP/s, against 1.03 ms
-// of fp32 instructions).  A tile with a value that three parts do not hold exactly (NaN,
+// take 256 (16384 rows over 8 experts of 2048 x 2048: 0.75-0.80 ms, 172-184 TFLOP/s, against
+// 1.03 ms of fp32 instructions).  A tile with a value that three parts do not hold exactly (NaN,
 // infinities, the few that round to one, those below about 2^-110 whose last bits lie below
 // the smallest bf16) or with a result that is not finite is done again with fp32
-// instructions.  On the smaller tiles the splitting costs what the
+// instructions (where every tile is: 1.74 ms).  On the smaller tiles the splitting costs what the
 // instructions save (2048 rows of 1024 x 1024: 45 us, 40 without; 80 rows over 5 experts
 // of 7960 x 1970: 111 against 95), and fp32 multiplies as it is.
 //
 // Rows that only fill a tile cost as much as real ones: groups of a few rows take
 // tiles of 16 or 32 rows, which are bound by the reading of the matrices: 24 rows over
-// 8 experts of 768 x 2048 bf16 6.5 us of kernel, 3.9 TB/s; 192 rows over 16 of 2048 x 4096
-// 64 us, 4.2 TB/s.  The larger tiles are bound by their fp32 instructions (3001 rows
-// over 5 of 515 x 777 fp32: 33.6 us, 71 TFLOP/s of 153) or, for bf16 of odd strides, by
+// 8 experts of 768 x 2048 bf16 8.0 us a call, 3.1 TB/s (9.6 where the matrices of thirty calls
+// in turn come from HBM; 8.5 in the kernel under the tracer); 192 rows over 16 of
+// 2048 x 4096 64 us, 4.2 TB/s.  The larger tiles are bound by their fp32 instructions (3001 rows
+// over 5 of 515 x 777 fp32: 33.8 us, 71 TFLOP/s of 153) or, for bf16 of odd strides, by
 // the way through the registers (2048 rows of 2049 x 2048: 36 us, 0.48 PFLOP/s).
 #include "tm_elem.h"
 #include "tm_expert.h"

@@ -240,8 +240,8 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
 
 // Rows wider than a workgroup's registers (kNormMaxFused): one workgroup of
 // 1024 threads per row, which reads the row once for each sum and once for the
-// result (the later passes find it in a cache).  Bound by the cache's rate: 4096 x
-// 20000 bf16 313 us, 1.05 TB/s of what has to move.
+// result (the later passes find it in a cache).  4096 x 20000 bf16 313 us, 1.05 TB/s of
+// what has to move: three passes, and loops that fetch weight and bias an element at a time.
 constexpr int kWide = 1024;
 
 template <class T, class F>

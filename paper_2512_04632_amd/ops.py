@@ -89,6 +89,9 @@ class _PolicyLoss(torch.autograd.Function):
 def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low: float = 0.2,
                 clip_high: float = 0.2, kl: float = 0.0, temperature: float = 1.0):
     """(loss, logp) of the clipped policy loss (see _lib.policy_loss); only the logits are
-    differentiated, logp is what the next step keeps as old_logp."""
+    differentiated, logp is what the next step keeps as old_logp.
+
+    The gradient takes its probabilities from the row's lse in fp32 and carries its rounding, 2^-24
+    of it; for logits of large size use _lib.policy_loss_with_grad, which does not."""
     return _PolicyLoss.apply(logits, targets, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl,
                              temperature)
