@@ -2,12 +2,14 @@
 
     python examples/expert_policy.py [--steps 20]
 
-Per step: layer norm, a router (torch), the experts' two products around a
-squared ReLU, layer norm, logits, the clipped policy loss with its KL term,
-the backward pass, and one step of TurboMuon on the experts' matrices and the
-head (the vectors, the embedding and the router go to SGD).  The task is a toy
-one: the advantage of a sampled token is 1 where it is the successor of the
-token before it, -1 otherwise, so the share of right tokens has to rise.
+Per step: layer norm, scores (torch), the routing of every row to two experts with its
+balance loss, the rows' way to their experts, the experts' two products around a squared
+ReLU, the way back onto the residual stream, root-mean-square norm, logits, the log
+probabilities of the sampled tokens, the clipped policy loss with its KL term, the
+backward pass, and one step of TurboMuon on the experts' matrices and the head (the
+vectors, the embedding and the router go to SGD).  The task is a toy one: the advantage
+of a sampled token is 1 where it is the successor of the token before it, -1 otherwise,
+so the share of right tokens has to rise.
 """
 import argparse
 import os
@@ -29,7 +31,7 @@ class ExpertPolicy(torch.nn.Module):
 
         self.embed = param(vocab, dim, scale=1.0)
         self.norm_in = torch.nn.ParameterList([torch.ones(dim), torch.zeros(dim)])
-        self.norm_out = torch.nn.ParameterList([torch.ones(dim), torch.zeros(dim)])
+        self.norm_out = torch.nn.Parameter(torch.ones(dim))
         self.router = param(dim, experts, scale=dim ** -0.5)
         self.up = param(experts, dim, hidden, scale=dim ** -0.5)
         self.down = param(experts, hidden, dim, scale=hidden ** -0.5)
@@ -39,21 +41,19 @@ class ExpertPolicy(torch.nn.Module):
         return [self.up, self.down, self.head]
 
     def vectors(self):
-        return [self.embed, self.router, *self.norm_in, *self.norm_out]
+        return [self.embed, self.router, *self.norm_in, self.norm_out]
 
     def forward(self, tokens):
+        """(logits, balance loss)"""
         x = self.embed[tokens].bfloat16()
         h = ops.layer_norm(x, *self.norm_in)
-        share, expert = (h.float() @ self.router).softmax(-1).max(-1)
-        order = expert.argsort(stable=True)
-        ends = torch.bincount(expert, minlength=self.up.shape[0]).cumsum(0).to(torch.int32)
-        a = ops.expert_linear(h[order], self.up, ends)
+        weights, balance, _, slots, ends = ops.expert_route(h.float() @ self.router, top=2)
+        a = ops.expert_linear(ops.expert_gather(h, slots, ends), self.up, ends)
         y = ops.expert_linear(a.relu().square(), self.down, ends)
-        back = torch.empty_like(order).scatter_(0, order, torch.arange(len(order), device=order.device))
-        x = x + y[back] * share[:, None].bfloat16()
-        h = ops.layer_norm(x, *self.norm_out)
+        x = ops.expert_combine(y, slots, weights, x, ends)
+        h = ops.rms_norm(x, self.norm_out)
         everyone = torch.full((1,), len(tokens), dtype=torch.int32, device=tokens.device)
-        return ops.expert_linear(h, self.head, everyone)   # one matrix for every row
+        return ops.expert_linear(h, self.head, everyone), balance   # one matrix for every row
 
 
 def train(steps=20, rows=4096, vocab=512, seed=0, say=print):
@@ -66,20 +66,21 @@ def train(steps=20, rows=4096, vocab=512, seed=0, say=print):
     for step in range(steps):
         tokens = torch.randint(vocab, (rows,), device="cuda")
         with torch.no_grad():
-            logits = policy(tokens).float()
+            logits = policy(tokens)[0]
             # half of the samples are the wanted token, as from a replayed good answer
-            sampled = torch.multinomial(logits.softmax(-1), 1)[:, 0]
+            sampled = torch.multinomial(logits.float().softmax(-1), 1)[:, 0]
             wanted = (tokens + 1) % vocab
             taken = torch.where(torch.rand(rows, device="cuda") < 0.5, wanted, sampled)
-            old = logits.log_softmax(-1).gather(-1, taken[:, None])[:, 0]
+            old, _ = ops.token_logp(logits, taken)
         advantage = torch.where(taken == wanted, 1.0, -1.0)
         weights = torch.full((rows,), 1.0 / rows, device="cuda")
         right.append(float((sampled == wanted).float().mean()))
         for _ in range(2):   # two updates on the same samples, so that ratios leave one
             muon.zero_grad()
             sgd.zero_grad()
-            loss, _ = ops.policy_loss(policy(tokens), taken, old, advantage, weights, ref_logp=old, kl=0.01)
-            loss.backward()
+            logits, balance = policy(tokens)
+            loss, _ = ops.policy_loss(logits, taken, old, advantage, weights, ref_logp=old, kl=0.01)
+            (loss + 0.01 * balance).backward()
             muon.step()
             sgd.step()
         say(f"step {step:3d}  loss {float(loss.detach()):+.4f}  right {right[-1]:.3f}")

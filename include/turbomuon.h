@@ -223,10 +223,12 @@ tm_status tm_orthogonalize_noalloc(void* X, int64_t m, int64_t n, int64_t batch,
                                    const float* coeffs, int precond, void* stream);
 
 /* ------------------------------------------------------------------ operators
- * What a training step needs around the optimizer: layer norm, products of
- * ragged groups of rows with one matrix per expert (whose weight gradients are
- * the matrices that tm_muon_step_grouped takes) and the clipped policy loss
- * with its gradient.  Matrices are row-major with a stride between rows (in
+ * What a training step needs around the optimizer: layer norm and
+ * root-mean-square norm, the routing of rows to experts, rows on their way to
+ * the experts' order and back, products of ragged groups of rows with one
+ * matrix per expert (whose weight gradients are the matrices that
+ * tm_muon_step_grouped takes), the log probabilities of given tokens and the
+ * clipped policy loss, with their gradients.  Matrices are row-major with a stride between rows (in
  * elements, at least the width); pointers are aligned to their element only,
  * though 16-byte alignment and strides are faster.  `dtype` is the type of the
  * activations; parameters, statistics and sums are fp32.  Streams, errors,
@@ -243,6 +245,7 @@ tm_status tm_orthogonalize_noalloc(void* X, int64_t m, int64_t n, int64_t batch,
 #define TM_MAX_ROWS    1073741824  /* rows of an operator */
 #define TM_MAX_EXPERTS 8192
 #define TM_MAX_VOCAB   1073741824
+#define TM_MAX_TOP     64          /* experts of a row, alternatives of a token */
 
 /*
  * tm_layer_norm - per row of d elements
@@ -268,6 +271,110 @@ tm_status tm_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
                                  const float* weight, const float* mean, const float* rstd, void* dx,
                                  int64_t lddx, float* dweight, float* dbias, int64_t rows, int64_t d,
                                  int dtype, void* stream);
+
+/*
+ * tm_rms_norm - per row of d elements
+ *   s = x + residual (rounded to the type), or x without a residual,
+ *   rstd = 1 / sqrt(sum s^2 / d + eps),  y = s rstd weight.
+ *   residual  rows x d, or NULL.
+ *   weight    d floats, or NULL (ones).
+ *   sum       rows x d: s, written where there is a residual, else ignored.
+ *   rstd      rows floats, written.
+ *   sum and y may be x or the residual (same stride), not each other.  Squares
+ *   are summed in fp32: a row with values of 1e19 and more gives zeros.
+ */
+tm_status tm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                      void* sum, int64_t lds, void* y, int64_t ldy, float* rstd, int64_t rows, int64_t d,
+                      float eps, int dtype, void* stream);
+
+/*
+ * tm_rms_norm_backward (W) - with h = s rstd and g = dy weight
+ *   ds = rstd (g - h sum(g h) / d) + dsum,  dweight = sum over rows of dy h.
+ *   s        what was normalised: tm_rms_norm's sum, or its x.
+ *   dsum     rows x d, the gradient that reaches s by another way, or NULL.
+ *   ds       gradient of x and, the same, of the residual.
+ *   dweight  d floats, written in full (zeros for no rows), or NULL.
+ *   ds may be dy, s or dsum (same stride).
+ */
+tm_status tm_rms_norm_backward(const void* dy, int64_t lddy, const void* s, int64_t lds, const float* weight,
+                               const float* rstd, const void* dsum, int64_t lddsum, void* ds, int64_t ldds,
+                               float* dweight, int64_t rows, int64_t d, int dtype, void* stream);
+
+/*
+ * tm_expert_route (W) - the `top` experts of each row, by its scores l.  With
+ * p = softmax(l) over the experts and N rows that take part:
+ *   chosen   rows x top: the experts of the `top` largest l, largest first; of equal
+ *            ones the lowest index; NaN counts as -inf.
+ *   weights  rows x top: scale p of the chosen, over the sum of the row's chosen p
+ *            if `renormalize`.
+ *   slots    rows x top: where each choice stands in the experts' order (by expert,
+ *            then by row), without gaps from 0.
+ *   ends     `experts` entries: the choices of the experts up to and with each one, as
+ *            tm_expert_matmul takes them.
+ *   balance  one float: experts sum_e (c_e / (top N)) (sum over rows of p_e / N), c_e
+ *            the choices of expert e: 1 where all are alike, 0 if N = 0.
+ *   active   one byte per row, or NULL: rows of 0 take no part; they are not read,
+ *            their choices and slots are -1, their weights 0.
+ *   experts 1..TM_MAX_EXPERTS, top 1..min(experts, TM_MAX_TOP), rows top at most
+ *   TM_MAX_ROWS.  A row of nothing but -inf, or with NaN, has weights of NaN, and so is
+ *   the balance; its choices are experts all the same.
+ */
+tm_status tm_expert_route(const void* logits, int64_t ld, const uint8_t* active, int renormalize, float scale,
+                          int32_t* chosen, float* weights, int32_t* slots, int32_t* ends, float* balance,
+                          int64_t rows, int64_t experts, int64_t top, int dtype, void* stream);
+
+/*
+ * tm_expert_route_backward - gradient by the logits from those of the weights
+ * (dweights, rows x top) and of the balance (dbalance, a device float); NULL: zero.
+ *   chosen, ends  tm_expert_route's; renormalize, scale as there.  A row whose first
+ *                 choice is negative takes no part, its gradient is zero; other
+ *                 choices that are no experts are left out.
+ *   dlogits may be the logits.
+ */
+tm_status tm_expert_route_backward(const void* logits, int64_t ld, const int32_t* chosen, const int32_t* ends,
+                                   const float* dweights, const float* dbalance, int renormalize, float scale,
+                                   void* dlogits, int64_t ldd, int64_t rows, int64_t experts, int64_t top,
+                                   int dtype, void* stream);
+
+/*
+ * tm_expert_gather - out[slots[i, j], :] = x[i, :].
+ *   x      rows x d;  out  count x d, of the same type.
+ *   slots  rows x top.  A slot that is negative, or not below *used, is none.  No two
+ *          may be the same: their row would hold either.
+ *   used   device int32: rows of `out` that are filled (tm_expert_route's last entry of
+ *          ends), or NULL: all.  Rows from there on come out as zeros; one below it
+ *          that no slot names is left as it was.
+ * Whatever slots and *used hold, nothing outside the matrices is read or written.
+ */
+tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, const int32_t* used, void* out,
+                           int64_t ldo, int64_t count, int64_t rows, int64_t top, int64_t d, int dtype,
+                           void* stream);
+
+/*
+ * tm_expert_combine - out[i, :] = residual[i, :] + sum_j weights[i, j] y[slots[i, j], :],
+ * summed in fp32 in the order of j, the residual last, and rounded once.
+ *   y         count x d;  out  rows x d.
+ *   weights   rows x top, or NULL: ones (what the gradient of tm_expert_gather is).
+ *   residual  rows x d, or NULL.
+ *   Slots that are negative or not below count are left out; the same one may be
+ *   named twice.  out may be the residual (same stride).
+ */
+tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
+                            const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count,
+                            int64_t rows, int64_t top, int64_t d, int dtype, void* stream);
+
+/*
+ * tm_expert_combine_backward - dy[slots[i, j], :] = weights[i, j] dout[i, :],
+ * dweights[i, j] = sum over the columns of dout[i, :] y[slots[i, j], :].
+ *   slots, used  as in tm_expert_gather, for dy;  a choice without a slot has a
+ *                gradient of zero.
+ *   dweights     rows x top, or NULL: y is not read then, and may be NULL.
+ *   dy may be y (same stride).
+ */
+tm_status tm_expert_combine_backward(const void* dout, int64_t lddout, const void* y, int64_t ldy,
+                                     const int32_t* slots, const int32_t* used, const float* weights, void* dy,
+                                     int64_t lddy, float* dweights, int64_t count, int64_t rows, int64_t top,
+                                     int64_t d, int dtype, void* stream);
 
 /*
  * tm_expert_matmul (W) - y[i, :] = x[i, :] W[e], e the expert of row i.
@@ -308,6 +415,37 @@ tm_status tm_expert_matmul(const void* x, int64_t ldx, const void* w, int64_t ld
 tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* ends,
                           void* dw, int64_t lddw, int64_t stride_dw, int64_t rows, int64_t experts,
                           int64_t k, int64_t n, int dtype, int out_dtype, void* stream);
+
+/*
+ * tm_token_logp (W) - over rows of logits l with target y, at temperature tau, with
+ * m = max_v l_v and s = sum_v exp((l_v - m) / tau):
+ *   logp     log p_y = (l_y - m) / tau - log s,
+ *   entropy  -sum_v p_v log p_v,
+ *   stats    m and s, two floats per row (what the gradient is taken from),
+ *   top_logp, top_ids  rows x top: the largest log probabilities and their places,
+ *            largest first; of equal logits the lowest place.  -inf and NaN are no
+ *            alternatives: where there are fewer than `top`, -inf and -1.
+ *   targets  int64 per row.  A negative target takes its row out: zeros, places of -1,
+ *            its logits are not read; one of vocab or more makes its logp NaN.
+ *   top      0..min(vocab, TM_MAX_TOP); with 0 top_logp and top_ids may be NULL.
+ * A row of nothing but -inf, or with NaN, gives NaN.
+ */
+tm_status tm_token_logp(const void* logits, int64_t ld, const int64_t* targets, float temperature, float* logp,
+                        float* entropy, float* stats, int64_t top, float* top_logp, int64_t* top_ids,
+                        int64_t rows, int64_t vocab, int dtype, void* stream);
+
+/*
+ * tm_token_logp_backward - with p from stats, g = dlogp and h = dentropy per row (NULL:
+ * zeros)
+ *   dlogits_v = (g ([v = y] - p_v) - h p_v (log p_v + entropy)) / tau.
+ *   stats, entropy  tm_token_logp's on the same logits, targets and temperature.
+ * Rows without a target, or with g = h = 0, are not read, their gradient is zero.
+ * dlogits may be the logits.
+ */
+tm_status tm_token_logp_backward(const void* logits, int64_t ld, const int64_t* targets, const float* stats,
+                                 const float* entropy, const float* dlogp, const float* dentropy,
+                                 float temperature, void* dlogits, int64_t ld_dlogits, int64_t rows,
+                                 int64_t vocab, int dtype, void* stream);
 
 /*
  * tm_policy_loss (W) - clipped policy loss with a KL term over rows of logits
@@ -382,7 +520,16 @@ tm_status tm_release_workspaces(void);
 #define TM_PHASE_EXPERT_WGRAD         16
 #define TM_PHASE_POLICY_LOSS          17
 #define TM_PHASE_POLICY_LOSS_BACKWARD 18
-#define TM_NUM_PHASES         19
+#define TM_PHASE_RMS_NORM             19
+#define TM_PHASE_RMS_NORM_BACKWARD    20
+#define TM_PHASE_EXPERT_ROUTE         21
+#define TM_PHASE_EXPERT_ROUTE_BACKWARD   22
+#define TM_PHASE_EXPERT_GATHER        23
+#define TM_PHASE_EXPERT_COMBINE       24
+#define TM_PHASE_EXPERT_COMBINE_BACKWARD 25
+#define TM_PHASE_TOKEN_LOGP           26
+#define TM_PHASE_TOKEN_LOGP_BACKWARD  27
+#define TM_NUM_PHASES         28
 
 /* Timing hooks (a profiling aid for benchmarks).  While enabled, every kernel
  * launch of later calls is bracketed by a pair of HIP events recorded on the

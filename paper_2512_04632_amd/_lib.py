@@ -25,10 +25,14 @@ PRECOND = {"none": 0, "frobenius": 1, "frob": 1, "aol": 2, "schatten4": 3, "s4":
 PHASES = {"transpose_in": 0, "frob": 1, "gram": 2, "aol_vector": 3, "poly": 4, "update": 5,
           "apply_scale": 6, "copy_out": 7, "load_in": 8, "scale_a": 9, "opt_momentum": 10,
           "opt_apply": 11, "fused": 12, "layer_norm": 13, "layer_norm_backward": 14,
-          "expert_matmul": 15, "expert_wgrad": 16, "policy_loss": 17, "policy_loss_backward": 18}
+          "expert_matmul": 15, "expert_wgrad": 16, "policy_loss": 17, "policy_loss_backward": 18,
+          "rms_norm": 19, "rms_norm_backward": 20, "expert_route": 21, "expert_route_backward": 22,
+          "expert_gather": 23, "expert_combine": 24, "expert_combine_backward": 25,
+          "token_logp": 26, "token_logp_backward": 27}
 DTYPE_BF16, DTYPE_F32 = 0, 1
 TM_MAX_DIM = 65536
 TM_MAX_ITERS = 64
+TM_MAX_TOP = 64
 
 _c_i64p = ctypes.POINTER(ctypes.c_int64)
 _c_fp = ctypes.POINTER(ctypes.c_float)
@@ -68,6 +72,24 @@ _SIGNATURES = {
                                       _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, _vp]),
     "tm_policy_loss_backward": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _f32, _vp, _i64, _i64,
                                                _i64, ctypes.c_int, _vp]),
+    "tm_rms_norm": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _f32,
+                                   ctypes.c_int, _vp]),
+    "tm_rms_norm_backward": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64,
+                                            _i64, ctypes.c_int, _vp]),
+    "tm_expert_route": (ctypes.c_int, [_vp, _i64, _vp, ctypes.c_int, _f32, _vp, _vp, _vp, _vp, _vp, _i64,
+                                       _i64, _i64, ctypes.c_int, _vp]),
+    "tm_expert_route_backward": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, ctypes.c_int, _f32, _vp, _i64,
+                                                _i64, _i64, _i64, ctypes.c_int, _vp]),
+    "tm_expert_gather": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int,
+                                        _vp]),
+    "tm_expert_combine": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64,
+                                         ctypes.c_int, _vp]),
+    "tm_expert_combine_backward": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
+                                                  _i64, _i64, _i64, ctypes.c_int, _vp]),
+    "tm_token_logp": (ctypes.c_int, [_vp, _i64, _vp, _f32, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i64,
+                                     ctypes.c_int, _vp]),
+    "tm_token_logp_backward": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _i64, _i64, _i64,
+                                              ctypes.c_int, _vp]),
     "tm_schedule_tail": (_c_fp, [_c_fp, ctypes.c_int, ctypes.c_int]),
     "tm_workspace_bytes": (ctypes.c_uint64, [_c_i64p, _c_i64p, ctypes.c_int64, ctypes.c_int]),
     "tm_release_workspaces": (ctypes.c_int, []),
@@ -313,7 +335,9 @@ def timing_read(phase: str):
 # The operators around the optimizer live in _operators (which needs torch from its first line
 # on); here they are found by name.
 _OPERATORS = ("layer_norm", "layer_norm_backward", "expert_matmul", "expert_wgrad", "policy_loss",
-              "policy_loss_with_grad", "policy_loss_backward")
+              "policy_loss_with_grad", "policy_loss_backward", "rms_norm", "rms_norm_backward",
+              "expert_route", "expert_route_backward", "expert_gather", "expert_combine",
+              "expert_combine_backward", "token_logp", "token_logp_backward")
 
 
 def __getattr__(name: str):

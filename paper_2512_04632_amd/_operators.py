@@ -14,7 +14,7 @@ import torch
 
 from . import _lib
 
-_BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+_BF16, _F32, _I32, _I64, _BOOL = torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.bool
 _CODE = {_BF16: _lib.DTYPE_BF16, _F32: _lib.DTYPE_F32}
 
 
@@ -263,4 +263,252 @@ def policy_loss_backward(logits, targets, lse, slope, grad=None, temperature: fl
     dlogits = _empty_like(logits)
     _call("tm_policy_loss_backward", index, l2.data_ptr(), ld, targets.data_ptr(),
           lse.data_ptr(), slope.data_ptr(), _ptr(grad), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
+    return dlogits
+
+
+def _like(t, like, name: str):
+    """t checked to be of like's shape, type and device."""
+    if t.shape != like.shape or t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, the type {like.dtype} and the device of "
+                         f"what it goes with, not {tuple(t.shape)}, {t.dtype}, {t.device}")
+    return t
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-5, stream=None):
+    """Root-mean-square norm over the last dimension of s = x + residual (bf16 or fp32).
+
+    weight is an fp32 vector or None; residual has x's shape and type, or is None.  Returns
+    (y, s, rstd): y and s of x's shape and type (s is x itself without a residual, else rounded
+    to the type before it is normalised), rstd fp32, one per row.
+    """
+    if stream is not None:
+        return _on(stream, x, rms_norm, x, weight, residual, eps)
+    code, index = _code(x, "x"), x.get_device()
+    x2, rows, d, ld = _rows(x)
+    if weight is not None:
+        weight = _vector(weight, index, "weight", d, _F32)
+    s, ldr, r2 = x, d, None
+    if residual is not None:
+        r2, _, _, ldr = _rows(_like(residual, x, "residual"))
+        s = _empty_like(x)
+    y = _empty_like(x)
+    rstd = x.new_empty_strided((rows,), (1,), dtype=_F32)
+    _call("tm_rms_norm", index, x2.data_ptr(), ld, _ptr(r2), ldr, _ptr(weight), None if r2 is None else s.data_ptr(), d,
+          y.data_ptr(), d, rstd.data_ptr(), rows, d, eps, code)
+    return y, s, rstd
+
+
+def rms_norm_backward(dy, s, rstd, weight=None, dsum=None, param_grads: bool = True, stream=None):
+    """Gradients of rms_norm: (ds, dweight).  s and rstd are rms_norm's; dy and dsum (the gradient that
+    reaches s by another way, or None) have s's shape and type.  ds is the gradient of x and of the
+    residual; dweight is fp32, or None without param_grads."""
+    if stream is not None:
+        return _on(stream, s, rms_norm_backward, dy, s, rstd, weight, dsum, param_grads)
+    code, index = _code(s, "s"), s.get_device()
+    s2, rows, d, lds = _rows(s)
+    dy2, _, _, lddy = _rows(_like(dy, s, "dy"))
+    a2, lda = None, d
+    if dsum is not None:
+        a2, _, _, lda = _rows(_like(dsum, s, "dsum"))
+    rstd = _vector(rstd, index, "rstd", rows, _F32)
+    if weight is not None:
+        weight = _vector(weight, index, "weight", d, _F32)
+    ds = _empty_like(s)
+    dweight = s.new_empty_strided((d,), (1,), dtype=_F32) if param_grads else None
+    _call("tm_rms_norm_backward", index, dy2.data_ptr(), lddy, s2.data_ptr(), lds, _ptr(weight), rstd.data_ptr(),
+          _ptr(a2), lda, ds.data_ptr(), d, _ptr(dweight), rows, d, code)
+    return ds, dweight
+
+
+def _table(t, index: int, name: str, rows, top, dtype):
+    """A companion of `top` entries per row on device `index`, contiguous."""
+    if t.dim() != 2 or t.dtype is not dtype or t.get_device() != index or t.shape[0] != rows or \
+            (top is not None and t.shape[1] != top):
+        raise ValueError(f"{name} must be a {dtype} matrix of {rows} rows of {'the choices' if top is None else top} on "
+                         f"cuda:{index}, not a {t.dtype} tensor of shape {tuple(t.shape)} on {t.device}")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def expert_route(logits, top: int, active=None, renormalize: bool = True, scale: float = 1.0, stream=None):
+    """The `top` experts of each row of (rows, experts) scores, bf16 or fp32.
+
+    Returns (chosen, weights, slots, ends, balance): the experts (int32, most likely first, of equal
+    scores the lowest), their weights (fp32: scale times the softmax, over the sum of the chosen ones
+    with renormalize), where each choice stands among the rows sorted by expert (int32), the int32
+    ends that expert_matmul takes, and the balance loss (an fp32 scalar, 1 where all experts are
+    used alike).  Rows where the bool vector `active` is False take no part: their choices and slots
+    are -1, their weights 0.
+    """
+    if stream is not None:
+        return _on(stream, logits, expert_route, logits, top, active, renormalize, scale)
+    code, index = _code(logits, "logits"), logits.get_device()
+    if logits.dim() != 2:
+        raise ValueError("logits must be (rows, experts)")
+    l2, rows, experts, ld = _rows(logits)
+    if active is not None:
+        active = _vector(active, index, "active", rows, _BOOL)
+    held = min(max(top, 0), _lib.TM_MAX_TOP)   # any other is refused below
+    chosen = logits.new_empty_strided((rows, held), (held, 1), dtype=_I32)
+    slots = torch.empty_like(chosen)
+    weights = logits.new_empty_strided(chosen.shape, chosen.stride(), dtype=_F32)
+    ends = logits.new_empty_strided((experts,), (1,), dtype=_I32)
+    balance = logits.new_empty_strided((), (), dtype=_F32)
+    _call("tm_expert_route", index, l2.data_ptr(), ld, _ptr(active), 1 if renormalize else 0, scale, chosen.data_ptr(),
+          weights.data_ptr(), slots.data_ptr(), ends.data_ptr(), balance.data_ptr(), rows, experts, top, code)
+    return chosen, weights, slots, ends, balance
+
+
+def expert_route_backward(logits, chosen, ends, dweights=None, dbalance=None, renormalize: bool = True,
+                          scale: float = 1.0, stream=None):
+    """Gradient by the logits from those of expert_route's weights (fp32, of chosen's shape, or None)
+    and of its balance loss (an fp32 scalar on the device, or None).  chosen and ends are expert_route's."""
+    if stream is not None:
+        return _on(stream, logits, expert_route_backward, logits, chosen, ends, dweights, dbalance, renormalize, scale)
+    code, index = _code(logits, "logits"), logits.get_device()
+    if logits.dim() != 2:
+        raise ValueError("logits must be (rows, experts)")
+    l2, rows, experts, ld = _rows(logits)
+    chosen = _table(chosen, index, "chosen", rows, None, _I32)
+    ends = _vector(ends, index, "ends", experts, _I32)
+    if dweights is not None:
+        dweights = _table(dweights, index, "dweights", rows, chosen.shape[1], _F32)
+    if dbalance is not None and (dbalance.dim() != 0 or dbalance.dtype is not _F32 or dbalance.get_device() != index):
+        raise ValueError("dbalance must be an fp32 scalar on the logits' device")
+    dlogits = _empty_like(logits)
+    _call("tm_expert_route_backward", index, l2.data_ptr(), ld, chosen.data_ptr(), ends.data_ptr(), _ptr(dweights),
+          _ptr(dbalance), 1 if renormalize else 0, scale, dlogits.data_ptr(), experts, rows, experts, chosen.shape[1],
+          code)
+    return dlogits
+
+
+def _used(ends, index: int):
+    """Address of the last of the experts' ends: how many rows are filled (None: all)."""
+    if ends is None:
+        return None
+    ends = _ends(ends, index)
+    if ends.shape[0] < 1:
+        raise ValueError("ends must hold one entry per expert")
+    return ends.data_ptr() + 4 * (ends.shape[0] - 1)
+
+
+def _matrix(t, name: str):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix of rows")
+    return _rows(t)
+
+
+def expert_gather(x, slots, ends=None, stream=None):
+    """The rows of x (rows, d) in the experts' order: out[slots[i, j]] = x[i], of rows times top rows.
+
+    slots and ends are expert_route's; slots that are negative, or not below ends[-1], are none, and
+    the rows from ends[-1] on come out as zeros (ends None: every row has its slot).
+    """
+    if stream is not None:
+        return _on(stream, x, expert_gather, x, slots, ends)
+    code, index = _code(x, "x"), x.get_device()
+    x2, rows, d, ldx = _matrix(x, "x")
+    slots = _table(slots, index, "slots", rows, None, _I32)
+    top = slots.shape[1]
+    out = x.new_empty_strided((rows * top, d), (d, 1))
+    _call("tm_expert_gather", index, x2.data_ptr(), ldx, slots.data_ptr(), _used(ends, index), out.data_ptr(), d,
+          rows * top, rows, top, d, code)
+    return out
+
+
+def expert_combine(y, slots, weights=None, residual=None, stream=None):
+    """out[i] = residual[i] + sum over j of weights[i, j] y[slots[i, j]], summed in fp32.
+
+    y is (count, d), bf16 or fp32; slots int32 and weights fp32 (None: ones) are (rows, top);
+    residual is (rows, d) of y's type, or None.  Slots that are negative or past y are left out.
+    """
+    if stream is not None:
+        return _on(stream, y, expert_combine, y, slots, weights, residual)
+    code, index = _code(y, "y"), y.get_device()
+    y2, count, d, ldy = _matrix(y, "y")
+    if slots.dim() != 2:
+        raise ValueError("slots must be (rows, top)")
+    rows, top = slots.shape
+    slots = _table(slots, index, "slots", rows, top, _I32)
+    if weights is not None:
+        weights = _table(weights, index, "weights", rows, top, _F32)
+    r2, ldr = None, d
+    if residual is not None:
+        if residual.shape != (rows, d) or residual.dtype is not y.dtype or residual.get_device() != index:
+            raise ValueError(f"residual must be ({rows}, {d}) of y's type and device")
+        r2, _, _, ldr = _rows(residual)
+    out = y.new_empty_strided((rows, d), (d, 1))
+    _call("tm_expert_combine", index, y2.data_ptr(), ldy, slots.data_ptr(), _ptr(weights), _ptr(r2), ldr,
+          out.data_ptr(), d, count, rows, top, d, code)
+    return out
+
+
+def expert_combine_backward(dout, y, slots, ends=None, weights=None, weight_grads: bool = True, stream=None):
+    """Gradients of expert_combine by y and the weights: (dy, dweights), the second None without
+    weight_grads.  dout is (rows, d) of y's type; ends as for expert_gather.  (The residual's is dout.)"""
+    if stream is not None:
+        return _on(stream, y, expert_combine_backward, dout, y, slots, ends, weights, weight_grads)
+    code, index = _code(y, "y"), y.get_device()
+    y2, count, d, ldy = _matrix(y, "y")
+    g2, rows, dg, ldg = _matrix(dout, "dout")
+    if dg != d or dout.dtype is not y.dtype or dout.get_device() != index:
+        raise ValueError("dout must have y's width, type and device")
+    slots = _table(slots, index, "slots", rows, None, _I32)
+    top = slots.shape[1]
+    if weights is not None:
+        weights = _table(weights, index, "weights", rows, top, _F32)
+    dy = y.new_empty_strided((count, d), (d, 1))
+    dweights = y.new_empty_strided((rows, top), (top, 1), dtype=_F32) if weight_grads else None
+    _call("tm_expert_combine_backward", index, g2.data_ptr(), ldg, y2.data_ptr(), ldy, slots.data_ptr(),
+          _used(ends, index), _ptr(weights), dy.data_ptr(), d, _ptr(dweights), count, rows, top, d, code)
+    return dy, dweights
+
+
+def token_logp(logits, targets, top: int = 0, temperature: float = 1.0, stream=None):
+    """Log probabilities of int64 targets under (rows, vocabulary) logits, bf16 or fp32, at the temperature.
+
+    Returns (logp, entropy, stats, top_logp, top_ids): per row the target's log probability, the
+    entropy, the largest logit with the sum of exponentials about it (what token_logp_backward takes),
+    and the `top` most likely tokens, fp32 log probabilities and int64 places, of equal logits the
+    lowest (None with top 0).  Rows with a negative target take no part: zeros, places of -1.
+    """
+    if stream is not None:
+        return _on(stream, logits, token_logp, logits, targets, top, temperature)
+    code, index = _code(logits, "logits"), logits.get_device()
+    if logits.dim() != 2:
+        raise ValueError("logits must be (rows, vocabulary)")
+    l2, rows, vocab, ld = _rows(logits)
+    targets = _vector(targets, index, "targets", rows, _I64)
+    logp = logits.new_empty_strided((rows,), (1,), dtype=_F32)
+    entropy = torch.empty_like(logp)
+    stats = logits.new_empty_strided((rows, 2), (2, 1), dtype=_F32)
+    top_logp = top_ids = None
+    if top > 0:
+        held = min(top, _lib.TM_MAX_TOP)   # more are refused below
+        top_logp = logits.new_empty_strided((rows, held), (held, 1), dtype=_F32)
+        top_ids = targets.new_empty_strided((rows, held), (held, 1))
+    _call("tm_token_logp", index, l2.data_ptr(), ld, targets.data_ptr(), temperature, logp.data_ptr(),
+          entropy.data_ptr(), stats.data_ptr(), top, _ptr(top_logp), _ptr(top_ids), rows, vocab, code)
+    return logp, entropy, stats, top_logp, top_ids
+
+
+def token_logp_backward(logits, targets, stats, entropy, dlogp=None, dentropy=None, temperature: float = 1.0,
+                        stream=None):
+    """Gradient by the logits from those of token_logp's logp and entropy (fp32 per row, None: zeros);
+    stats and entropy are token_logp's."""
+    if stream is not None:
+        return _on(stream, logits, token_logp_backward, logits, targets, stats, entropy, dlogp, dentropy, temperature)
+    code, index = _code(logits, "logits"), logits.get_device()
+    if logits.dim() != 2:
+        raise ValueError("logits must be (rows, vocabulary)")
+    l2, rows, vocab, ld = _rows(logits)
+    targets = _vector(targets, index, "targets", rows, _I64)
+    stats = _table(stats, index, "stats", rows, 2, _F32)
+    entropy = _vector(entropy, index, "entropy", rows, _F32)
+    if dlogp is not None:
+        dlogp = _vector(dlogp, index, "dlogp", rows, _F32)
+    if dentropy is not None:
+        dentropy = _vector(dentropy, index, "dentropy", rows, _F32)
+    dlogits = _empty_like(logits)
+    _call("tm_token_logp_backward", index, l2.data_ptr(), ld, targets.data_ptr(), stats.data_ptr(), entropy.data_ptr(),
+          _ptr(dlogp), _ptr(dentropy), temperature, dlogits.data_ptr(), vocab, rows, vocab, code)
     return dlogits

@@ -52,7 +52,11 @@ def build(verbose: bool = False) -> str:
             (os.path.join(CSRC, "tm_noalloc.hip"), [], "noalloc.o"),
             (os.path.join(CSRC, "tm_small.hip"), [], "k_small.o"),
             (os.path.join(CSRC, "tm_norm.hip"), [], "norm.o"),
+            (os.path.join(CSRC, "tm_rms.hip"), [], "rms.o"),
             (os.path.join(CSRC, "tm_loss.hip"), [], "loss.o"),
+            (os.path.join(CSRC, "tm_logp.hip"), [], "logp.o"),
+            (os.path.join(CSRC, "tm_route.hip"), [], "route.o"),
+            (os.path.join(CSRC, "tm_rows.hip"), [], "rows.o"),
             (os.path.join(CSRC, "tm_expert.hip"), [], "expert.o"),
             (os.path.join(CSRC, "tm_expert_tiles.hip"), [], "expert_tiles.o"),
             (os.path.join(CSRC, "tm_expert_staged.hip"), [], "expert_staged.o"),

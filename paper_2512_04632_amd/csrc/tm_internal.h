@@ -223,7 +223,9 @@ enum Kind { kKindTransposeIn, kKindFrob, kKindGram, kKindAolVector, kKindPoly,
             kKindUpdate, kKindApplyScale, kKindCopyOut, kKindLoadIn, kKindScaleA,
             kKindOptMomentum, kKindOptApply, kKindSmall, kKindLayerNorm,
             kKindLayerNormBackward, kKindExpertMatmul, kKindExpertWgrad, kKindPolicyLoss,
-            kKindPolicyLossBackward, kNumKinds };
+            kKindPolicyLossBackward, kKindRmsNorm, kKindRmsNormBackward, kKindExpertRoute,
+            kKindExpertRouteBackward, kKindExpertGather, kKindExpertCombine,
+            kKindExpertCombineBackward, kKindTokenLogp, kKindTokenLogpBackward, kNumKinds };
 constexpr int kTransposeTile = 64;
 constexpr int kElemBlock = 2048;     // elements per block of the elementwise kernels
 

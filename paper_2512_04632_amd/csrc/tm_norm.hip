@@ -21,60 +21,10 @@
 // 8 us a call below some hundred rows (64 x 768: 4.1 us of kernel).
 #include <algorithm>
 
-#include "tm_elem.h"
-#include "tm_ops.h"
+#include "tm_norm.h"
 
 namespace tmk {
 namespace norm {
-
-using namespace elem;
-
-// Sum of v over the NT threads of a row, in every one of them.  `slot` holds
-// NT / 64 floats and is not used again before another barrier.
-template <int NT, int N>
-__device__ inline void row_sum(float (&v)[N], float* slot) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-  if constexpr (NT > 64) {
-    constexpr int NW = NT / 64;
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) slot[i * NW + (threadIdx.x >> 6)] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) s += slot[i * NW + w];
-      v[i] = s;
-    }
-  }
-}
-
-template <int NT>
-constexpr int block_threads() { return NT < 256 ? 256 : NT; }
-
-template <int NT, int E, class T>
-__device__ inline void load_cols(const float* p, float fill, int t, int d, float* v) {
-#pragma unroll
-  for (int j = 0; j < E / T::W; ++j) {
-    const int c = (j * NT + t) * T::W;
-    if (p != nullptr && c + T::W <= d) {
-#pragma unroll
-      for (int i = 0; i < T::W; i += F32::W) load_vec<F32>(reinterpret_cast<const char*>(p), c + i, d, fill, v + j * T::W + i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < T::W; ++i) v[j * T::W + i] = p != nullptr && c + i < d ? p[c + i] : fill;
-    }
-  }
-}
-
-// This thread's vectors of a row, as stored.
-template <int NT, int V, class T, bool TAIL>
-__device__ inline void load_row(const char* row, int t, int d, u32x4_t (&q)[V]) {
-#pragma unroll
-  for (int j = 0; j < V; ++j) q[j] = load_ahead<T, TAIL>(row, (j * NT + t) * T::W, d);
-}
 
 // Forward.  NT threads a row, E elements each (forward_t); TAIL: rows that end
 // inside a 16-byte vector.  Two sums
@@ -242,15 +192,6 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_norm_backward(const Nor
 // 1024 threads per row, which reads the row once for each sum and once for the
 // result (the later passes find it in a cache).  4096 x 20000 bf16 313 us, 1.05 TB/s of
 // what has to move: three passes, and loops that fetch weight and bias an element at a time.
-constexpr int kWide = 1024;
-
-template <class T, class F>
-__device__ inline void each_vec(int d, F f) {
-  for (int c = threadIdx.x * T::W; c < d; c += kWide * T::W) f(c);
-}
-
-__device__ inline float col(const float* p, float fill, int c, int d) { return p != nullptr && c < d ? p[c] : fill; }
-
 template <class T>
 __global__ __launch_bounds__(kWide) void k_norm_wide(const NormArgs A) {
   __shared__ float slots[2][kWide / 64];
@@ -349,9 +290,9 @@ __global__ __launch_bounds__(256) void k_norm_columns(const NormArgs A, int slic
   part[A.d + c] = ab;
 }
 
-// out[c] = sum of the blocks' partial sums of column c: 32 columns a block, 32
+// out[c] = sum of the blocks' partial sums of column c (`lines` of them a block): 32 columns a block, 32
 // threads each.  Bound by latency: 512 lines of 4096 columns, 16 MB, 4.5 us.
-__global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blocks, int d, float* dweight,
+__global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blocks, int lines, int d, float* dweight,
                                                       float* dbias) {
   float* out = blockIdx.y == 0 ? dweight : dbias;
   if (out == nullptr) return;
@@ -361,7 +302,7 @@ __global__ __launch_bounds__(1024) void k_norm_params(const float* part, int blo
   float s = 0.f;
   if (c < d) {
 #pragma unroll 4
-    for (int b = grp; b < blocks; b += G) s += part[(int64_t(b) * 2 + blockIdx.y) * d + c];
+    for (int b = grp; b < blocks; b += G) s += part[(int64_t(b) * lines + blockIdx.y) * d + c];
   }
   sums[lc][grp] = s;
   __syncthreads();
@@ -460,9 +401,9 @@ hipError_t launch_norm_backward(const NormArgs& A, bool f32, int blocks, hipStre
   return f32 ? norm::backward_t<elem::F32>(A, blocks, st) : norm::backward_t<elem::Bf16>(A, blocks, st);
 }
 
-hipError_t launch_norm_params(const float* part, int blocks, int d, float* dweight, float* dbias,
+hipError_t launch_norm_params(const float* part, int blocks, int lines, int d, float* dweight, float* dbias,
                               hipStream_t st) {
-  hipLaunchKernelGGL(norm::k_norm_params, dim3((d + 31) / 32, 2), dim3(1024), 0, st, part, blocks, d, dweight, dbias);
+  hipLaunchKernelGGL(norm::k_norm_params, dim3((d + 31) / 32, lines), dim3(1024), 0, st, part, blocks, lines, d, dweight, dbias);
   return hipGetLastError();
 }
 

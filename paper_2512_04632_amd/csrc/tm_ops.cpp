@@ -155,9 +155,245 @@ tm_status layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64
     A.part = params ? reinterpret_cast<float*>(ws) : nullptr;
     hipError_t e = hipSuccess;
     if (!empty) e = tmk::launch_norm_backward(A, dtype == TM_DTYPE_F32, blocks, st);
-    if (e == hipSuccess && params) e = tmk::launch_norm_params(A.part, blocks, A.d, dweight, dbias, st);
+    if (e == hipSuccess && params) e = tmk::launch_norm_params(A.part, blocks, 2, A.d, dweight, dbias, st);
     return e;
   });
+}
+
+tm_status rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, void* sum,
+                   int64_t lds, void* y, int64_t ldy, float* rstd, int64_t rows, int64_t d, float eps, int dtype,
+                   void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("d", d, 1, TM_MAX_DIM));
+  if (!(eps >= 0.f)) return refuse(TM_ERR_INVALID_ARG, "eps must not be negative");
+  if (rows == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  const bool res = residual != nullptr;
+  TM_CHECK(check_strides({{"ldx", ldx, d}, {"ldy", ldy, d}}));
+  if (res) TM_CHECK(check_strides({{"ldr", ldr, d}, {"lds", lds, d}}));
+  TM_CHECK(check_pointers({{"x", x, esz, false}, {"residual", residual, esz, true}, {"weight", weight, 4, true},
+                           {"sum", sum, esz, !res}, {"y", y, esz, false}, {"rstd", rstd, 4, false}}));
+  if (res && sum == y) return refuse(TM_ERR_INVALID_ARG, "sum and y are the same array");
+  tmk::RmsArgs A{};
+  A.x = static_cast<const char*>(x);
+  A.residual = static_cast<const char*>(residual);
+  A.sum = static_cast<char*>(sum);
+  A.out = static_cast<char*>(y);
+  A.weight = weight;
+  A.rstd = rstd;
+  A.ldx = ldx;
+  A.ldr = ldr;
+  A.lds = lds;
+  A.ldo = ldy;
+  A.rows = int32_t(rows);
+  A.d = int32_t(d);
+  A.eps = eps;
+  return run_op(TM_PHASE_RMS_NORM, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_rms(A, dtype == TM_DTYPE_F32, st); });
+}
+
+tm_status rms_norm_backward(const void* dy, int64_t lddy, const void* s, int64_t lds, const float* weight,
+                            const float* rstd, const void* dsum, int64_t lddsum, void* ds, int64_t ldds,
+                            float* dweight, int64_t rows, int64_t d, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("d", d, 1, TM_MAX_DIM));
+  const size_t esz = size_of(dtype);
+  const bool empty = rows == 0;
+  if (empty && dweight == nullptr) return TM_OK;
+  if (!empty) TM_CHECK(check_strides({{"lddy", lddy, d}, {"lds", lds, d}, {"ldds", ldds, d}}));
+  if (!empty && dsum != nullptr) TM_CHECK(check_strides({{"lddsum", lddsum, d}}));
+  TM_CHECK(check_pointers({{"dy", dy, esz, empty}, {"s", s, esz, empty}, {"weight", weight, 4, true},
+                           {"rstd", rstd, 4, empty}, {"dsum", dsum, esz, true}, {"ds", ds, esz, empty},
+                           {"dweight", dweight, 4, true}}));
+  tmk::RmsArgs A{};
+  A.x = static_cast<const char*>(s);
+  A.residual = static_cast<const char*>(dsum);
+  A.dy = static_cast<const char*>(dy);
+  A.out = static_cast<char*>(ds);
+  A.weight = weight;
+  A.rstd = const_cast<float*>(rstd);
+  A.ldx = lds;
+  A.ldr = lddsum;
+  A.lddy = lddy;
+  A.ldo = ldds;
+  A.rows = int32_t(rows);
+  A.d = int32_t(d);
+  A.dweight = dweight;
+  const int blocks = tmk::norm_blocks(rows, d, dtype == TM_DTYPE_F32);
+  const bool params = dweight != nullptr && (blocks != 1 || d > tmk::kNormMaxFused);
+  const size_t bytes = params ? size_t(blocks) * size_t(d) * 4u : 0u;
+  return run_op(TM_PHASE_RMS_NORM_BACKWARD, bytes, stream, [&](char* ws, hipStream_t st) {
+    A.part = params ? reinterpret_cast<float*>(ws) : nullptr;
+    hipError_t e = hipSuccess;
+    if (!empty) e = tmk::launch_rms_backward(A, dtype == TM_DTYPE_F32, blocks, st);
+    if (e == hipSuccess && params) e = tmk::launch_norm_params(A.part, blocks, 1, A.d, dweight, nullptr, st);
+    return e;
+  });
+}
+
+tm_status check_route_sizes(int64_t rows, int64_t experts, int64_t top, float scale) {
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("experts", experts, 1, TM_MAX_EXPERTS));
+  TM_CHECK(check_range("top", top, 1, experts < TM_MAX_TOP ? experts : TM_MAX_TOP));
+  TM_CHECK(check_range("rows top", rows * top, 0, TM_MAX_ROWS));
+  if (!(scale - scale == 0.f)) return refuse(TM_ERR_INVALID_ARG, "scale must be finite");
+  return TM_OK;
+}
+
+tm_status expert_route(const void* logits, int64_t ld, const uint8_t* active, int renormalize, float scale,
+                       int32_t* chosen, float* weights, int32_t* slots, int32_t* ends, float* balance,
+                       int64_t rows, int64_t experts, int64_t top, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_route_sizes(rows, experts, top, scale));
+  const size_t esz = size_of(dtype);
+  const bool empty = rows == 0;
+  if (!empty) TM_CHECK(check_strides({{"ld", ld, experts}}));
+  TM_CHECK(check_pointers({{"logits", logits, esz, empty}, {"chosen", chosen, 4, empty}, {"weights", weights, 4, empty},
+                           {"slots", slots, 4, empty}, {"ends", ends, 4, false}, {"balance", balance, 4, false}}));
+  tmk::RouteArgs A{};
+  A.logits = static_cast<const char*>(logits);
+  A.active = active;
+  A.chosen = chosen;
+  A.weights = weights;
+  A.slots = slots;
+  A.ends = ends;
+  A.balance = balance;
+  A.ld = ld;
+  A.rows = int32_t(rows);
+  A.experts = int32_t(experts);
+  A.top = int32_t(top);
+  A.renormalize = renormalize != 0;
+  A.scale = scale;
+  tmk::plan_route(A);
+  // workspace: the blocks' counts and sums of probabilities, lines of whole vectors
+  const uint64_t entries = uint64_t(A.blocks) * ((uint64_t(experts) + 7u) / 8u * 8u);
+  const uint64_t counts = tmk::align256(entries * sizeof(uint16_t));
+  return run_op(TM_PHASE_EXPERT_ROUTE, size_t(counts + entries * sizeof(float)), stream, [&](char* ws, hipStream_t st) {
+    A.counts = reinterpret_cast<uint16_t*>(ws);
+    A.shares = reinterpret_cast<float*>(ws + counts);
+    return tmk::launch_route(A, dtype == TM_DTYPE_F32, st);
+  });
+}
+
+tm_status expert_route_backward(const void* logits, int64_t ld, const int32_t* chosen, const int32_t* ends,
+                                const float* dweights, const float* dbalance, int renormalize, float scale,
+                                void* dlogits, int64_t ldd, int64_t rows, int64_t experts, int64_t top, int dtype,
+                                void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_route_sizes(rows, experts, top, scale));
+  if (rows == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  TM_CHECK(check_strides({{"ld", ld, experts}, {"ldd", ldd, experts}}));
+  TM_CHECK(check_pointers({{"logits", logits, esz, false}, {"chosen", chosen, 4, false}, {"ends", ends, 4, false},
+                           {"dweights", dweights, 4, true}, {"dbalance", dbalance, 4, true},
+                           {"dlogits", dlogits, esz, false}}));
+  tmk::RouteGradArgs A{};
+  A.logits = static_cast<const char*>(logits);
+  A.chosen = chosen;
+  A.ends = ends;
+  A.dweights = dweights;
+  A.dbalance = dbalance;
+  A.dlogits = static_cast<char*>(dlogits);
+  A.ld = ld;
+  A.ldd = ldd;
+  A.rows = int32_t(rows);
+  A.experts = int32_t(experts);
+  A.top = int32_t(top);
+  A.renormalize = renormalize != 0;
+  A.scale = scale;
+  return run_op(TM_PHASE_EXPERT_ROUTE_BACKWARD, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_route_backward(A, dtype == TM_DTYPE_F32, st); });
+}
+
+tm_status check_rows_sizes(int64_t count, int64_t rows, int64_t top, int64_t d) {
+  TM_CHECK(check_range("count", count, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("top", top, 1, TM_MAX_TOP));
+  return check_range("d", d, 1, TM_MAX_DIM);
+}
+
+tmk::RowsArgs rows_args(const int32_t* slots, int64_t count, int64_t rows, int64_t top, int64_t d) {
+  tmk::RowsArgs A{};
+  A.slots = slots;
+  A.count = count;
+  A.rows = int32_t(rows);
+  A.top = int32_t(top);
+  A.d = int32_t(d);
+  return A;
+}
+
+tm_status expert_gather(const void* x, int64_t ldx, const int32_t* slots, const int32_t* used, void* out,
+                        int64_t ldo, int64_t count, int64_t rows, int64_t top, int64_t d, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_rows_sizes(count, rows, top, d));
+  if (count == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  const bool empty = rows == 0;
+  if (!empty) TM_CHECK(check_strides({{"ldx", ldx, d}}));
+  TM_CHECK(check_strides({{"ldo", ldo, d}}));
+  TM_CHECK(check_pointers({{"x", x, esz, empty}, {"slots", slots, 4, empty}, {"used", used, 4, true}, {"out", out, esz, false}}));
+  tmk::RowsArgs A = rows_args(slots, count, rows, top, d);
+  A.x = static_cast<const char*>(x);
+  A.used = used;
+  A.out = static_cast<char*>(out);
+  A.ldx = ldx;
+  A.ldo = ldo;
+  return run_op(TM_PHASE_EXPERT_GATHER, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_gather(A, dtype == TM_DTYPE_F32, st); });
+}
+
+tm_status expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
+                         const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count, int64_t rows,
+                         int64_t top, int64_t d, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_rows_sizes(count, rows, top, d));
+  if (rows == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  if (count > 0) TM_CHECK(check_strides({{"ldy", ldy, d}}));
+  TM_CHECK(check_strides({{"ldo", ldo, d}}));
+  if (residual != nullptr) TM_CHECK(check_strides({{"ldr", ldr, d}}));
+  TM_CHECK(check_pointers({{"y", y, esz, count == 0}, {"slots", slots, 4, false}, {"weights", weights, 4, true},
+                           {"residual", residual, esz, true}, {"out", out, esz, false}}));
+  tmk::RowsArgs A = rows_args(slots, count, rows, top, d);
+  A.x = static_cast<const char*>(residual);
+  A.y = static_cast<const char*>(y);
+  A.weights = weights;
+  A.out = static_cast<char*>(out);
+  A.ldx = ldr;
+  A.ldy = ldy;
+  A.ldo = ldo;
+  return run_op(TM_PHASE_EXPERT_COMBINE, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_combine(A, dtype == TM_DTYPE_F32, st); });
+}
+
+tm_status expert_combine_backward(const void* dout, int64_t lddout, const void* y, int64_t ldy, const int32_t* slots,
+                                  const int32_t* used, const float* weights, void* dy, int64_t lddy, float* dweights,
+                                  int64_t count, int64_t rows, int64_t top, int64_t d, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_rows_sizes(count, rows, top, d));
+  const size_t esz = size_of(dtype);
+  const bool empty = rows == 0, reads = !empty && count > 0 && dweights != nullptr;
+  if (count == 0 && (empty || dweights == nullptr)) return TM_OK;
+  if (!empty) TM_CHECK(check_strides({{"lddout", lddout, d}}));
+  if (reads) TM_CHECK(check_strides({{"ldy", ldy, d}}));
+  if (count > 0) TM_CHECK(check_strides({{"lddy", lddy, d}}));
+  TM_CHECK(check_pointers({{"dout", dout, esz, empty}, {"y", y, esz, !reads}, {"slots", slots, 4, empty},
+                           {"used", used, 4, true}, {"weights", weights, 4, true}, {"dy", dy, esz, count == 0},
+                           {"dweights", dweights, 4, true}}));
+  tmk::RowsArgs A = rows_args(slots, count, rows, top, d);
+  A.x = static_cast<const char*>(dout);
+  A.y = static_cast<const char*>(y);
+  A.used = used;
+  A.weights = weights;
+  A.out = static_cast<char*>(dy);
+  A.dweights = dweights;
+  A.ldx = lddout;
+  A.ldy = ldy;
+  A.ldo = lddy;
+  return run_op(TM_PHASE_EXPERT_COMBINE_BACKWARD, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_combine_backward(A, dtype == TM_DTYPE_F32, st); });
 }
 
 tm_status check_expert_sizes(int64_t rows, int64_t experts, int64_t k, int64_t n) {
@@ -344,6 +580,78 @@ tm_status policy_loss_backward(const void* logits, int64_t ld, const int64_t* ta
                 [&](char*, hipStream_t st) { return tmk::launch_loss_backward(A, dtype == TM_DTYPE_F32, st); });
 }
 
+tm_status token_logp(const void* logits, int64_t ld, const int64_t* targets, float temperature, float* logp,
+                     float* entropy, float* stats, int64_t top, float* top_logp, int64_t* top_ids, int64_t rows,
+                     int64_t vocab, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("vocab", vocab, 1, TM_MAX_VOCAB));
+  TM_CHECK(check_range("top", top, 0, vocab < TM_MAX_TOP ? vocab : TM_MAX_TOP));
+  TM_CHECK(check_temperature(temperature));
+  if (rows == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  TM_CHECK(check_strides({{"ld", ld, vocab}}));
+  TM_CHECK(check_pointers({{"logits", logits, esz, false}, {"targets", targets, 8, false}, {"logp", logp, 4, false},
+                           {"entropy", entropy, 4, false}, {"stats", stats, 8, false},
+                           {"top_logp", top_logp, 4, top == 0}, {"top_ids", top_ids, 8, top == 0}}));
+  tmk::LogpArgs A{};
+  A.logits = static_cast<const char*>(logits);
+  A.targets = targets;
+  A.logp = logp;
+  A.entropy = entropy;
+  A.stats = reinterpret_cast<float2*>(stats);
+  A.top_logp = top_logp;
+  A.top_ids = top_ids;
+  A.ld = ld;
+  A.rows = int32_t(rows);
+  A.vocab = int32_t(vocab);
+  A.top = int32_t(top);
+  A.inv_temp = 1.f / temperature;
+  tmk::plan_logp(A, dtype == TM_DTYPE_F32);
+  TM_CHECK(check_blocks(rows, A.chunks, uint64_t(tmk::logp_threads(A, dtype == TM_DTYPE_F32))));
+  const uint64_t chunks = A.chunks > 1 ? uint64_t(rows) * uint64_t(A.chunks) : 0u;
+  return run_op(TM_PHASE_TOKEN_LOGP, size_t(chunks * (sizeof(float4) + uint64_t(top) * 8u)), stream,
+                [&](char* ws, hipStream_t st) {
+                  A.part = reinterpret_cast<float4*>(ws);
+                  A.keys = reinterpret_cast<uint64_t*>(ws + chunks * sizeof(float4));
+                  return tmk::launch_logp(A, dtype == TM_DTYPE_F32, st);
+                });
+}
+
+tm_status token_logp_backward(const void* logits, int64_t ld, const int64_t* targets, const float* stats,
+                              const float* entropy, const float* dlogp, const float* dentropy, float temperature,
+                              void* dlogits, int64_t ldd, int64_t rows, int64_t vocab, int dtype, void* stream) {
+  TM_CHECK(check_dtype("dtype", dtype));
+  TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
+  TM_CHECK(check_range("vocab", vocab, 1, TM_MAX_VOCAB));
+  TM_CHECK(check_temperature(temperature));
+  if (rows == 0) return TM_OK;
+  const size_t esz = size_of(dtype);
+  TM_CHECK(check_strides({{"ld", ld, vocab}, {"ld_dlogits", ldd, vocab}}));
+  TM_CHECK(check_pointers({{"logits", logits, esz, false}, {"targets", targets, 8, false}, {"stats", stats, 8, false},
+                           {"entropy", entropy, 4, false}, {"dlogp", dlogp, 4, true},
+                           {"dentropy", dentropy, 4, true}, {"dlogits", dlogits, esz, false}}));
+  tmk::LogpArgs A{};
+  A.logits = static_cast<const char*>(logits);
+  A.targets = targets;
+  A.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
+  A.entropy = const_cast<float*>(entropy);
+  A.dlogp = dlogp;
+  A.dentropy = dentropy;
+  A.dlogits = static_cast<char*>(dlogits);
+  A.ld = ld;
+  A.ldd = ldd;
+  A.rows = int32_t(rows);
+  A.vocab = int32_t(vocab);
+  A.inv_temp = 1.f / temperature;
+  const int64_t chunks = (vocab * int64_t(esz) + kGradBytes - 1) / kGradBytes;
+  TM_CHECK(check_blocks(rows, chunks, 256));
+  A.chunks = int32_t(chunks);
+  A.chunk = int32_t(chunk_length(vocab, chunks));
+  return run_op(TM_PHASE_TOKEN_LOGP_BACKWARD, 0, stream,
+                [&](char*, hipStream_t st) { return tmk::launch_logp_backward(A, dtype == TM_DTYPE_F32, st); });
+}
+
 }  // namespace
 
 extern "C" {
@@ -394,6 +702,85 @@ tm_status tm_policy_loss_backward(const void* logits, int64_t ld, const int64_t*
   return guarded([&] {
     return policy_loss_backward(logits, ld, targets, lse, slope, grad, temperature, dlogits, ld_dlogits, rows,
                                 vocab, dtype, stream);
+  });
+}
+
+tm_status tm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                      void* sum, int64_t lds, void* y, int64_t ldy, float* rstd, int64_t rows, int64_t d,
+                      float eps, int dtype, void* stream) {
+  return guarded([&] {
+    return rms_norm(x, ldx, residual, ldr, weight, sum, lds, y, ldy, rstd, rows, d, eps, dtype, stream);
+  });
+}
+
+tm_status tm_rms_norm_backward(const void* dy, int64_t lddy, const void* s, int64_t lds, const float* weight,
+                               const float* rstd, const void* dsum, int64_t lddsum, void* ds, int64_t ldds,
+                               float* dweight, int64_t rows, int64_t d, int dtype, void* stream) {
+  return guarded([&] {
+    return rms_norm_backward(dy, lddy, s, lds, weight, rstd, dsum, lddsum, ds, ldds, dweight, rows, d, dtype,
+                             stream);
+  });
+}
+
+tm_status tm_expert_route(const void* logits, int64_t ld, const uint8_t* active, int renormalize, float scale,
+                          int32_t* chosen, float* weights, int32_t* slots, int32_t* ends, float* balance,
+                          int64_t rows, int64_t experts, int64_t top, int dtype, void* stream) {
+  return guarded([&] {
+    return expert_route(logits, ld, active, renormalize, scale, chosen, weights, slots, ends, balance, rows,
+                        experts, top, dtype, stream);
+  });
+}
+
+tm_status tm_expert_route_backward(const void* logits, int64_t ld, const int32_t* chosen, const int32_t* ends,
+                                   const float* dweights, const float* dbalance, int renormalize, float scale,
+                                   void* dlogits, int64_t ldd, int64_t rows, int64_t experts, int64_t top,
+                                   int dtype, void* stream) {
+  return guarded([&] {
+    return expert_route_backward(logits, ld, chosen, ends, dweights, dbalance, renormalize, scale, dlogits,
+                                 ldd, rows, experts, top, dtype, stream);
+  });
+}
+
+tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, const int32_t* used, void* out,
+                           int64_t ldo, int64_t count, int64_t rows, int64_t top, int64_t d, int dtype,
+                           void* stream) {
+  return guarded([&] { return expert_gather(x, ldx, slots, used, out, ldo, count, rows, top, d, dtype, stream); });
+}
+
+tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
+                            const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count, int64_t rows,
+                            int64_t top, int64_t d, int dtype, void* stream) {
+  return guarded([&] {
+    return expert_combine(y, ldy, slots, weights, residual, ldr, out, ldo, count, rows, top, d, dtype, stream);
+  });
+}
+
+tm_status tm_expert_combine_backward(const void* dout, int64_t lddout, const void* y, int64_t ldy,
+                                     const int32_t* slots, const int32_t* used, const float* weights, void* dy,
+                                     int64_t lddy, float* dweights, int64_t count, int64_t rows, int64_t top,
+                                     int64_t d, int dtype, void* stream) {
+  return guarded([&] {
+    return expert_combine_backward(dout, lddout, y, ldy, slots, used, weights, dy, lddy, dweights, count,
+                                   rows, top, d, dtype, stream);
+  });
+}
+
+tm_status tm_token_logp(const void* logits, int64_t ld, const int64_t* targets, float temperature, float* logp,
+                        float* entropy, float* stats, int64_t top, float* top_logp, int64_t* top_ids, int64_t rows,
+                        int64_t vocab, int dtype, void* stream) {
+  return guarded([&] {
+    return token_logp(logits, ld, targets, temperature, logp, entropy, stats, top, top_logp, top_ids, rows,
+                      vocab, dtype, stream);
+  });
+}
+
+tm_status tm_token_logp_backward(const void* logits, int64_t ld, const int64_t* targets, const float* stats,
+                                 const float* entropy, const float* dlogp, const float* dentropy,
+                                 float temperature, void* dlogits, int64_t ld_dlogits, int64_t rows, int64_t vocab,
+                                 int dtype, void* stream) {
+  return guarded([&] {
+    return token_logp_backward(logits, ld, targets, stats, entropy, dlogp, dentropy, temperature, dlogits,
+                               ld_dlogits, rows, vocab, dtype, stream);
   });
 }
 
