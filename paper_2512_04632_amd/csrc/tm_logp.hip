@@ -38,64 +38,67 @@ constexpr float kFar = -200.f;   // a power of 2 that is zero in fp32
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---------------------------------------------------------------- sums
-// m the maximum, s the sum of e = exp2((l - m) c), t the sum of e (l - m) c.
+// What a thread has seen: `m` the maximum; s the sum of e = exp2((l - at) c) and t that of e (l - at) c, about a value
+// `at` that follows the maximum at a distance: it moves when a logit passes `limit`, where e is 2^kAbove.
+constexpr float kAbove = 24.f;
 struct Sums {
-  float m, s, t;
+  float m = -INFINITY, at = -INFINITY, limit = -INFINITY, s = 0.f, t = 0.f;
 };
-__device__ inline Sums nothing() { return Sums{-INFINITY, 0.f, 0.f}; }
 
-// The sums of `a` about the maximum m.
-__device__ inline void move_to(Sums& a, float m, float c) {
-  const float by = (a.m - m) * c;
-  const float f = a.m == -INFINITY ? 0.f : exp2_fast(by);   // nothing was summed about -inf
+// The sums about another value.
+__device__ inline void move_to(Sums& a, float at, float c) {
+  const float by = (a.at - at) * c;
+  const float f = a.at == -INFINITY ? 0.f : exp2_fast(by);   // nothing was summed about -inf
   a.t = (a.t + a.s * fmaxf(by, kFar)) * f;
   a.s *= f;
-  a.m = m;
+  a.at = at;
 }
 
-__device__ inline Sums join(Sums a, Sums b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  const bool nan = a.s != a.s || b.s != b.s;   // one about -inf would vanish
-  move_to(a, m, c);
-  move_to(b, m, c);
-  return Sums{m, nan ? NAN : a.s + b.s, a.t + b.t};
-}
-
+// The largest of N values; NaN counts as -inf.
 template <int N>
 __device__ inline float largest(const float* v) {
-  float m = v[0];
+  float m = -INFINITY;
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+  for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
   return m;
 }
 
 // Adds N logits whose maximum is m.
 template <int N>
-__device__ inline void add_terms(Sums& a, const float* v, float m, float c) {
-  if (m > a.m) move_to(a, m, c);
-  const float at = a.m == -INFINITY ? 0.f : a.m;   // terms of -inf are exp(-inf - 0) = 0
+__device__ inline void add_terms(Sums& a, const float* v, float m, float c, float above) {
+  a.m = fmaxf(a.m, m);
+  if (m > a.limit) {
+    move_to(a, m, c);
+    a.limit = m + above;
+  }
+  const float at = a.at == -INFINITY ? 0.f : a.at;   // terms of -inf are exp(-inf - 0) = 0
+  float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float u = (v[i] - at) * c, e = exp2_fast(u);
-    a.s += e;
-    a.t += e * fmaxf(u, kFar);
+    s[i % 2] += e;
+    t[i % 2] += e * u;
   }
+  t[0] += t[1];
+  if (t[0] != t[0]) {   // 0 (-inf), which is 0; a value that is not a number shows in s
+    t[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float u = (v[i] - at) * c;
+      t[0] += exp2_fast(u) * fmaxf(u, kFar);
+    }
+  }
+  a.s += s[0] + s[1];
+  a.t += t[0];
 }
 
-__device__ inline Sums wave_join(Sums a, float c) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    Sums b;
-    b.m = __shfl_xor(a.m, o);
-    b.s = __shfl_xor(a.s, o);
-    b.t = __shfl_xor(a.t, o);
-    a = join(a, b, c);
-  }
-  return a;
-}
+// m, and the sums about it.
+struct Joined {
+  float m, s, t;
+};
 
 template <class T>
-__device__ inline void write_row(const LogpArgs& A, int64_t r, int64_t y, Sums a) {
+__device__ inline void write_row(const LogpArgs& A, int64_t r, int64_t y, Joined a) {
   const float log_sum = logf(a.s);
   const float ly = y < A.vocab ? T::load1(A.logits + (r * A.ld + y) * T::kBytes) : NAN;
   A.logp[r] = (ly - a.m) * A.inv_temp - log_sum;
@@ -106,19 +109,20 @@ __device__ inline void write_row(const LogpArgs& A, int64_t r, int64_t y, Sums a
 // ---------------------------------------------------------------- alternatives
 typedef uint64_t Key;
 
-__device__ inline uint32_t ordered(float v) {
-  const uint32_t b = __float_as_uint(v + 0.f);   // -0 and 0 are equal
-  return b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
+// Whole numbers in the order of the floats.
+__device__ inline int ordered(float v) {
+  const int b = __float_as_int(v + 0.f);   // -0 and 0 are equal
+  return b ^ ((b >> 31) & 0x7fffffff);
 }
-__device__ inline float value_of(Key k) {
-  const uint32_t b = uint32_t(k >> 32);
-  return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
-}
+__device__ inline float value_of(int order) { return __int_as_float(order ^ ((order >> 31) & 0x7fffffff)); }
+__device__ inline Key key_of(float v, int place) { return Key(uint32_t(ordered(v)) ^ 0x80000000u) << 32 | uint32_t(~place); }
+__device__ inline float value_of(Key k) { return value_of(int(uint32_t(k >> 32) ^ 0x80000000u)); }
 __device__ inline int place_of(Key k) { return int(~uint32_t(k)); }
-// 0, less than every entry's, for what is no alternative.
-__device__ inline Key key_of(float v, int place) {
-  return v > -INFINITY ? Key(ordered(v)) << 32 | uint32_t(~place) : Key(0);
-}
+
+// That of -inf, for what is not there.
+constexpr Key kNone = Key(0x007fffffu) << 32;
+// Every number but -inf is at least this.
+constexpr float kLowest = -3.402823466e38f;
 
 // LDS of one wave: what one lane has written the others read.
 __device__ inline void wave_sync() {
@@ -127,27 +131,46 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// The maximum over the wave, the same in every lane: as wave_sum, by data-parallel moves.
+__device__ inline int wave_max(int v) {
+  auto step = [&](auto ctrl, auto rows) {
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // row_shr:1, :2, :4, :8
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // row_bcast:15, :31
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 constexpr int kListed = 320;
 struct List {
-  Key keys[kListed], best[64];
+  Key keys[kListed + 8], best[64];
 };
 
-// A wave's picking of the `top` best of the keys that it is given.
+// A wave's picking of the `top` best of the entries that it is given.
 struct Picker {
   List& list;
   int top, n = 0;
-  Key floor = 1;   // keys below it are out
+  Key floor = 0;         // keys below it are out
+  float low = kLowest;   // and so are values below this
 
   __device__ Picker(List& l, int k) : list(l), top(k) {}
 
   // The best `top` of the listed keys, in order.
   __device__ void settle() {
     const int lane = threadIdx.x & 63;
+    if (lane < 8) list.keys[n + lane] = 0;   // whole runs of eight
     wave_sync();
     for (int i = lane; i < n; i += 64) {
       const Key mine = list.keys[i];
       int better = 0;
-      for (int j = 0; j < n; ++j) better += list.keys[j] > mine ? 1 : 0;
+      for (int j = 0; j < n; j += 8)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) better += list.keys[j + u] > mine ? 1 : 0;
       if (better < top) list.best[better] = mine;
     }
     wave_sync();
@@ -156,35 +179,54 @@ struct Picker {
     wave_sync();
     if (n == top) floor = list.keys[top - 1];
   }
-  // One key of each lane (0: none).
-  __device__ void push(Key key) {
-    const bool in = key >= floor;
+  // One entry of each lane (-inf: none).
+  __device__ void push(float v, int place) {
+    bool in = v >= low;
+    if (__ballot(in) == 0) return;
+    const Key key = key_of(v, place);
+    in = in && key >= floor;
     const uint64_t who = __ballot(in);
-    if (who == 0) return;
     const int lane = threadIdx.x & 63;
     if (in) list.keys[n + __popcll(who & ((uint64_t(1) << lane) - 1))] = key;
     n += __popcll(who);
     if (n > kListed - 64) settle();
   }
-  // Raises the floor to the `top`-th best of the lanes' own best keys: of each lane one
-  // entry, and `top` of them reach it.
-  __device__ void start(Key lanes_best) {
-    push(lanes_best);
-    settle();
-    n = 0;
+  // Raises the bound to the `top`-th best of values of which each lane has one (of different entries), where there
+  // are so many: the least value that fewer than `top` are above.
+  __device__ void start(float lanes_best) {
+    float* values = reinterpret_cast<float*>(list.keys);
+    values[threadIdx.x & 63] = lanes_best;
     wave_sync();
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) above += values[i] > lanes_best ? 1 : 0;
+    wave_sync();
+    low = fmaxf(value_of(~wave_max(above < top ? ~ordered(lanes_best) : INT32_MIN)), kLowest);
   }
 };
 
-template <class T>
-__device__ inline void write_top(const LogpArgs& A, int64_t r, const Key* keys, int n, float m, float s) {
+// What was picked of row r, by the lanes of a wave.
+__device__ inline void write_top(const LogpArgs& A, int64_t r, const Picker& pick, Joined row) {
   const int lane = threadIdx.x & 63;
   if (lane < A.top) {
-    const bool there = lane < n;
-    const float v = there ? value_of(keys[lane]) : -INFINITY;
-    A.top_logp[r * A.top + lane] = (v - m) * A.inv_temp - logf(s);
-    A.top_ids[r * A.top + lane] = there ? place_of(keys[lane]) : -1;
+    const bool there = lane < pick.n;
+    const float v = there ? value_of(pick.list.keys[lane]) : -INFINITY;
+    A.top_logp[r * A.top + lane] = (v - row.m) * A.inv_temp - logf(row.s);
+    A.top_ids[r * A.top + lane] = there ? place_of(pick.list.keys[lane]) : -1;
   }
+}
+
+// The same of a whole row, or of chunk `id` for k_logp_join.
+template <class T>
+__device__ inline void write_sums(const LogpArgs& A, int64_t id, int64_t r, int64_t y, Joined row) {
+  if (A.chunks == 1) write_row<T>(A, r, y, row);
+  else A.part[id] = make_float4(row.m, row.s, row.t, 0.f);
+}
+template <class T>
+__device__ inline void write_picked(const LogpArgs& A, int64_t id, int64_t r, const Picker& pick, Joined row) {
+  const int lane = threadIdx.x & 63;
+  if (A.chunks == 1) write_top(A, r, pick, row);
+  else if (lane < A.top) A.keys[id * A.top + lane] = lane < pick.n ? pick.list.keys[lane] : kNone;
 }
 
 // A row that takes no part; `lanes` threads of it.
@@ -216,20 +258,19 @@ __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   float v[K * W];
 #pragma unroll
   for (int j = 0; j < K; ++j) load_vec<T>(l, (j * 64 + lane) * W, n, -INFINITY, v + j * W);
-  Sums a = nothing();
-  add_terms<K * W>(a, v, largest<K * W>(v), c);
-  a = wave_join(a, c);
-  if (lane == 0) write_row<T>(A, r, y, a);
+  const float mine = largest<K * W>(v);
+  Sums a;
+  a.m = value_of(wave_max(ordered(mine)));
+  add_terms<K * W>(a, v, a.m, c, 0.f);
+  const Joined row{a.m, wave_sum(a.s), wave_sum(a.t)};
+  if (lane == 0) write_row<T>(A, r, y, row);
   if constexpr (TOP) {
     Picker pick(lists[threadIdx.x >> 6], A.top);
-    Key best = 0;
+    pick.start(mine);
 #pragma unroll
-    for (int e = 0; e < K * W; ++e) best = max(best, key_of(v[e], ((e / W) * 64 + lane) * W + e % W));
-    pick.start(best);
-#pragma unroll
-    for (int e = 0; e < K * W; ++e) pick.push(key_of(v[e], ((e / W) * 64 + lane) * W + e % W));
+    for (int e = 0; e < K * W; ++e) pick.push(v[e], ((e / W) * 64 + lane) * W + e % W);
     pick.settle();
-    write_top<T>(A, r, pick.list.keys, pick.n, a.m, a.s);
+    write_top(A, r, pick, row);
   }
 }
 
@@ -239,10 +280,8 @@ template <class T>
 constexpr int group_size() { return 16 * T::W; }
 
 // The maximum over 16 neighbouring lanes, in each of them.
-__device__ inline float max16(float v) {
-  auto step = [&](auto ctrl) {
-    v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, false)));
-  };
+__device__ inline int max16(int v) {
+  auto step = [&](auto ctrl) { v = max(v, __builtin_amdgcn_update_dpp(v, v, decltype(ctrl)::value, 0xf, 0xf, true)); };
   step(std::integral_constant<int, 0x128>{});   // row_ror:8, :4, :2, :1
   step(std::integral_constant<int, 0x124>{});
   step(std::integral_constant<int, 0x122>{});
@@ -255,36 +294,52 @@ template <class T>
 __device__ inline void pick_entries(Picker& pick, const float* maxima, const char* l, int first, int last) {
   constexpr int W = T::W, GROUP = group_size<T>();
   const int lane = threadIdx.x & 63, groups = (last - first + GROUP - 1) / GROUP;
-  Key best = 0;
-  for (int g = lane; g < groups; g += 64) best = max(best, key_of(maxima[g], g));
+  float best = -INFINITY;
+  for (int g = lane; g < groups; g += 64) best = fmaxf(best, maxima[g]);
   pick.start(best);
   for (int base = 0; base < groups; base += 64) {
     const int g = base + lane;
-    pick.push(g < groups ? key_of(maxima[g], g) : Key(0));
+    pick.push(g < groups ? maxima[g] : -INFINITY, g);
   }
   pick.settle();
-  // the picked groups, a lane each; their best entries reach the last one's maximum
+  // the picked groups, a lane each
   const int found = pick.n;
   const Key mine = lane < found ? pick.list.keys[lane] : Key(0);
+  const float worst = found > 0 ? value_of(pick.list.keys[found - 1]) : 0.f;
   wave_sync();
-  pick.floor = found == pick.top ? pick.floor >> 32 << 32 : Key(1);
+  pick.floor = 0;
   pick.n = 0;
-  for (int base = 0; base < found; base += 4) {
+  auto read = [&](int base, float* v) __attribute__((always_inline)) {
     const int from = base + (lane >> 4), g = place_of(__shfl((unsigned long long)mine, from & 63));
     const int at = from < found ? first + g * GROUP + (lane & 15) * W : last;
-    float v[W];
     load_vec<T>(l, at, last, -INFINITY, v);
+    return at;
+  };
+  float v[W];
+  if (found == pick.top) {
+    pick.low = worst;   // the groups' best entries reach it
+  } else {
+    pick.low = kLowest;
+    best = -INFINITY;
+    for (int base = 0; base < found; base += 4) {
+      read(base, v);
+      best = fmaxf(best, largest<W>(v));
+    }
+    pick.start(best);
+  }
+  for (int base = 0; base < found; base += 4) {
+    const int at = read(base, v);
 #pragma unroll
-    for (int i = 0; i < W; ++i) pick.push(key_of(v[i], at + i));
+    for (int i = 0; i < W; ++i) pick.push(v[i], at + i);
   }
   pick.settle();
 }
 
-// NT threads for a row, or a chunk of one.
+// NT threads for a row, or a chunk of one.  The next G vectors of a thread are on their way while G are summed.
 template <class T, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void k_logp_rows(const LogpArgs A) {
-  constexpr int W = T::W, STEP = NT * W, G = 4;
-  __shared__ Sums slots[NT / 64];
+  constexpr int W = T::W, STEP = NT * W, G = 4, NW = NT / 64;
+  __shared__ float slots[3][NW];
   __shared__ float maxima[TOP ? kGroups : 1];
   __shared__ List list[1];
   const int64_t r = blockIdx.x / A.chunks;
@@ -293,55 +348,76 @@ __global__ __launch_bounds__(NT) void k_logp_rows(const LogpArgs A) {
     if (A.chunks == 1) write_none(A, r, threadIdx.x);
     return;
   }
+  const int tid = threadIdx.x;
   const int first = int(blockIdx.x - r * A.chunks) * A.chunk, last = min(A.vocab, first + A.chunk);
   const char* l = A.logits + r * A.ld * T::kBytes;
-  const float c = A.inv_temp * kLog2e;
-  Sums a = nothing();
-  auto take = [&](const float* v, int at) __attribute__((always_inline)) {
-    const float m = largest<W>(v);
-    add_terms<W>(a, v, m, c);
-    if constexpr (TOP) {
-      const float g = max16(m);
-      if ((threadIdx.x & 15) == 0 && at < last) maxima[(at - first) / group_size<T>()] = g;
-    }
+  const float c = A.inv_temp * kLog2e, above = kAbove / c;
+  Sums a;
+  u32x4_t q[G];
+  auto load = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) q[g] = T::load(l + int64_t(base + g * STEP + tid * W) * T::kBytes);
   };
   int base = first;
-  for (; base + G * STEP <= last; base += G * STEP) {
-    u32x4_t q[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) q[g] = T::load(l + int64_t(base + g * STEP + int(threadIdx.x) * W) * T::kBytes);
+  bool more = base + G * STEP <= last;
+  if (more) load(base);
+  while (more) {
+    float v[G * W], m[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      float v[W];
-      T::unpack(q[g], v);
-      take(v, base + g * STEP + int(threadIdx.x) * W);
+      T::unpack(q[g], v + g * W);
+      m[g] = largest<W>(v + g * W);
+    }
+    const int at = (base - first) / group_size<T>();
+    base += G * STEP;
+    more = base + G * STEP <= last;
+    if (more) load(base);
+    add_terms<G * W>(a, v, largest<G>(m), c, above);
+    if constexpr (TOP) {
+      int mine = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int best = max16(ordered(m[g]));
+        mine = (tid & 15) == g ? best : mine;
+      }
+      if ((tid & 15) < G) maxima[at + (tid & 15) * (NT / 16) + tid / 16] = value_of(mine);
     }
   }
   for (; base < last; base += STEP) {   // every lane, those past the end with -inf
-    const int at = base + int(threadIdx.x) * W;
+    const int at = base + tid * W;
     float v[W];
     load_vec<T>(l, at, last, -INFINITY, v);
-    take(v, at);
+    const float m = largest<W>(v);
+    add_terms<W>(a, v, m, c, above);
+    if constexpr (TOP) {
+      const int best = max16(ordered(m));
+      if ((tid & 15) == 0 && at < last) maxima[(at - first) / group_size<T>()] = value_of(best);
+    }
   }
-  a = wave_join(a, c);
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = a;
+  // about the row's maximum, then plain sums
+  a.m = value_of(wave_max(ordered(a.m)));
+  if ((tid & 63) == 0) slots[0][tid >> 6] = a.m;
   __syncthreads();
-  if (threadIdx.x >= 64) return;
-  a = slots[0];
-#pragma unroll
-  for (int w = 1; w < NT / 64; ++w) a = join(a, slots[w], c);
-  if (threadIdx.x == 0) {
-    if (A.chunks == 1) write_row<T>(A, r, y, a);
-    else A.part[blockIdx.x] = make_float4(a.m, a.s, a.t, 0.f);
+  Joined row{largest<NW>(slots[0]), 0.f, 0.f};
+  move_to(a, row.m, c);
+  a.s = wave_sum(a.s);
+  a.t = wave_sum(a.t);
+  if ((tid & 63) == 0) {
+    slots[1][tid >> 6] = a.s;
+    slots[2][tid >> 6] = a.t;
   }
+  __syncthreads();
+  if (tid >= 64) return;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    row.s += slots[1][w];
+    row.t += slots[2][w];
+  }
+  if (tid == 0) write_sums<T>(A, blockIdx.x, r, y, row);
   if constexpr (TOP) {
     Picker pick(list[0], A.top);
     pick_entries<T>(pick, maxima, l, first, last);
-    if (A.chunks == 1) {
-      write_top<T>(A, r, pick.list.keys, pick.n, a.m, a.s);
-    } else if (int(threadIdx.x) < A.top) {
-      A.keys[int64_t(blockIdx.x) * A.top + threadIdx.x] = int(threadIdx.x) < pick.n ? pick.list.keys[threadIdx.x] : Key(0);
-    }
+    write_picked<T>(A, blockIdx.x, r, pick, row);
   }
 }
 
@@ -355,23 +431,38 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs A) {
   const int64_t y = A.targets[r];
   if (y < 0) return write_none(A, r, lane);
   const float c = A.inv_temp * kLog2e;
-  Sums a = nothing();
-  for (int q = lane; q < A.chunks; q += 64) {
-    const float4 p = A.part[r * A.chunks + q];
-    a = join(a, Sums{p.x, p.y, p.z}, c);
+  const float4* part = A.part + r * A.chunks;
+  const float4 none = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float4 own = lane < A.chunks ? part[lane] : none;   // more than 64 chunks are read a second time
+  Sums a;
+  a.m = own.x;
+  for (int q = lane + 64; q < A.chunks; q += 64) a.m = fmaxf(a.m, part[q].x);
+  a.m = value_of(wave_max(ordered(a.m)));
+  for (int q = lane; q < A.chunks; q += 64) {   // about the row's maximum
+    const float4 p = q == lane ? own : part[q];
+    Sums b;
+    b.at = p.x;
+    b.s = p.y;
+    b.t = p.z;
+    move_to(b, a.m, c);
+    a.s += b.s;
+    a.t += b.t;
   }
-  a = wave_join(a, c);
-  if (lane == 0) write_row<T>(A, r, y, a);
+  const Joined row{a.m, wave_sum(a.s), wave_sum(a.t)};
+  if (lane == 0) write_row<T>(A, r, y, row);
   if constexpr (TOP) {
     const Key* keys = A.keys + r * A.chunks * A.top;
     const int n = A.chunks * A.top;
     Picker pick(lists[threadIdx.x >> 6], A.top);
-    Key best = 0;
-    for (int i = lane; i < n; i += 64) best = max(best, keys[i]);
+    float best = -INFINITY;
+    for (int i = lane; i < n; i += 64) best = fmaxf(best, value_of(keys[i]));
     pick.start(best);
-    for (int base = 0; base < n; base += 64) pick.push(base + lane < n ? keys[base + lane] : Key(0));
+    for (int base = 0; base < n; base += 64) {
+      const Key key = base + lane < n ? keys[base + lane] : kNone;
+      pick.push(value_of(key), place_of(key));
+    }
     pick.settle();
-    write_top<T>(A, r, pick.list.keys, pick.n, a.m, a.s);
+    write_top(A, r, pick, row);
   }
 }
 
@@ -414,13 +505,12 @@ template <class T, bool TOP>
 hipError_t forward_t(const LogpArgs& A, hipStream_t st) {
   const dim3 quads(uint32_t((A.rows + 3) / 4)), each(uint32_t(A.rows) * uint32_t(A.chunks));
   switch (logp_threads(A, T::kBytes == 4)) {
-    case 64:
-      if (A.vocab <= 128 * T::W) hipLaunchKernelGGL((k_logp_held<T, 2, TOP>), quads, dim3(256), 0, st, A);
-      else hipLaunchKernelGGL((k_logp_held<T, 4, TOP>), quads, dim3(256), 0, st, A);
+    case 0:
+      if (A.vocab <= 1024) hipLaunchKernelGGL((k_logp_held<T, 16 / T::W, TOP>), quads, dim3(256), 0, st, A);
+      else hipLaunchKernelGGL((k_logp_held<T, 32 / T::W, TOP>), quads, dim3(256), 0, st, A);
       break;
-    case 256: hipLaunchKernelGGL((k_logp_rows<T, 256, TOP>), each, dim3(256), 0, st, A); break;
-    case 512: hipLaunchKernelGGL((k_logp_rows<T, 512, TOP>), each, dim3(512), 0, st, A); break;
-    default: hipLaunchKernelGGL((k_logp_rows<T, 1024, TOP>), each, dim3(1024), 0, st, A);
+    case 64: hipLaunchKernelGGL((k_logp_rows<T, 64, TOP>), each, dim3(64), 0, st, A); break;
+    default: hipLaunchKernelGGL((k_logp_rows<T, 256, TOP>), each, dim3(256), 0, st, A);
   }
   if (A.chunks > 1) hipLaunchKernelGGL((k_logp_join<T, TOP>), quads, dim3(256), 0, st, A);
   return hipGetLastError();
@@ -428,19 +518,24 @@ hipError_t forward_t(const LogpArgs& A, hipStream_t st) {
 
 }  // namespace logp
 
+// A few long rows are cut, about 32 KB a part (us, 5 to 20 alternatives, whole and cut: 1 x 131072 bf16 21 and 15, 64 of
+// them 22 and 18, 200 23 and 25; 16 x 50257 14 and 16); and rows beyond a workgroup's list of groups.
 void plan_logp(LogpArgs& A, bool f32) {
   const int64_t rows = std::max(A.rows, 1), group = f32 ? 64 : 128, most = group * logp::kGroups;
-  int64_t chunks = rows < 256 ? std::min<int64_t>(512 / rows, A.vocab / 4096) : 1;
+  const int64_t bytes = int64_t(A.vocab) * (f32 ? 4 : 2);
+  int64_t chunks = rows <= 128 && bytes > 200 * 1024 ? std::min<int64_t>(bytes / 32768, 64) : 1;
   chunks = std::max<int64_t>({chunks, 1, (A.vocab + most - 1) / most});
   A.chunk = int32_t(((A.vocab + chunks - 1) / chunks + group - 1) / group * group);
   A.chunks = (A.vocab + A.chunk - 1) / A.chunk;
 }
 
-// 64: a wave holds the row, four rows a workgroup.
+// Threads of a row; 0: a wave holds it, four rows a workgroup (us, with alternatives: 20000 x 2000 fp32 held 40, by
+// 64 threads 58, by 256 55; 10000 x 4099 bf16 by 64 threads 32, by 256 51, by 512 105; 10000 x 4096 fp32, 16 KB a row,
+// by 64 52, by 256 45; 4096 x 131072 bf16 by 256 152, by 1024 250).
 int logp_threads(const LogpArgs& A, bool f32) {
   const int64_t bytes = int64_t(A.chunk) * (f32 ? 4 : 2);
-  if (A.chunks == 1 && int64_t(A.vocab) * (f32 ? 4 : 2) <= 4096) return 64;
-  return bytes <= 48 * 1024 ? 256 : bytes <= 160 * 1024 ? 512 : 1024;
+  if (A.chunks == 1 && A.vocab <= 2048) return 0;
+  return bytes <= 12 * 1024 ? 64 : 256;
 }
 
 hipError_t launch_logp(const LogpArgs& A, bool f32, hipStream_t st) {

@@ -1,6 +1,7 @@
 // C entry points of the operators beside the orthogonalizer: argument checks,
 // workspace layout and launches.  Nothing is enqueued for a refused call, and
 // no exception leaves an entry point.
+#include <algorithm>
 #include <new>
 #include <string>
 
@@ -580,6 +581,13 @@ tm_status policy_loss_backward(const void* logits, int64_t ld, const int64_t* ta
                 [&](char*, hipStream_t st) { return tmk::launch_loss_backward(A, dtype == TM_DTYPE_F32, st); });
 }
 
+// A temperature whose inverse stays finite as the factor of an exponent of 2.
+tm_status check_exponent(float t) {
+  TM_CHECK(check_temperature(t));
+  if (!(1.f / t <= 2.0e38f)) return refuse(TM_ERR_INVALID_ARG, "temperature must be 5e-39 or more");
+  return TM_OK;
+}
+
 tm_status token_logp(const void* logits, int64_t ld, const int64_t* targets, float temperature, float* logp,
                      float* entropy, float* stats, int64_t top, float* top_logp, int64_t* top_ids, int64_t rows,
                      int64_t vocab, int dtype, void* stream) {
@@ -587,7 +595,7 @@ tm_status token_logp(const void* logits, int64_t ld, const int64_t* targets, flo
   TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
   TM_CHECK(check_range("vocab", vocab, 1, TM_MAX_VOCAB));
   TM_CHECK(check_range("top", top, 0, vocab < TM_MAX_TOP ? vocab : TM_MAX_TOP));
-  TM_CHECK(check_temperature(temperature));
+  TM_CHECK(check_exponent(temperature));
   if (rows == 0) return TM_OK;
   const size_t esz = size_of(dtype);
   TM_CHECK(check_strides({{"ld", ld, vocab}}));
@@ -608,7 +616,7 @@ tm_status token_logp(const void* logits, int64_t ld, const int64_t* targets, flo
   A.top = int32_t(top);
   A.inv_temp = 1.f / temperature;
   tmk::plan_logp(A, dtype == TM_DTYPE_F32);
-  TM_CHECK(check_blocks(rows, A.chunks, uint64_t(tmk::logp_threads(A, dtype == TM_DTYPE_F32))));
+  TM_CHECK(check_blocks(rows, A.chunks, uint64_t(std::max(tmk::logp_threads(A, dtype == TM_DTYPE_F32), 64))));
   const uint64_t chunks = A.chunks > 1 ? uint64_t(rows) * uint64_t(A.chunks) : 0u;
   return run_op(TM_PHASE_TOKEN_LOGP, size_t(chunks * (sizeof(float4) + uint64_t(top) * 8u)), stream,
                 [&](char* ws, hipStream_t st) {
@@ -624,7 +632,7 @@ tm_status token_logp_backward(const void* logits, int64_t ld, const int64_t* tar
   TM_CHECK(check_dtype("dtype", dtype));
   TM_CHECK(check_range("rows", rows, 0, TM_MAX_ROWS));
   TM_CHECK(check_range("vocab", vocab, 1, TM_MAX_VOCAB));
-  TM_CHECK(check_temperature(temperature));
+  TM_CHECK(check_exponent(temperature));
   if (rows == 0) return TM_OK;
   const size_t esz = size_of(dtype);
   TM_CHECK(check_strides({{"ld", ld, vocab}, {"ld_dlogits", ldd, vocab}}));

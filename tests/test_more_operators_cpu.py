@@ -107,7 +107,7 @@ def test_nothing_to_do():
 
 @pytest.mark.parametrize("call,size", [
     (_logp, dict(rows=1 << 27, vocab=2000, ld=2000)), (_logp, dict(rows=1 << 24, vocab=8000, ld=8000)),
-    (_logp, dict(rows=1 << 23, vocab=100000, ld=100000)), (_logp_back, dict(rows=1 << 24, vocab=64)),
+    (_logp, dict(rows=1 << 24, vocab=100000, ld=100000)), (_logp_back, dict(rows=1 << 24, vocab=64)),
     (_logp_back, dict(rows=1 << 30, vocab=1 << 20, ld=1 << 20, ldd=1 << 20)),
 ])
 def test_launches_past_32_bits_of_threads_are_refused(call, size):
