@@ -270,10 +270,12 @@ tm_status expert_route(const void* logits, int64_t ld, const uint8_t* active, in
   tmk::plan_route(A);
   // workspace: the blocks' counts and sums of probabilities, lines of whole vectors
   const uint64_t entries = uint64_t(A.blocks) * ((uint64_t(experts) + 7u) / 8u * 8u);
-  const uint64_t counts = tmk::align256(entries * sizeof(uint16_t));
-  return run_op(TM_PHASE_EXPERT_ROUTE, size_t(counts + entries * sizeof(float)), stream, [&](char* ws, hipStream_t st) {
-    A.counts = reinterpret_cast<uint16_t*>(ws);
-    A.shares = reinterpret_cast<float*>(ws + counts);
+  const uint64_t dots = 256u + tmk::align256(uint64_t(A.blocks) * sizeof(double)), counts = tmk::align256(entries * sizeof(uint16_t));
+  return run_op(TM_PHASE_EXPERT_ROUTE, size_t(dots + counts + entries * sizeof(float)), stream, [&](char* ws, hipStream_t st) {
+    A.arrived = reinterpret_cast<int32_t*>(ws);
+    A.dots = reinterpret_cast<double*>(ws + 256u);
+    A.counts = reinterpret_cast<uint16_t*>(ws + dots);
+    A.shares = reinterpret_cast<float*>(ws + dots + counts);
     return tmk::launch_route(A, dtype == TM_DTYPE_F32, st);
   });
 }

@@ -105,6 +105,8 @@ struct RouteArgs {
   float* balance;
   uint16_t* counts;       // workspace: choices of each expert in each block of rows, [blocks][experts]
   float* shares;          // workspace: sums of its probabilities there, [blocks][experts]
+  double* dots;           // workspace: parts of the balance loss, one for a block or for several
+  int32_t* arrived;       // workspace: how many of them are there
   int64_t ld;
   int32_t rows, experts, top;
   int32_t blocks, turns;  // blocks of rows; runs of kRouteRows rows in each

@@ -27,13 +27,32 @@ namespace route {
 
 using namespace elem;
 
-constexpr int kThreads = 256, kRows = kRouteRows;
+constexpr int kRows = kRouteRows;
+constexpr float kLog2e = 1.4426950408889634f;
 
-// A reduction over the L lanes of a row, in each of them.  `slot`: LDS of a row of 256.
+// A reduction over the 16 lanes of a data-parallel row, the same in each of them.
+template <class V, class F>
+__device__ inline V over16(V v, F f) {
+  auto step = [&](auto ctrl) {
+    const int b = __builtin_bit_cast(int, v);
+    v = f(v, __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(b, b, decltype(ctrl)::value, 0xf, 0xf, true)));
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x128>{});   // row_ror:8, :4, :2, :1
+  step(integral_constant<int, 0x124>{});
+  step(integral_constant<int, 0x122>{});
+  step(integral_constant<int, 0x121>{});
+  return v;
+}
+
+// A reduction over the L lanes of a row of logits, the same in each of them.  `slot`: LDS for a row of 256.
 template <int L, class V, class F>
 __device__ inline V over_row(V v, V* slot, F f) {
-#pragma unroll
-  for (int o = (L < 64 ? L : 64) / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
+  v = over16(v, f);
+  if constexpr (L >= 64) {
+    auto of = [&](int lane) { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+    v = f(f(of(0), of(16)), f(of(32), of(48)));
+  }
   if constexpr (L > 64) {
     __syncthreads();   // the last use of the slot is over
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
@@ -47,8 +66,10 @@ __device__ inline V over_row(V v, V* slot, F f) {
 
 template <int L>
 struct Slots {
-  float f[L > 64 ? L / 64 : 1];
-  int i[L > 64 ? L / 64 : 1];
+  static constexpr int N = L > 64 ? L / 64 : 1;
+  float f[N];
+  int i[N];
+  uint32_t u[N];
 };
 template <int L>
 __device__ inline float row_max(float v, Slots<L>& s) { return over_row<L>(v, s.f, [](float a, float b) { return fmaxf(a, b); }); }
@@ -58,31 +79,171 @@ template <int L>
 __device__ inline int row_max(int v, Slots<L>& s) { return over_row<L>(v, s.i, [](int a, int b) { return max(a, b); }); }
 template <int L>
 __device__ inline int row_min(int v, Slots<L>& s) { return over_row<L>(v, s.i, [](int a, int b) { return min(a, b); }); }
+template <int L>
+__device__ inline uint32_t row_min(uint32_t v, Slots<L>& s) { return over_row<L>(v, s.u, [](uint32_t a, uint32_t b) { return min(a, b); }); }
 
 // Whole numbers in the order of the floats; -0 is 0, NaN is -inf.
 __device__ inline int ordered(float v) {
   const int b = __float_as_int(v > -INFINITY ? v + 0.f : -INFINITY);
   return b ^ ((b >> 31) & 0x7fffffff);
 }
-__device__ inline float value_of(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
 
 // L lanes a row, J vectors each: element (j L + t) W + i of the row is number j W + i of lane t.
 template <class T, int L, int J>
 struct Held {
   static constexpr int W = T::W, N = J * W, MOST = L * N;
   __device__ static int place(int t, int n) { return ((n / W) * L + t) * W + n % W; }
-  __device__ static void load(const char* row, int t, int experts, float* v) {
+  // Read ahead, and in place; past the row's end -inf.
+  __device__ static void load(const char* row, int t, int experts, u32x4_t (&q)[J]) {
+    if (experts % W == 0) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) load_vec<T>(row, (j * L + t) * W, experts, -INFINITY, v + j * W);
+      for (int j = 0; j < J; ++j) q[j] = load_ahead<T, false>(row, (j * L + t) * W, experts);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) q[j] = load_ahead<T, true>(row, (j * L + t) * W, experts);
+    }
+  }
+  __device__ static void values(const u32x4_t (&q)[J], int t, int experts, float (&v)[N]) {
+    if (experts % W == 0) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) T::unpack(q[j], v + j * W);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) T::unpack(settle<T, true>(q[j], (j * L + t) * W, experts), v + j * W);
+    }
+    if (experts < MOST) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] = place(t, n) < experts ? v[n] : -INFINITY;
+    }
   }
 };
 
+// The row's `top` best, exactly, by value and, of equal values, by place: the row is read again for each of them.
+// put(j, place) is called by one lane for each j.
+template <class T, int L, int J, class F>
+__device__ inline void pick_exact(const char* row, int t, int experts, int top, Slots<L>& slots, F put) {
+  int last = INT32_MAX, at = -1;   // the last one's order and place
+  for (int j = 0; j < top; ++j) {
+    int best = INT32_MIN, first = INT32_MAX;
+#pragma unroll 1
+    for (int u = 0; u < J; ++u) {
+      float v[T::W];
+      load_vec<T>(row, (u * L + t) * T::W, experts, -INFINITY, v);
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) {
+        const int place = (u * L + t) * T::W + i, k = ordered(v[i]);
+        const bool better = place < experts && k > best && (k < last || (k == last && place > at));
+        best = better ? k : best;
+        first = better ? place : first;
+      }
+    }
+    last = row_max<L>(best, slots);
+    at = row_min<L>(best == last ? first : INT32_MAX, slots);
+    if (t == 0) put(j, at);
+  }
+}
+
+// The same by keys of 32 bits: the value's order above the complement of the place, so that no two are the same and
+// a key tells its place (past the row's end they are those of -inf, behind all others).  The next best is the one that
+// is least below the last: one subtraction and half a minimum for each value.  Not for rows with NaN.  A bf16 value has its 16 bits beside a place of 16.  Of an fp32 value the last bits make way for
+// the place: one key more is taken, and where two neighbours in the list are the same in what is left, keys are taken
+// until the list's end is clear and its entries ranked by their whole values (256 scores: one row in 200).  Rows whose
+// list would pass the L lanes are picked exactly: many of the same value, all of them for a router that starts at zero.
 template <class T, int L, int J>
-__global__ __launch_bounds__(kThreads) void k_route(const RouteArgs A) {
+struct Keys {
+  static constexpr int N = Held<T, L, J>::N;
+  static constexpr bool EXACT = T::kBytes == 2;
+  static constexpr uint32_t places = EXACT ? 0xffffu : uint32_t(Held<T, L, J>::MOST - 1);   // of a power of two
+  static_assert(((places + 1) & places) == 0 && places >= uint32_t(Held<T, L, J>::MOST - 1), "a bit for each");
+  uint32_t key[N];
+  __device__ Keys(const float (&v)[N], int t) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int b = __float_as_int(v[n] + 0.f);
+      const uint32_t u = uint32_t(b) ^ (uint32_t(b >> 31) | 0x80000000u);
+      key[n] = ((u & ~places) | (places - uint32_t(Held<T, L, J>::place(t, 0)))) - uint32_t(Held<T, L, J>::place(0, n));
+    }
+  }
+  template <class F>
+  __device__ bool pick(const char* row, int t, int experts, int top, Slots<L>& slots, F put) const;
+};
+
+template <class T, int L, int J>
+template <class F>
+__device__ inline bool Keys<T, L, J>::pick(const char* row, int t, int experts, int top, Slots<L>& slots, F put) const {
+  if constexpr (!EXACT) {
+    if (L > 64 || top >= L) return false;
+  }
+  uint32_t below = 0xffffffffu;   // the next key is this or less
+  auto next = [&]() __attribute__((always_inline)) {
+    uint32_t least = below - key[0];
+#pragma unroll
+    for (int n = 1; n < N; ++n) least = min(least, below - key[n]);
+    const uint32_t found = below - row_min<L>(least, slots);
+    below = found - 1u;
+    return found;
+  };
+  uint32_t mine = 0u;   // key t of the list (of a long bf16 list, of the last L)
+  if constexpr (EXACT) {
+    for (int from = 0; from < top; from += L) {
+      const int here = min(top - from, L);
+      for (int j = 0; j < here; ++j) {
+        const uint32_t found = next();
+        mine = t == j ? found : mine;
+      }
+      if (t < here) put(from + t, int(places - (mine & places)));
+    }
+  } else {
+    int n = min(top + 1, experts);
+    uint32_t end = 0u, last = 0u;   // the last two keys
+    for (int j = 0; j < n; ++j) {
+      last = end;
+      end = next();
+      mine = t == j ? end : mine;
+    }
+    const uint32_t before = __shfl_up(mine, 1);   // of lane t - 1
+    const bool same = t > 0 && t < n && ((before ^ mine) & ~places) == 0u;
+    if (row_min<L>(same ? 0 : 1, slots) != 0) {
+      if (t < top) put(t, int(places - (mine & places)));
+      return true;
+    }
+    while (n < L && n < experts && ((end ^ last) & ~places) == 0u) {
+      last = end;
+      end = next();
+      mine = t == n ? end : mine;
+      ++n;
+    }
+    if (n < experts && ((end ^ last) & ~places) == 0u) return false;
+    const int place = int(places - (mine & places));
+    const int order = t < n && place < experts ? ordered(T::load1(row + int64_t(place) * T::kBytes)) : INT32_MIN;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) {
+      const int from = int(threadIdx.x & 63) - t + i, other = __shfl(order, from), there = __shfl(place, from);
+      rank += other > order || (other == order && there < place) ? 1 : 0;
+    }
+    if (t < n && rank < top) put(rank, place);
+  }
+  return true;
+}
+
+// LDS of one wave: what one lane has written the others read.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Threads of a block of rows.
+template <int L>
+constexpr int route_threads() { return L > 64 ? 256 : 512; }
+
+template <class T, int L, int J>
+__global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(const RouteArgs A) {
   using H = Held<T, L, J>;
-  constexpr int N = H::N, G = kThreads / L;
+  constexpr int N = H::N, NT = route_threads<L>(), G = NT / L;
   __shared__ uint64_t mask[H::MOST];
   __shared__ int before[H::MOST];
+  __shared__ float sums[L > 64 ? 1 : NT / 64][H::MOST];
   __shared__ float share[kRows * TM_MAX_TOP], whole[kRows];
   __shared__ uint16_t sel[kRows * TM_MAX_TOP];
   __shared__ Slots<L> slots;
@@ -90,66 +251,61 @@ __global__ __launch_bounds__(kThreads) void k_route(const RouteArgs A) {
   float acc[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) acc[n] = 0.f;
-  for (int e = threadIdx.x; e < experts; e += kThreads) before[e] = 0;
+  for (int e = threadIdx.x; e < experts; e += NT) before[e] = 0;
   for (int turn = 0; turn < A.turns; ++turn) {
     const int64_t first = (int64_t(blockIdx.x) * A.turns + turn) * kRows;
     const int rows = int(min(int64_t(kRows), A.rows - first));
     if (rows <= 0) break;
-    for (int e = threadIdx.x; e < experts; e += kThreads) mask[e] = 0;
+    for (int e = threadIdx.x; e < experts; e += NT) mask[e] = 0;
     __syncthreads();
+    auto active = [&](int at) { return at < rows && (A.active == nullptr || A.active[first + at] != 0); };
+    u32x4_t q[J];
+    bool on = active(grp);
+    if (on) H::load(A.logits + (first + grp) * A.ld * T::kBytes, t, experts, q);
     for (int at = grp; at < rows; at += G) {
-      const int64_t r = first + at;
-      if (A.active != nullptr && A.active[r] == 0) {
+      const bool now = on;
+      float v[N];
+      if (now) H::values(q, t, experts, v);
+      // the next row is on its way while this one is worked on
+      on = active(at + G);
+      if (on) H::load(A.logits + (first + at + G) * A.ld * T::kBytes, t, experts, q);
+      if (!now) {
         if (t == 0) whole[at] = -1.f;
         continue;
       }
-      float v[N];
-      H::load(A.logits + r * A.ld * T::kBytes, t, experts, v);
+      const char* row = A.logits + (first + at) * A.ld * T::kBytes;
       float m = v[0];
 #pragma unroll
       for (int n = 1; n < N; ++n) m = fmaxf(m, v[n]);
       m = row_max<L>(m, slots);
-      int key[N];
+      const Keys<T, L, J> keys(v, t);
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const bool there = H::place(t, n) < experts;
-        key[n] = there ? ordered(v[n]) : INT32_MIN;
-        v[n] = there ? expf(v[n] - m) : 0.f;
+        v[n] = __builtin_amdgcn_exp2f((v[n] - m) * kLog2e);
         sum += v[n];
       }
       sum = row_sum<L>(sum, slots);
       const float inv = 1.f / sum;
 #pragma unroll
       for (int n = 0; n < N; ++n) acc[n] += v[n] * inv;
+      auto put = [&](int j, int place) { sel[at * top + j] = uint16_t(place); };
+      if (sum != sum || !keys.pick(row, t, experts, top, slots, put)) pick_exact<T, L, J>(row, t, experts, top, slots, put);
+      wave_sync();
       float chosen = 0.f;
-      for (int j = 0; j < top; ++j) {
-        int best = key[0], place = 0;
-#pragma unroll
-        for (int n = 1; n < N; ++n)
-          if (key[n] > best) {
-            best = key[n];
-            place = n;
-          }
-        const int most = row_max<L>(best, slots);
-        const int mine = best == most ? H::place(t, place) : INT32_MAX;
-        const int e = row_min<L>(mine, slots);
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          if (e == mine && n == place) key[n] = INT32_MIN;
-        const float p = expf(value_of(most) - m);
+      for (int j = t; j < top; j += L) {
+        const int e = sel[at * top + j];
+        const float p = __builtin_amdgcn_exp2f((T::load1(row + int64_t(e) * T::kBytes) - m) * kLog2e);
+        share[at * top + j] = p;
         chosen += p;
-        if (t == 0) {
-          sel[at * top + j] = uint16_t(e);
-          share[at * top + j] = p;
-          atomicOr((unsigned long long*)&mask[e], 1ull << at);
-        }
+        atomicOr((unsigned long long*)&mask[e], 1ull << at);
       }
+      chosen = row_sum<L>(chosen, slots);
       // a sum that is not a number shows in the weights either way
       if (t == 0) whole[at] = A.renormalize ? chosen + 0.f * sum : sum;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * top; i += kThreads) {
+    for (int i = threadIdx.x; i < rows * top; i += NT) {
       const int at = i / top;
       const int64_t out = first * top + i;
       if (whole[at] == -1.f) {
@@ -163,62 +319,128 @@ __global__ __launch_bounds__(kThreads) void k_route(const RouteArgs A) {
       A.slots[out] = before[e] + __popcll(mask[e] & ((1ull << at) - 1));
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < experts; e += kThreads) before[e] += __popcll(mask[e]);
+    for (int e = threadIdx.x; e < experts; e += NT) before[e] += __popcll(mask[e]);
   }
-  // the groups' sums, one after the other, in the words that the last turn leaves free
-  float* sums = reinterpret_cast<float*>(mask);
-  for (int q = 0; q < G; ++q) {
-    __syncthreads();
-    if (grp == q)
+  // the groups of a wave, then the waves
+  if constexpr (L == 16) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) sums[H::place(t, n)] = (q > 0 ? sums[H::place(t, n)] : 0.f) + acc[n];
+    for (int n = 0; n < N; ++n) {
+      acc[n] += __shfl_xor(acc[n], 16);
+      acc[n] += __shfl_xor(acc[n], 32);
+    }
+  }
+  if (L > 64 || (threadIdx.x & 63) < L) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) sums[L > 64 ? 0 : threadIdx.x / 64][H::place(t, n)] = acc[n];
   }
   __syncthreads();
   const int width = (experts + 7) / 8 * 8;
-  for (int e = threadIdx.x; e < width; e += kThreads) {
+  for (int e = threadIdx.x; e < width; e += NT) {
+    float s = 0.f;
+    if (e < experts)
+      for (int w = 0; w < (L > 64 ? 1 : NT / 64); ++w) s += sums[w][e];
     A.counts[int64_t(blockIdx.x) * width + e] = uint16_t(e < experts ? before[e] : 0);
-    A.shares[int64_t(blockIdx.x) * width + e] = e < experts ? sums[e] : 0.f;
+    A.shares[int64_t(blockIdx.x) * width + e] = s;
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *A.arrived = 0;   // for k_route_place
 }
 
 constexpr int kPlace = 1024;
 
-// `span` blocks of k_route a workgroup; the first writes ends, the last the balance loss.
-template <int MOST>
-__global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A, int span) {
-  __shared__ int total[MOST], base[MOST], waves[kPlace / 64];
+typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
+
+// SPAN blocks of k_route a workgroup, each a share of its threads; the first workgroup writes ends.  The balance loss is
+// added up by vectors of eight experts, dealt out among the workgroups, and by the last of these to arrive.
+template <int MOST, int SPAN>
+__global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A) {
+  // expert 8 v + i at i vecs + v: neighbouring lanes, neighbouring words
+  __shared__ int total[MOST], base[SPAN][MOST], waves[kPlace / 64];
   __shared__ double parts[kPlace / 64];
+  constexpr int PER = (MOST + kPlace - 1) / kPlace, SHARE = kPlace / SPAN;
   const int experts = A.experts, width = (experts + 7) / 8 * 8, tid = threadIdx.x, lane = tid & 63;
-  const int own = int(blockIdx.x) * span;
-  for (int e = tid; e < width; e += kPlace) total[e] = base[e] = 0;
+  const int own = int(blockIdx.x) * SPAN, vecs = width / 8;
+  auto word = [&](int e) { return (e % 8) * vecs + e / 8; };
+  // what is needed last is asked for first: this thread's choices, its experts' counts in the blocks, and the first of
+  // the sums of probabilities that it adds up (vector blockIdx.x + m gridDim.x, block, half)
+  const int share = tid / SHARE, block = own + share;
+  const int64_t entries = int64_t(A.turns) * kRows * A.top, first = int64_t(block) * entries + tid % SHARE;
+  const int64_t last = block < A.blocks ? min(int64_t(block + 1) * entries, int64_t(A.rows) * A.top) : 0;
+  constexpr int EARLY = 2;
+  int chosen[EARLY], at[EARLY];
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i) {
+    chosen[i] = first + i * SHARE < last ? A.chosen[first + i * SHARE] : -1;
+    at[i] = first + i * SHARE < last ? A.slots[first + i * SHARE] : 0;
+  }
+  int count[PER > 1 ? 1 : SPAN];
+  if constexpr (PER == 1) {
+#pragma unroll
+    for (int u = 0; u < SPAN; ++u)
+      count[u] = own + u < A.blocks && tid < experts ? A.counts[int64_t(own + u) * width + tid] : 0;
+  }
+  const int grid = int(gridDim.x), summers = min(grid, vecs);   // workgroups that have sums to add up
+  const int64_t sums = int(blockIdx.x) < vecs ? int64_t((vecs - 1 - int(blockIdx.x)) / grid + 1) * A.blocks * 2 : 0;
+  auto expert_of = [&](int64_t i) { return (int(blockIdx.x) + int(i / 2 / A.blocks) * grid) * 8 + int(i % 2) * 4; };
+  auto sums_at = [&](int64_t i) {
+    return *reinterpret_cast<const float4*>(A.shares + (i / 2) % A.blocks * width + expert_of(i));
+  };
+  float4 early = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (tid < sums) early = sums_at(tid);
+  for (int e = tid; e < width; e += kPlace) total[e] = base[0][e] = 0;
   __syncthreads();
-  // the blocks' counts: vectors of eight experts, the blocks dealt out among the threads
-  const int vecs = width / 8, segments = max(kPlace / vecs, 1);
-  for (int at = tid; at < vecs * segments; at += kPlace) {
-    const int v = at % vecs;
+  // the blocks' counts: vectors of eight experts, `pitch` lanes for them, the blocks dealt out among the rest
+  int pitch = 16;
+  while (pitch < vecs && pitch < kPlace) pitch *= 2;
+  const int step = kPlace / pitch, each = A.turns <= 65535 / (8 * kRows) ? 8 : 1;   // counts that 16 bits hold the sum of
+  for (int v = tid % pitch; v < (vecs + pitch - 1) / pitch * pitch; v += pitch) {
     int all[8] = {}, low[8] = {};
-    for (int b = at / vecs; b < A.blocks; b += segments) {
-      const u32x4_t q = *reinterpret_cast<const u32x4_t*>(A.counts + int64_t(b) * width + v * 8);
+    for (int b = tid / pitch; v < vecs && b < A.blocks; b += 8 * step) {
+      u16x8_t q[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        q[u] = u16x8_t{0, 0, 0, 0, 0, 0, 0, 0};
+        if (b + u * step < A.blocks) q[u] = *reinterpret_cast<const u16x8_t*>(A.counts + int64_t(b + u * step) * width + v * 8);
+      }
+      auto add = [&](u16x8_t every, u16x8_t before) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          all[i] += every[i];
+          low[i] += before[i];
+        }
+      };
+      const u16x8_t none = u16x8_t{0, 0, 0, 0, 0, 0, 0, 0};
+      u16x8_t every = none, before = none;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        every += q[u];
+        before += b + u * step < own ? q[u] : none;
+        if (each == 1) {
+          add(every, before);
+          every = before = none;
+        }
+      }
+      add(every, before);
+    }
+    for (int o = pitch; o < 64; o *= 2)   // lanes of the same experts
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int n = int(i % 2 ? q[i / 2] >> 16 : q[i / 2] & 0xffffu);
-        all[i] += n;
-        if (b < own) low[i] += n;
+        all[i] += __shfl_xor(all[i], o);
+        low[i] += __shfl_xor(low[i], o);
       }
-    }
+    if (v < vecs && lane < pitch) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (all[i] != 0) atomicAdd(&total[v * 8 + i], all[i]);
-      if (low[i] != 0) atomicAdd(&base[v * 8 + i], low[i]);
+      for (int i = 0; i < 8; ++i) {
+        atomicAdd(&total[i * vecs + v], all[i]);
+        atomicAdd(&base[0][i * vecs + v], low[i]);
+      }
     }
   }
   __syncthreads();
   // exclusive sums of the totals: PER neighbouring experts a thread
-  constexpr int PER = (MOST + kPlace - 1) / kPlace;
   int mine[PER], sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    mine[i] = tid * PER + i < experts ? total[tid * PER + i] : 0;
+    mine[i] = tid * PER + i < experts ? total[word(tid * PER + i)] : 0;
     sum += mine[i];
   }
   int scan = sum;
@@ -235,48 +457,69 @@ __global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A, int s
     if (w < tid >> 6) start += waves[w];
     used += waves[w];
   }
+  // where each block's choices of an expert begin
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = tid * PER + i;
     if (e >= experts) continue;
-    base[e] += start;
+    int from = base[0][word(e)] + start;
+    if constexpr (PER > 1) {
+      static_assert(PER == 1 || SPAN == 1, "one block's");
+      base[0][word(e)] = from;
+    } else {
+#pragma unroll
+      for (int u = 0; u < SPAN; ++u) {
+        base[u][word(e)] = from;
+        from += count[u];
+      }
+    }
     start += mine[i];
     if (blockIdx.x == 0) A.ends[e] = start;
   }
-  for (int b = own; b < min(own + span, A.blocks); ++b) {
-    __syncthreads();
-    const int64_t first = int64_t(b) * A.turns * kRows * A.top;
-    const int64_t last = min(first + int64_t(A.turns) * kRows * A.top, int64_t(A.rows) * A.top);
-    for (int64_t i = first + tid; i < last; i += kPlace) {
-      const int e = A.chosen[i];
-      if (e >= 0) A.slots[i] += base[e];
-    }
-    __syncthreads();
-    for (int e = tid; e < experts; e += kPlace) base[e] += A.counts[int64_t(b) * width + e];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i)
+    if (chosen[i] >= 0) A.slots[first + i * SHARE] = at[i] + base[share][word(chosen[i])];
+  for (int64_t i = first + EARLY * SHARE; i < last; i += SHARE) {
+    const int e = A.chosen[i];
+    if (e >= 0) A.slots[i] += base[share][word(e)];
   }
-  if (blockIdx.x + 1 != gridDim.x) return;
+  if (int(blockIdx.x) >= summers) return;
   double dot = 0.0;
-  for (int at = tid; at < vecs * segments; at += kPlace) {
-    const int v = at % vecs;
-    double s[8] = {};
-    for (int b = at / vecs; b < A.blocks; b += segments) {
-      const float* from = A.shares + int64_t(b) * width + v * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += double(from[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dot += s[i] * double(total[v * 8 + i]);
+  for (int64_t i = tid; i < sums; i += kPlace) {
+    const float4 p = i == tid ? early : sums_at(i);
+    const int e = expert_of(i);
+    dot += double(p.x) * double(total[word(e)]) + double(p.y) * double(total[word(e + 1)]) +
+           double(p.z) * double(total[word(e + 2)]) + double(p.w) * double(total[word(e + 3)]);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
   if (lane == 0) parts[tid >> 6] = dot;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kPlace / 64; ++w) dot += parts[w];
-    const double rows = double(used) / double(A.top);
-    *A.balance = used > 0 ? float(double(experts) * dot / (double(used) * rows)) : 0.f;
+  if (tid >= 64) return;
+  dot = 0.0;
+  for (int w = 0; w < kPlace / 64; ++w) dot += parts[w];
+  if (summers > 1) {
+    // The part is written through to memory and waited for before the count goes up; the one who finds the count full
+    // reads the parts from memory.  A release would write back the whole cache for one value.
+    int arrived = 0;
+    if (tid == 0) {
+      __hip_atomic_store(&A.dots[blockIdx.x], dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      arrived = __hip_atomic_fetch_add(A.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (__builtin_amdgcn_readfirstlane(arrived) + 1 != summers) return;
+    asm volatile("" ::: "memory");   // no part is read before
+    dot = 0.0;
+    for (int i = tid; i < summers; i += 64)   // in the workgroups' order
+      dot += __hip_atomic_load(&A.dots[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
   }
+  if (tid == 0) *A.balance = used > 0 ? float(double(experts) * dot * double(A.top) / (double(used) * double(used))) : 0.f;
 }
+
+constexpr int kThreads = 256;
 
 template <class T, int L, int J>
 __global__ __launch_bounds__(kThreads) void k_route_backward(const RouteGradArgs A) {
@@ -302,7 +545,9 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(const RouteGradArgs
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = add[n] = 0.f;
     if (on) {
-      H::load(row, t, experts, v);
+      u32x4_t q[J];
+      H::load(row, t, experts, q);
+      H::values(q, t, experts, v);
       float m = v[0];
 #pragma unroll
       for (int n = 1; n < N; ++n) m = fmaxf(m, v[n]);
@@ -374,14 +619,20 @@ void with_shape(int experts, F f) {
 template <class T>
 hipError_t forward(const RouteArgs& A, hipStream_t st) {
   with_shape<T>(A.experts, [&](auto l, auto j) {
-    hipLaunchKernelGGL((k_route<T, decltype(l)::value, decltype(j)::value>), dim3(A.blocks), dim3(kThreads), 0, st, A);
+    constexpr int L = decltype(l)::value;
+    hipLaunchKernelGGL((k_route<T, L, decltype(j)::value>), dim3(A.blocks), dim3(route_threads<L>()), 0, st, A);
   });
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int span = (A.blocks + 127) / 128;
-  const dim3 grid((A.blocks + span - 1) / span);
-  if (A.experts <= 1024) hipLaunchKernelGGL((k_route_place<1024>), grid, dim3(kPlace), 0, st, A, span);
-  else hipLaunchKernelGGL((k_route_place<TM_MAX_EXPERTS>), grid, dim3(kPlace), 0, st, A, span);
+  if (A.experts > 1024) {
+    hipLaunchKernelGGL((k_route_place<TM_MAX_EXPERTS, 1>), dim3(A.blocks), dim3(kPlace), 0, st, A);
+  } else if (A.blocks <= 256) {
+    hipLaunchKernelGGL((k_route_place<1024, 1>), dim3(A.blocks), dim3(kPlace), 0, st, A);
+  } else if (A.blocks <= 512) {
+    hipLaunchKernelGGL((k_route_place<1024, 2>), dim3((A.blocks + 1) / 2), dim3(kPlace), 0, st, A);
+  } else {
+    hipLaunchKernelGGL((k_route_place<1024, 4>), dim3((A.blocks + 3) / 4), dim3(kPlace), 0, st, A);
+  }
   return hipGetLastError();
 }
 
