@@ -30,16 +30,6 @@ __device__ inline int64_t used_of(const RowsArgs& A) {
   return A.used != nullptr ? min(max(int64_t(*A.used), int64_t(0)), A.count) : A.count;
 }
 
-// Elements first .. of a row as stored, whole vectors as they are.
-template <class T>
-__device__ inline void copy_vec(char* to, const char* from, int n, u32x4_t q, bool whole) {
-  if (whole) {
-    T::store(to, q);
-  } else {
-    for (int i = 0; i < n; ++i) T::store1(to + i * T::kBytes, T::load1(from + i * T::kBytes));
-  }
-}
-
 // Zeros in the rows past the filled ones, dealt out among the groups of L threads.
 template <class T, int L>
 __device__ inline void zero_rest(const RowsArgs& A, int64_t used) {
@@ -50,43 +40,107 @@ __device__ inline void zero_rest(const RowsArgs& A, int64_t used) {
     for (int c = t * T::W; c < A.d; c += L * T::W) store_vec<T>(A.out + p * A.ldo * T::kBytes, c, A.d, z);
 }
 
-template <class T, int L>
+// Row r, the same in every lane of a wave where L is a wave or more: what is read by it comes by scalar loads then.
+template <int L>
+__device__ inline int64_t row_of(int64_t r) {
+  if constexpr (L < 64) return r;
+  return int64_t(__builtin_amdgcn_readfirstlane(int(r >> 32))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(r)));
+}
+
+// K choices of a row, from `first` on: their places, or -1.
+template <int K>
+struct Choices {
+  int64_t slot[K];
+  float weight[K];
+  __device__ void read(const RowsArgs& A, int64_t r, int first, int64_t used, bool weights) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int64_t i = r * A.top + first + j;
+      slot[j] = first + j < A.top ? slot_of(A, i, used) : -1;
+      weight[j] = 1.f;
+      if (weights && slot[j] >= 0) weight[j] = A.weights[i];
+    }
+  }
+};
+
+// A row goes to its slots, K of them at a time: read once for all of them.
+template <class T, int L, int K>
 __global__ __launch_bounds__(kThreads) void k_gather(const RowsArgs A) {
   constexpr int G = kThreads / L, W = T::W;
   const int t = threadIdx.x % L;
   const int64_t used = used_of(A);
-  for (int64_t r = int64_t(blockIdx.x) * G + threadIdx.x / L; r < A.rows; r += int64_t(gridDim.x) * G) {
+  for (int64_t at = int64_t(blockIdx.x) * G + threadIdx.x / L; at < A.rows; at += int64_t(gridDim.x) * G) {
+    const int64_t r = row_of<L>(at);
     const char* x = A.x + r * A.ldx * T::kBytes;
-    for (int c = t * W; c < A.d; c += L * W) {
-      const bool whole = c + W <= A.d;
-      u32x4_t q = {0u, 0u, 0u, 0u};
-      if (whole) q = T::load(x + int64_t(c) * T::kBytes);
-      for (int j = 0; j < A.top; ++j) {
-        const int64_t s = slot_of(A, r * A.top + j, used);
-        if (s >= 0) copy_vec<T>(A.out + (s * A.ldo + c) * T::kBytes, x + int64_t(c) * T::kBytes, A.d - c, q, whole);
+    for (int first = 0; first < A.top; first += K) {
+      Choices<K> to;
+      to.read(A, r, first, used, false);
+      for (int c = t * W; c < A.d; c += L * W) {
+        const uint32_t by = uint32_t(c) * T::kBytes;
+        if (c + W <= A.d) {
+          const u32x4_t q = T::load(x + by);
+#pragma unroll
+          for (int j = 0; j < K; ++j)
+            if (to.slot[j] >= 0) T::store(A.out + to.slot[j] * A.ldo * T::kBytes + by, q);
+        } else {
+          for (int i = 0; i < A.d - c; ++i) {
+            typedef std::conditional_t<T::kBytes == 2, uint16_t, uint32_t> Bits;
+            const Bits v = reinterpret_cast<const Bits*>(x + by)[i];
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+              if (to.slot[j] >= 0) reinterpret_cast<Bits*>(A.out + to.slot[j] * A.ldo * T::kBytes + by)[i] = v;
+          }
+        }
       }
     }
   }
   zero_rest<T, L>(A, used);
 }
 
-template <class T, int L>
+// Elements c .. of a row, zeros past its end.
+template <class T>
+__device__ inline u32x4_t load_part(const char* p, int left) {
+  if (left >= T::W) return T::load(p);
+  u32x4_t q = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < T::W; ++i)
+    if (i < left) T::put1(q, i, p + i * T::kBytes);
+  return q;
+}
+
+// K slots are read at a time; ONE: a row has no more.
+template <class T, int L, int K, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_combine(const RowsArgs A) {
   constexpr int G = kThreads / L, W = T::W;
   const int t = threadIdx.x % L;
-  for (int64_t r = int64_t(blockIdx.x) * G + threadIdx.x / L; r < A.rows; r += int64_t(gridDim.x) * G) {
+  for (int64_t at = int64_t(blockIdx.x) * G + threadIdx.x / L; at < A.rows; at += int64_t(gridDim.x) * G) {
+    const int64_t r = row_of<L>(at);
+    Choices<K> from;
+    if constexpr (ONE) from.read(A, r, 0, A.count, A.weights != nullptr);
     for (int c = t * W; c < A.d; c += L * W) {
+      const uint32_t by = uint32_t(c) * T::kBytes;
+      const int left = A.d - c;
       float acc[W] = {}, v[W];
-      for (int j = 0; j < A.top; ++j) {
-        const int64_t s = slot_of(A, r * A.top + j, A.count);
-        if (s < 0) continue;
-        const float w = A.weights != nullptr ? A.weights[r * A.top + j] : 1.f;
-        load_vec<T>(A.y + s * A.ldy * T::kBytes, c, A.d, 0.f, v);
+      u32x4_t res = {0u, 0u, 0u, 0u};
+      if (A.x != nullptr) res = load_part<T>(A.x + r * A.ldx * T::kBytes + by, left);
+      for (int first = 0; first < (ONE ? 1 : A.top); first += K) {
+        if constexpr (!ONE) from.read(A, r, first, A.count, A.weights != nullptr);
+        u32x4_t q[K];
 #pragma unroll
-        for (int i = 0; i < W; ++i) acc[i] += w * v[i];
+        for (int j = 0; j < K; ++j) {
+          q[j] = u32x4_t{0u, 0u, 0u, 0u};
+          if (from.slot[j] >= 0) q[j] = load_part<T>(A.y + from.slot[j] * A.ldy * T::kBytes + by, left);
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          if (from.slot[j] < 0) continue;   // a weight that is not a number would show
+          T::unpack(q[j], v);
+#pragma unroll
+          for (int i = 0; i < W; ++i) acc[i] += from.weight[j] * v[i];
+        }
       }
       if (A.x != nullptr) {
-        load_vec<T>(A.x + r * A.ldx * T::kBytes, c, A.d, 0.f, v);
+        T::unpack(res, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) acc[i] += v[i];
       }
@@ -95,50 +149,77 @@ __global__ __launch_bounds__(kThreads) void k_combine(const RowsArgs A) {
   }
 }
 
-// Sum over the L threads of a row, in the first of them.
-template <int L>
-__device__ inline float row_total(float v, float* slots) {
+// Sums over the L threads of a row, in the first of them.  `slots`: LDS of K floats a wave, for rows of 256.
+template <int L, int K>
+__device__ inline void row_totals(float (&v)[K], float* slots) {
 #pragma unroll
-  for (int o = (L < 64 ? L : 64) / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  if constexpr (L > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = slots[0];
+  for (int j = 0; j < K; ++j) {
+    if constexpr (L >= 64) {
+      v[j] = wave_sum(v[j]);
+    } else {
 #pragma unroll
-    for (int w = 1; w < L / 64; ++w) v += slots[w];
+      for (int o = L / 2; o > 0; o >>= 1) v[j] += __shfl_xor(v[j], o);
+    }
   }
-  return v;
+  if constexpr (L > 64) {
+    __syncthreads();   // the last row's are read
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int j = 0; j < K; ++j) slots[(threadIdx.x >> 6) * K + j] = v[j];
+    __syncthreads();
+    if (threadIdx.x == 0)
+#pragma unroll
+      for (int w = 1; w < L / 64; ++w)
+#pragma unroll
+        for (int j = 0; j < K; ++j) v[j] += slots[w * K + j];
+  }
 }
 
-template <class T, int L>
+// The gradient's row is read once for K slots.  DOTS: with the weights' gradient.
+template <class T, int L, int K, bool DOTS>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A) {
   constexpr int G = kThreads / L, W = T::W;
-  __shared__ float slots[kThreads / 64];
+  __shared__ float slots[L > 64 ? L / 64 * K : 1];
   const int t = threadIdx.x % L;
   const int64_t used = used_of(A);
-  for (int64_t r = int64_t(blockIdx.x) * G + threadIdx.x / L; r < A.rows; r += int64_t(gridDim.x) * G) {
-    for (int j = 0; j < A.top; ++j) {
-      const int64_t s = slot_of(A, r * A.top + j, used);
-      float dot = 0.f;
-      if (s >= 0) {
-        const float w = A.weights != nullptr ? A.weights[r * A.top + j] : 1.f;
-        for (int c = t * W; c < A.d; c += L * W) {
-          float g[W], v[W];
-          load_vec<T>(A.x + r * A.ldx * T::kBytes, c, A.d, 0.f, g);
-          if (A.dweights != nullptr) {
-            load_vec<T>(A.y + s * A.ldy * T::kBytes, c, A.d, 0.f, v);
+  for (int64_t at = int64_t(blockIdx.x) * G + threadIdx.x / L; at < A.rows; at += int64_t(gridDim.x) * G) {
+    const int64_t r = row_of<L>(at);
+    for (int first = 0; first < A.top; first += K) {
+      Choices<K> to;
+      to.read(A, r, first, used, A.weights != nullptr);
+      float dot[K] = {};
+      for (int c = t * W; c < A.d; c += L * W) {
+        const uint32_t by = uint32_t(c) * T::kBytes;
+        const int left = A.d - c;
+        float g[W], v[W];
+        u32x4_t q[K];
+        const u32x4_t own = load_part<T>(A.x + r * A.ldx * T::kBytes + by, left);
+        if constexpr (DOTS) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) dot += g[i] * v[i];
+          for (int j = 0; j < K; ++j) {
+            q[j] = u32x4_t{0u, 0u, 0u, 0u};
+            if (to.slot[j] >= 0) q[j] = load_part<T>(A.y + to.slot[j] * A.ldy * T::kBytes + by, left);
+          }
+        }
+        T::unpack(own, g);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          if (to.slot[j] < 0) continue;
+          if constexpr (DOTS) {
+            T::unpack(q[j], v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) dot[j] += g[i] * v[i];
           }
 #pragma unroll
-          for (int i = 0; i < W; ++i) g[i] *= w;
-          store_vec<T>(A.out + s * A.ldo * T::kBytes, c, A.d, g);
+          for (int i = 0; i < W; ++i) v[i] = g[i] * to.weight[j];
+          store_vec<T>(A.out + to.slot[j] * A.ldo * T::kBytes, c, A.d, v);
         }
       }
-      if (A.dweights != nullptr) {
-        dot = row_total<L>(dot, slots);
-        if (t == 0) A.dweights[r * A.top + j] = dot;
+      if constexpr (DOTS) {
+        row_totals<L, K>(dot, slots);
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+          if (t == 0 && first + j < A.top) A.dweights[r * A.top + first + j] = to.slot[j] >= 0 ? dot[j] : 0.f;
       }
     }
   }
@@ -154,6 +235,16 @@ void with_lanes(int d, F f) {
   else f(std::integral_constant<int, 256>{});
 }
 
+// f(K, whether a row has no more) with the slots that are gone through at a time.
+template <class F>
+void with_slots(int top, F f) {
+  using std::integral_constant;
+  if (top <= 2) f(integral_constant<int, 2>{}, std::true_type{});
+  else if (top <= 4) f(integral_constant<int, 4>{}, std::true_type{});
+  else if (top <= 8) f(integral_constant<int, 8>{}, std::true_type{});
+  else f(integral_constant<int, 8>{}, std::false_type{});
+}
+
 // Workgroups: a group of L threads for each row, or for each row past the filled ones.
 template <int L>
 dim3 grid_of(int64_t rows) {
@@ -165,7 +256,9 @@ template <class T>
 hipError_t gather(const RowsArgs& A, hipStream_t st) {
   with_lanes<T>(A.d, [&](auto l) {
     constexpr int L = decltype(l)::value;
-    hipLaunchKernelGGL((k_gather<T, L>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    with_slots(A.top, [&](auto k, auto) {
+      hipLaunchKernelGGL((k_gather<T, L, decltype(k)::value>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    });
   });
   return hipGetLastError();
 }
@@ -174,7 +267,9 @@ template <class T>
 hipError_t combine(const RowsArgs& A, hipStream_t st) {
   with_lanes<T>(A.d, [&](auto l) {
     constexpr int L = decltype(l)::value;
-    hipLaunchKernelGGL((k_combine<T, L>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    with_slots(A.top, [&](auto k, auto one) {
+      hipLaunchKernelGGL((k_combine<T, L, decltype(k)::value, decltype(one)::value>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    });
   });
   return hipGetLastError();
 }
@@ -183,7 +278,11 @@ template <class T>
 hipError_t combine_backward(const RowsArgs& A, hipStream_t st) {
   with_lanes<T>(A.d, [&](auto l) {
     constexpr int L = decltype(l)::value;
-    hipLaunchKernelGGL((k_combine_backward<T, L>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    with_slots(A.top, [&](auto k, auto) {
+      constexpr int K = decltype(k)::value;
+      if (A.dweights != nullptr) hipLaunchKernelGGL((k_combine_backward<T, L, K, true>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+      else hipLaunchKernelGGL((k_combine_backward<T, L, K, false>), grid_of<L>(A.rows), dim3(kThreads), 0, st, A);
+    });
   });
   return hipGetLastError();
 }
