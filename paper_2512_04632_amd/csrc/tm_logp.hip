@@ -63,8 +63,9 @@ __device__ inline float largest(const float* v) {
   return m;
 }
 
-// Adds N logits whose maximum is m.
-template <int N>
+// Adds N logits whose maximum is m.  FILLED: some of them may be the -inf past a row's end, where e u is held at 0;
+// else that is done only where one is met.
+template <int N, bool FILLED>
 __device__ inline void add_terms(Sums& a, const float* v, float m, float c, float above) {
   a.m = fmaxf(a.m, m);
   if (m > a.limit) {
@@ -77,19 +78,41 @@ __device__ inline void add_terms(Sums& a, const float* v, float m, float c, floa
   for (int i = 0; i < N; ++i) {
     const float u = (v[i] - at) * c, e = exp2_fast(u);
     s[i % 2] += e;
-    t[i % 2] += e * u;
+    t[i % 2] += e * (FILLED ? fmaxf(u, kFar) : u);
   }
   t[0] += t[1];
-  if (t[0] != t[0]) {   // 0 (-inf), which is 0; a value that is not a number shows in s
+  if (!FILLED && __ballot(t[0] != t[0]) != 0) {   // 0 (-inf), which is 0; a value that is not a number shows in s
+    float from = at;
+    asm volatile("" : "+v"(from));   // keeps this out of the way that all other terms take
     t[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float u = (v[i] - at) * c;
+      const float u = (v[i] - from) * c;
       t[0] += exp2_fast(u) * fmaxf(u, kFar);
     }
   }
   a.s += s[0] + s[1];
   a.t += t[0];
+}
+
+// Entries at .. at + W - 1 of a row that ends at `last`, at a multiple of W, and what they are; -inf past the end.
+template <class T>
+__device__ inline u32x4_t load_to(const char* l, int at, int last) {
+  return last % T::W == 0 ? load_ahead<T, false>(l, at, last) : load_ahead<T, true>(l, at, last);
+}
+template <class T>
+__device__ inline void values_to(u32x4_t q, int at, int last, float* v) {
+  if (last % T::W == 0) {   // whole, or wholly past the end
+    T::unpack(q, v);
+    if (at >= last)
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) v[i] = -INFINITY;
+  } else {
+    T::unpack(settle<T, true>(q, at, last), v);
+    if (at + T::W > last)
+#pragma unroll
+      for (int i = 0; i < T::W; ++i) v[i] = at + i < last ? v[i] : -INFINITY;
+  }
 }
 
 // m, and the sums about it.
@@ -192,8 +215,18 @@ struct Picker {
     if (n > kListed - 64) settle();
   }
   // Raises the bound to the `top`-th best of values of which each lane has one (of different entries), where there
-  // are so many: the least value that fewer than `top` are above.
+  // are so many: for a few the best is taken away top - 1 times, else it is the least value that fewer than `top` are
+  // above.
   __device__ void start(float lanes_best) {
+    if (top <= 8) {
+      int v = ordered(lanes_best);
+      for (int i = 1; i < top; ++i) {
+        const uint64_t who = __ballot(v == wave_max(v));
+        if ((threadIdx.x & 63) == __ffsll((unsigned long long)who) - 1) v = INT32_MIN;
+      }
+      low = fmaxf(value_of(wave_max(v)), kLowest);
+      return;
+    }
     float* values = reinterpret_cast<float*>(list.keys);
     values[threadIdx.x & 63] = lanes_best;
     wave_sync();
@@ -243,7 +276,8 @@ __device__ inline void write_none(const LogpArgs& A, int64_t r, int t) {
 }
 
 // ---------------------------------------------------------------- forward
-// A wave per row, which holds it in registers, K vectors a lane.
+// A wave per row, which holds it in registers, K vectors a lane.  (Waves that go on to other rows, the next one on its
+// way, are slower: what the compiler keeps from row to row takes the registers of half the waves.)
 template <class T, int K, bool TOP>
 __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   constexpr int W = T::W;
@@ -256,12 +290,15 @@ __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   const char* l = A.logits + r * A.ld * T::kBytes;
   const float c = A.inv_temp * kLog2e;
   float v[K * W];
+  u32x4_t q[K];
 #pragma unroll
-  for (int j = 0; j < K; ++j) load_vec<T>(l, (j * 64 + lane) * W, n, -INFINITY, v + j * W);
+  for (int j = 0; j < K; ++j) q[j] = load_to<T>(l, (j * 64 + lane) * W, n);
+#pragma unroll
+  for (int j = 0; j < K; ++j) values_to<T>(q[j], (j * 64 + lane) * W, n, v + j * W);
   const float mine = largest<K * W>(v);
   Sums a;
   a.m = value_of(wave_max(ordered(mine)));
-  add_terms<K * W>(a, v, a.m, c, 0.f);
+  add_terms<K * W, true>(a, v, a.m, c, 0.f);
   const Joined row{a.m, wave_sum(a.s), wave_sum(a.t)};
   if (lane == 0) write_row<T>(A, r, y, row);
   if constexpr (TOP) {
@@ -274,8 +311,8 @@ __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   }
 }
 
-// Most groups of a chunk.
-constexpr int kGroups = 2048;
+// Most groups of a chunk; a wave has rows of kWaveBytes at most, and the less LDS, the more of them there are.
+constexpr int kGroups = 2048, kWaveBytes = 12 * 1024;
 template <class T>
 constexpr int group_size() { return 16 * T::W; }
 
@@ -312,7 +349,7 @@ __device__ inline void pick_entries(Picker& pick, const float* maxima, const cha
   auto read = [&](int base, float* v) __attribute__((always_inline)) {
     const int from = base + (lane >> 4), g = place_of(__shfl((unsigned long long)mine, from & 63));
     const int at = from < found ? first + g * GROUP + (lane & 15) * W : last;
-    load_vec<T>(l, at, last, -INFINITY, v);
+    values_to<T>(load_to<T>(l, at, last), at, last, v);
     return at;
   };
   float v[W];
@@ -340,7 +377,8 @@ template <class T, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void k_logp_rows(const LogpArgs A) {
   constexpr int W = T::W, STEP = NT * W, G = 4, NW = NT / 64;
   __shared__ float slots[3][NW];
-  __shared__ float maxima[TOP ? kGroups : 1];
+  constexpr int GROUPS = NT > 64 ? kGroups : kWaveBytes / 256;   // of 256 bytes
+  __shared__ float maxima[TOP ? GROUPS : 1];
   __shared__ List list[1];
   const int64_t r = blockIdx.x / A.chunks;
   const int64_t y = A.targets[r];
@@ -372,7 +410,7 @@ __global__ __launch_bounds__(NT) void k_logp_rows(const LogpArgs A) {
     base += G * STEP;
     more = base + G * STEP <= last;
     if (more) load(base);
-    add_terms<G * W>(a, v, largest<G>(m), c, above);
+    add_terms<G * W, false>(a, v, largest<G>(m), c, above);
     if constexpr (TOP) {
       int mine = 0;
 #pragma unroll
@@ -386,9 +424,9 @@ __global__ __launch_bounds__(NT) void k_logp_rows(const LogpArgs A) {
   for (; base < last; base += STEP) {   // every lane, those past the end with -inf
     const int at = base + tid * W;
     float v[W];
-    load_vec<T>(l, at, last, -INFINITY, v);
+    values_to<T>(load_to<T>(l, at, last), at, last, v);
     const float m = largest<W>(v);
-    add_terms<W>(a, v, m, c, above);
+    add_terms<W, true>(a, v, m, c, above);
     if constexpr (TOP) {
       const int best = max16(ordered(m));
       if ((tid & 15) == 0 && at < last) maxima[(at - first) / group_size<T>()] = value_of(best);
@@ -535,7 +573,7 @@ void plan_logp(LogpArgs& A, bool f32) {
 int logp_threads(const LogpArgs& A, bool f32) {
   const int64_t bytes = int64_t(A.chunk) * (f32 ? 4 : 2);
   if (A.chunks == 1 && A.vocab <= 2048) return 0;
-  return bytes <= 12 * 1024 ? 64 : 256;
+  return bytes <= logp::kWaveBytes ? 64 : 256;
 }
 
 hipError_t launch_logp(const LogpArgs& A, bool f32, hipStream_t st) {

@@ -82,9 +82,15 @@ __global__ __launch_bounds__(kThreads) void k_gather(const RowsArgs A) {
 #pragma unroll
           for (int j = 0; j < K; ++j)
             if (to.slot[j] >= 0) T::store(A.out + to.slot[j] * A.ldo * T::kBytes + by, q);
+        } else if (A.d >= W) {   // the row's last W elements: some are written a second time, as they are
+          const uint32_t end = uint32_t(A.d - W) * T::kBytes;
+          const u32x4_t q = T::load(x + end);
+#pragma unroll
+          for (int j = 0; j < K; ++j)
+            if (to.slot[j] >= 0) T::store(A.out + to.slot[j] * A.ldo * T::kBytes + end, q);
         } else {
+          typedef std::conditional_t<T::kBytes == 2, uint16_t, uint32_t> Bits;
           for (int i = 0; i < A.d - c; ++i) {
-            typedef std::conditional_t<T::kBytes == 2, uint16_t, uint32_t> Bits;
             const Bits v = reinterpret_cast<const Bits*>(x + by)[i];
 #pragma unroll
             for (int j = 0; j < K; ++j)
@@ -97,15 +103,11 @@ __global__ __launch_bounds__(kThreads) void k_gather(const RowsArgs A) {
   zero_rest<T, L>(A, used);
 }
 
-// Elements c .. of a row, zeros past its end.
+// Elements c .. of a row, zeros past its end, from what load_ahead read.
 template <class T>
-__device__ inline u32x4_t load_part(const char* p, int left) {
-  if (left >= T::W) return T::load(p);
-  u32x4_t q = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int i = 0; i < T::W; ++i)
-    if (i < left) T::put1(q, i, p + i * T::kBytes);
-  return q;
+__device__ inline void part(u32x4_t q, int c, int d, float* v) {
+  if (d % T::W == 0) T::unpack(q, v);
+  else T::unpack(settle<T, true>(q, c, d), v);
 }
 
 // K slots are read at a time; ONE: a row has no more.
@@ -118,29 +120,27 @@ __global__ __launch_bounds__(kThreads) void k_combine(const RowsArgs A) {
     Choices<K> from;
     if constexpr (ONE) from.read(A, r, 0, A.count, A.weights != nullptr);
     for (int c = t * W; c < A.d; c += L * W) {
-      const uint32_t by = uint32_t(c) * T::kBytes;
-      const int left = A.d - c;
       float acc[W] = {}, v[W];
       u32x4_t res = {0u, 0u, 0u, 0u};
-      if (A.x != nullptr) res = load_part<T>(A.x + r * A.ldx * T::kBytes + by, left);
+      if (A.x != nullptr) res = load_ahead<T, true>(A.x + r * A.ldx * T::kBytes, c, A.d);
       for (int first = 0; first < (ONE ? 1 : A.top); first += K) {
         if constexpr (!ONE) from.read(A, r, first, A.count, A.weights != nullptr);
         u32x4_t q[K];
 #pragma unroll
         for (int j = 0; j < K; ++j) {
           q[j] = u32x4_t{0u, 0u, 0u, 0u};
-          if (from.slot[j] >= 0) q[j] = load_part<T>(A.y + from.slot[j] * A.ldy * T::kBytes + by, left);
+          if (from.slot[j] >= 0) q[j] = load_ahead<T, true>(A.y + from.slot[j] * A.ldy * T::kBytes, c, A.d);
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
           if (from.slot[j] < 0) continue;   // a weight that is not a number would show
-          T::unpack(q[j], v);
+          part<T>(q[j], c, A.d, v);
 #pragma unroll
           for (int i = 0; i < W; ++i) acc[i] += from.weight[j] * v[i];
         }
       }
       if (A.x != nullptr) {
-        T::unpack(res, v);
+        part<T>(res, c, A.d, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) acc[i] += v[i];
       }
@@ -189,24 +189,22 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A)
       to.read(A, r, first, used, A.weights != nullptr);
       float dot[K] = {};
       for (int c = t * W; c < A.d; c += L * W) {
-        const uint32_t by = uint32_t(c) * T::kBytes;
-        const int left = A.d - c;
         float g[W], v[W];
         u32x4_t q[K];
-        const u32x4_t own = load_part<T>(A.x + r * A.ldx * T::kBytes + by, left);
+        const u32x4_t own = load_ahead<T, true>(A.x + r * A.ldx * T::kBytes, c, A.d);
         if constexpr (DOTS) {
 #pragma unroll
           for (int j = 0; j < K; ++j) {
             q[j] = u32x4_t{0u, 0u, 0u, 0u};
-            if (to.slot[j] >= 0) q[j] = load_part<T>(A.y + to.slot[j] * A.ldy * T::kBytes + by, left);
+            if (to.slot[j] >= 0) q[j] = load_ahead<T, true>(A.y + to.slot[j] * A.ldy * T::kBytes, c, A.d);
           }
         }
-        T::unpack(own, g);
+        part<T>(own, c, A.d, g);
 #pragma unroll
         for (int j = 0; j < K; ++j) {
           if (to.slot[j] < 0) continue;
           if constexpr (DOTS) {
-            T::unpack(q[j], v);
+            part<T>(q[j], c, A.d, v);
 #pragma unroll
             for (int i = 0; i < W; ++i) dot[j] += g[i] * v[i];
           }
