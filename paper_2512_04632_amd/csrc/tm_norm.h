@@ -14,6 +14,13 @@ using namespace elem;
 // NT / 64 floats and is not used again before another barrier.
 template <int NT, int N>
 __device__ inline void row_sum(float (&v)[N], float* slot) {
+  if constexpr (NT < 64) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int o = NT / 2; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
   if constexpr (NT > 64) {

@@ -222,7 +222,7 @@ tm_status rms_norm_backward(const void* dy, int64_t lddy, const void* s, int64_t
   A.rows = int32_t(rows);
   A.d = int32_t(d);
   A.dweight = dweight;
-  const int blocks = tmk::norm_blocks(rows, d, dtype == TM_DTYPE_F32);
+  const int blocks = tmk::rms_backward_blocks(rows, d, dtype == TM_DTYPE_F32);
   const bool params = dweight != nullptr && (blocks != 1 || d > tmk::kNormMaxFused);
   const size_t bytes = params ? size_t(blocks) * size_t(d) * 4u : 0u;
   return run_op(TM_PHASE_RMS_NORM_BACKWARD, bytes, stream, [&](char* ws, hipStream_t st) {

@@ -56,7 +56,7 @@ struct RmsArgs {
 };
 
 hipError_t launch_rms(const RmsArgs& A, bool f32, hipStream_t st);
-// `blocks` of norm_blocks.
+int rms_backward_blocks(int64_t rows, int64_t d, bool f32);   // and so column sums in `part`
 hipError_t launch_rms_backward(const RmsArgs& A, bool f32, int blocks, hipStream_t st);
 
 // ---------------------------------------------------------------- expert products

@@ -233,6 +233,28 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Exclusive sums of the experts' bits, by one wave.
+__device__ inline void starts(const uint64_t* mask, int* before, int experts) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int base = 0; base < experts; base += 64) {
+    const int e = base + lane, n = e < experts ? __popcll(mask[e]) : 0;
+    int scan = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(scan, o);
+      if (lane >= o) scan += up;
+    }
+    if (e < experts) before[e] = sum + scan - n;
+    sum += __shfl(scan, 63);
+  }
+}
+
+// The balance loss from sum_e c_e (sum of the rows' p_e) and the number of choices.
+__device__ inline float balance_of(const RouteArgs& A, double dot, int used) {
+  return used > 0 ? float(double(A.experts) * dot * double(A.top) / (double(used) * double(used))) : 0.f;
+}
+
 // Threads of a block of rows.
 template <int L>
 constexpr int route_threads() { return L > 64 ? 256 : 512; }
@@ -244,7 +266,7 @@ __global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(co
   __shared__ uint64_t mask[H::MOST];
   __shared__ int before[H::MOST];
   __shared__ float sums[L > 64 ? 1 : NT / 64][H::MOST];
-  __shared__ float share[kRows * TM_MAX_TOP], whole[kRows];
+  __shared__ __attribute__((aligned(8))) float share[kRows * TM_MAX_TOP], whole[kRows];
   __shared__ uint16_t sel[kRows * TM_MAX_TOP];
   __shared__ Slots<L> slots;
   const int t = threadIdx.x % L, grp = threadIdx.x / L, experts = A.experts, top = A.top;
@@ -305,6 +327,10 @@ __global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(co
       if (t == 0) whole[at] = A.renormalize ? chosen + 0.f * sum : sum;
     }
     __syncthreads();
+    if (A.blocks == 1) {   // one turn: what stands before the experts' choices is known at once
+      if (threadIdx.x < 64) starts(mask, before, experts);
+      __syncthreads();
+    }
     for (int i = threadIdx.x; i < rows * top; i += NT) {
       const int at = i / top;
       const int64_t out = first * top + i;
@@ -334,6 +360,27 @@ __global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(co
     for (int n = 0; n < N; ++n) sums[L > 64 ? 0 : threadIdx.x / 64][H::place(t, n)] = acc[n];
   }
   __syncthreads();
+  if (A.blocks == 1) {
+    // the counts have been added to what stands before them; the choices are their differences
+    double dot = 0.0;
+    for (int e = threadIdx.x; e < experts; e += NT) {
+      float s = 0.f;
+      for (int w = 0; w < (L > 64 ? 1 : NT / 64); ++w) s += sums[w][e];
+      A.ends[e] = before[e];
+      dot += double(s) * double(before[e] - (e > 0 ? before[e - 1] : 0));
+    }
+    const int used = before[experts - 1];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
+    double* parts = reinterpret_cast<double*>(share);
+    if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = dot;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < NT / 64; ++w) dot += parts[w];
+      *A.balance = balance_of(A, dot, used);
+    }
+    return;
+  }
   const int width = (experts + 7) / 8 * 8;
   for (int e = threadIdx.x; e < width; e += NT) {
     float s = 0.f;
@@ -516,7 +563,7 @@ __global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
   }
-  if (tid == 0) *A.balance = used > 0 ? float(double(experts) * dot * double(A.top) / (double(used) * double(used))) : 0.f;
+  if (tid == 0) *A.balance = balance_of(A, dot, used);
 }
 
 constexpr int kThreads = 256;
@@ -623,7 +670,7 @@ hipError_t forward(const RouteArgs& A, hipStream_t st) {
     hipLaunchKernelGGL((k_route<T, L, decltype(j)::value>), dim3(A.blocks), dim3(route_threads<L>()), 0, st, A);
   });
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || A.blocks == 1) return e;
   if (A.experts > 1024) {
     hipLaunchKernelGGL((k_route_place<TM_MAX_EXPERTS, 1>), dim3(A.blocks), dim3(kPlace), 0, st, A);
   } else if (A.blocks <= 256) {

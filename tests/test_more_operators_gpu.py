@@ -24,7 +24,7 @@ def _all(seed, rows=ROWS, vocab=VOCAB):
     return dict(x=randn(rows, D).bfloat16(), residual=randn(rows, D).bfloat16(), norm=1 + 0.1 * randn(D),
                 scores=randn(rows, EXPERTS), active=torch.rand(rows, generator=g, device="cuda") < 0.9,
                 up=randn(EXPERTS, D, HIDDEN).bfloat16() * D ** -0.5, down=randn(EXPERTS, HIDDEN, D).bfloat16() * HIDDEN ** -0.5,
-                logits=randn(rows, vocab).bfloat16(), targets=targets, gw=randn(rows, TOP), gb=randn(1)[0],
+                logits=randn(rows, vocab).bfloat16(), targets=targets, long=randn(3, 131072).bfloat16(), gw=randn(rows, TOP), gb=randn(1)[0],
                 gx=randn(rows, D).bfloat16(), gl=randn(rows), gh=randn(rows))
 
 
@@ -41,7 +41,7 @@ def _run(s):
     ds, dnorm = tm.rms_norm_backward(dh, total, rstd, s["norm"], s["gx"])
     found = tm.token_logp(s["logits"], s["targets"], 5)
     dl = tm.token_logp_backward(s["logits"], s["targets"], found[2], found[1], s["gl"], s["gh"])
-    few = tm.token_logp(s["logits"][:5], s["targets"][:5], 5)
+    few = tm.token_logp(s["long"], s["targets"][1:4], 5)
     return [y, total, rstd, chosen, weights, slots, ends, balance, out, back, x, dy, dw, dscores, dh, ds, dnorm, *found, dl, *few]
 
 
@@ -208,7 +208,7 @@ def test_capture_without_workspace_is_refused():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=st):
         kept = s["x"] + 1
-        for call in (lambda: tm.expert_route(s["scores"], TOP), lambda: tm.token_logp(s["logits"][:5], s["targets"][:5])):
+        for call in (lambda: tm.expert_route(s["scores"], TOP), lambda: tm.token_logp(s["long"], s["targets"][1:4])):
             with pytest.raises(tm.TurboMuonError) as e:
                 call()
             assert e.value.status == tm.TM_ERR_UNSUPPORTED
@@ -222,7 +222,7 @@ def test_failed_allocation_is_reported(monkeypatch):
     ref = _run(s)
     tm.release_workspaces()
     monkeypatch.setenv("TM_TEST_FAIL_ALLOC", "1")
-    for call in (lambda: tm.expert_route(s["scores"], TOP), lambda: tm.token_logp(s["logits"][:5], s["targets"][:5]),
+    for call in (lambda: tm.expert_route(s["scores"], TOP), lambda: tm.token_logp(s["long"], s["targets"][1:4]),
                  lambda: tm.rms_norm_backward(s["gx"], ref[1], ref[2], s["norm"])):
         with pytest.raises(tm.TurboMuonError) as e:
             call()
