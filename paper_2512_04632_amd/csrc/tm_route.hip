@@ -49,10 +49,16 @@ __device__ inline V over16(V v, F f) {
 template <int L, class V, class F>
 __device__ inline V over_row(V v, V* slot, F f) {
   v = over16(v, f);
-  if constexpr (L >= 64) {
-    auto of = [&](int lane) { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
-    v = f(f(of(0), of(16)), f(of(32), of(48)));
-  }
+  // rows of 16 lanes in pairs, then halves of the wave: a swap leaves one of the two in each operand, which the compiler
+  // must not take for the same value
+  auto swap = [&](auto how) __attribute__((always_inline)) {
+    uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+    asm("" : "+v"(y));
+    const auto both = how(x, y);
+    v = f(__builtin_bit_cast(V, uint32_t(both[0])), __builtin_bit_cast(V, uint32_t(both[1])));
+  };
+  if constexpr (L >= 32) swap([](uint32_t x, uint32_t y) { return __builtin_amdgcn_permlane16_swap(x, y, false, false); });
+  if constexpr (L >= 64) swap([](uint32_t x, uint32_t y) { return __builtin_amdgcn_permlane32_swap(x, y, false, false); });
   if constexpr (L > 64) {
     __syncthreads();   // the last use of the slot is over
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
@@ -348,13 +354,10 @@ __global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(co
     for (int e = threadIdx.x; e < experts; e += NT) before[e] += __popcll(mask[e]);
   }
   // the groups of a wave, then the waves
-  if constexpr (L == 16) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      acc[n] += __shfl_xor(acc[n], 16);
-      acc[n] += __shfl_xor(acc[n], 32);
-    }
-  }
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int o = L; o < 64; o *= 2) acc[n] += __shfl_xor(acc[n], o);
   if (L > 64 || (threadIdx.x & 63) < L) {
 #pragma unroll
     for (int n = 0; n < N; ++n) sums[L > 64 ? 0 : threadIdx.x / 64][H::place(t, n)] = acc[n];
@@ -659,6 +662,7 @@ void with_shape(int experts, F f) {
   if (experts <= 16 * W) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
   else if (experts <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8 / W>{});
   else if (experts <= 256) f(integral_constant<int, 16>{}, integral_constant<int, 16 / W>{});
+  else if (experts <= 512) f(integral_constant<int, 32>{}, integral_constant<int, 16 / W>{});
   else if (experts <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 16 / W>{});
   else f(integral_constant<int, 256>{}, integral_constant<int, 32 / W>{});
 }

@@ -102,7 +102,7 @@ def _check_gradient(got, logits, chosen, ends, dweights, dbalance, renormalize, 
 # rows, experts, top: one of each to many; sizes around those at which a row gets more lanes, a block more
 # rows, or the launch more blocks; odd ones
 SIZES = [(1, 1, 1), (1, 2, 2), (3, 5, 3), (63, 8, 2), (64, 8, 2), (65, 8, 1), (200, 60, 4), (129, 64, 6), (1000, 65, 8),
-         (77, 128, 64), (500, 129, 5), (333, 255, 8), (400, 256, 8), (70, 257, 7), (90, 1000, 3), (65, 1025, 4), (30, 4097, 64),
+         (77, 128, 64), (500, 129, 5), (333, 255, 8), (400, 256, 8), (70, 257, 7), (900, 512, 8), (130, 513, 31), (300, 400, 40), (90, 1000, 3), (65, 1025, 4), (30, 4097, 64),
          (66, 8192, 8), (5000, 16, 2), (20001, 7, 3), (70001, 12, 2), (131073, 4, 1)]
 
 
