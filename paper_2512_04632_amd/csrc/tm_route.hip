@@ -288,15 +288,17 @@ __global__ __launch_bounds__(route_threads<L>(), L > 64 ? 1 : 4) void k_route(co
     __syncthreads();
     auto active = [&](int at) { return at < rows && (A.active == nullptr || A.active[first + at] != 0); };
     u32x4_t q[J];
+    constexpr bool AHEAD = T::kBytes == 2 || J < 4;   // registers
     bool on = active(grp);
-    if (on) H::load(A.logits + (first + grp) * A.ld * T::kBytes, t, experts, q);
+    if (AHEAD && on) H::load(A.logits + (first + grp) * A.ld * T::kBytes, t, experts, q);
     for (int at = grp; at < rows; at += G) {
       const bool now = on;
       float v[N];
+      if (!AHEAD && now) H::load(A.logits + (first + at) * A.ld * T::kBytes, t, experts, q);
       if (now) H::values(q, t, experts, v);
       // the next row is on its way while this one is worked on
       on = active(at + G);
-      if (on) H::load(A.logits + (first + at + G) * A.ld * T::kBytes, t, experts, q);
+      if (AHEAD && on) H::load(A.logits + (first + at + G) * A.ld * T::kBytes, t, experts, q);
       if (!now) {
         if (t == 0) whole[at] = -1.f;
         continue;
@@ -571,32 +573,95 @@ __global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A) {
 
 constexpr int kThreads = 256;
 
+// What the lanes of a row have written in LDS the others read.
+template <int L>
+__device__ inline void group_sync() {
+  if constexpr (L > 64) __syncthreads();
+  else wave_sync();
+}
+
+// Backward: the row's lanes take a choice each (L at a time) and put its share of the gradient where the expert's lane
+// finds it.  A choice that the caller names twice counts twice, in the order of the choices.
 template <class T, int L, int J>
-__global__ __launch_bounds__(kThreads) void k_route_backward(const RouteGradArgs A) {
+__global__ __launch_bounds__(kThreads, L > 64 ? 1 : 4) void k_route_backward(const RouteGradArgs A) {
   using H = Held<T, L, J>;
   constexpr int N = H::N, G = kThreads / L;
   __shared__ Slots<L> slots;
-  const int t = threadIdx.x % L, experts = A.experts, top = A.top;
+  __shared__ __attribute__((aligned(16))) float extra[G][H::MOST];
+  __shared__ int2 picks[G][TM_MAX_TOP];   // expert and gradient
+  const int t = threadIdx.x % L, grp = threadIdx.x / L, experts = A.experts, top = A.top;
   const float used = float(A.ends[experts - 1]), taking = used / float(top);
   const float per = A.dbalance != nullptr && used > 0.f ? *A.dbalance * float(experts) / (used * taking) : 0.f;
   float u[N];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int e = H::place(t, n);
-    u[n] = e < experts ? per * float(A.ends[e] - (e > 0 ? A.ends[e - 1] : 0)) : 0.f;
+  for (int j = 0; j < J; ++j) {
+    const int first = (j * L + t) * T::W;
+    int last = first > 0 && first <= experts ? A.ends[first - 1] : 0;
+#pragma unroll
+    for (int i = 0; i < T::W; ++i) {
+      const int end = first + i < experts ? A.ends[first + i] : last;
+      u[j * T::W + i] = per * float(end - last);
+      last = end;
+    }
   }
-  for (int64_t r = int64_t(blockIdx.x) * G + threadIdx.x / L; r < A.rows; r += int64_t(gridDim.x) * G) {
+  for (int64_t r = int64_t(blockIdx.x) * G + grp; r < A.rows; r += int64_t(gridDim.x) * G) {
     const char* row = A.logits + r * A.ld * T::kBytes;
     char* out = A.dlogits + r * A.ldd * T::kBytes;
     const int32_t* chosen = A.chosen + r * top;
     const float* dw = A.dweights != nullptr ? A.dweights + r * top : nullptr;
-    float v[N], g[N], add[N];
-    const bool on = chosen[0] >= 0;
+    float v[N];
+    if (chosen[0] < 0) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = add[n] = 0.f;
-    if (on) {
+      for (int n = 0; n < N; ++n) v[n] = 0.f;
+    } else {
       u32x4_t q[J];
       H::load(row, t, experts, q);
+      // choice j of this lane: its expert (-1: none) and, of the gradients, dw scale
+      auto choice = [&](int j, float& at) {
+        const int e = j < top ? chosen[j] : -1;
+        at = j < top ? A.scale * dw[j] : 0.f;
+        return e >= 0 && e < experts ? e : -1;
+      };
+      float most = -INFINITY, whole = 0.f, mean = 0.f;
+      if (dw != nullptr && A.renormalize) {   // the chosen's softmax, about their own maximum
+        for (int j = t; j < top; j += L) {
+          float at;
+          const int e = choice(j, at);
+          if (e >= 0) most = fmaxf(most, T::load1(row + int64_t(e) * T::kBytes));
+        }
+        most = row_max<L>(most, slots);
+        for (int j = t; j < top; j += L) {
+          float at;
+          const int e = choice(j, at);
+          if (e < 0) continue;
+          const float p = expf(T::load1(row + int64_t(e) * T::kBytes) - most);
+          whole += p;
+          mean += p * at;
+        }
+        whole = row_sum<L>(whole, slots);
+        mean = row_sum<L>(mean, slots) / whole;
+      }
+      if (dw != nullptr) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) extra[grp][H::place(t, n)] = 0.f;
+        for (int j = t; j < top; j += L) {
+          float at;
+          const int e = choice(j, at);
+          if (e >= 0 && A.renormalize) at = expf(T::load1(row + int64_t(e) * T::kBytes) - most) / whole * (at - mean);
+          picks[grp][j] = make_int2(e, __float_as_int(at));
+        }
+        group_sync<L>();
+        for (int j = t; j < top; j += L) {
+          const int e = picks[grp][j].x;
+          float sum = 0.f;
+          for (int i = 0; i < top; ++i) {
+            const int2 p = picks[grp][i];
+            sum += p.x == e ? __int_as_float(p.y) : 0.f;
+          }
+          if (e >= 0) extra[grp][e] = sum;
+        }
+        group_sync<L>();
+      }
       H::values(q, t, experts, v);
       float m = v[0];
 #pragma unroll
@@ -605,49 +670,22 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(const RouteGradArgs
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        v[n] = H::place(t, n) < experts ? expf(v[n] - m) : 0.f;
+        v[n] = H::place(t, n) < experts ? __builtin_amdgcn_exp2f((v[n] - m) * kLog2e) : 0.f;
         sum += v[n];
-        g[n] = u[n];
       }
       sum = row_sum<L>(sum, slots);
       const float inv = 1.f / sum;
-      if (dw != nullptr) {
-        float most = -INFINITY, whole = 0.f, mean = 0.f;
-        if (A.renormalize) {   // about the chosen's own maximum
-          for (int j = 0; j < top; ++j) {
-            const int e = chosen[j];
-            if (e < 0 || e >= experts) continue;
-            const float l = T::load1(row + int64_t(e) * T::kBytes);
-            if (l > most) most = l;
-          }
-          for (int j = 0; j < top; ++j) {
-            const int e = chosen[j];
-            if (e < 0 || e >= experts) continue;
-            const float q = expf(T::load1(row + int64_t(e) * T::kBytes) - most);
-            whole += q;
-            mean += q * (A.scale * dw[j]);
-          }
-          mean /= whole;
-        }
-        for (int j = 0; j < top; ++j) {
-          const int e = chosen[j];
-          if (e < 0 || e >= experts) continue;
-          float at = A.scale * dw[j];
-          if (A.renormalize) at = expf(T::load1(row + int64_t(e) * T::kBytes) - most) / whole * (at - mean);
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-            if (H::place(t, n) == e) (A.renormalize ? add[n] : g[n]) += at;
-        }
-      }
-      float dot = 0.f;
+      float x[N], dot = 0.f;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
+        x[n] = dw != nullptr ? extra[grp][H::place(t, n)] : 0.f;
         v[n] *= inv;
-        dot += v[n] * g[n];
+        dot += v[n] * (A.renormalize ? u[n] : u[n] + x[n]);
       }
       dot = row_sum<L>(dot, slots);
 #pragma unroll
-      for (int n = 0; n < N; ++n) v[n] = v[n] * (g[n] - dot) + add[n];
+      for (int n = 0; n < N; ++n) v[n] = A.renormalize ? v[n] * (u[n] - dot) + x[n] : v[n] * (u[n] + x[n] - dot);
+      if (dw != nullptr) group_sync<L>();   // before the next row's zeros
     }
 #pragma unroll
     for (int j = 0; j < J; ++j) store_vec<T>(out, (j * L + t) * T::W, experts, v + j * T::W);
@@ -691,7 +729,7 @@ template <class T>
 hipError_t backward(const RouteGradArgs& A, hipStream_t st) {
   with_shape<T>(A.experts, [&](auto l, auto j) {
     constexpr int G = kThreads / decltype(l)::value;
-    const dim3 grid(uint32_t(std::min<int64_t>((int64_t(A.rows) + G - 1) / G, 2048)));
+    const dim3 grid(uint32_t(std::min<int64_t>((int64_t(A.rows) + G - 1) / G, 1024)));
     hipLaunchKernelGGL((k_route_backward<T, decltype(l)::value, decltype(j)::value>), grid, dim3(kThreads), 0, st, A);
   });
   return hipGetLastError();
