@@ -301,7 +301,7 @@ tm_status tm_rms_norm_backward(const void* dy, int64_t lddy, const void* s, int6
                                float* dweight, int64_t rows, int64_t d, int dtype, void* stream);
 
 /*
- * tm_expert_route (W) - the `top` experts of each row, by its scores l.  With
+ * tm_expert_route (W, more than 64 rows) - the `top` experts of each row, by its scores l.  With
  * p = softmax(l) over the experts and N rows that take part:
  *   chosen   rows x top: the experts of the `top` largest l, largest first; of equal
  *            ones the lowest index; NaN counts as -inf.
@@ -345,6 +345,7 @@ tm_status tm_expert_route_backward(const void* logits, int64_t ld, const int32_t
  *          ends), or NULL: all.  Rows from there on come out as zeros; one below it
  *          that no slot names is left as it was.
  * Whatever slots and *used hold, nothing outside the matrices is read or written.
+ * out overlaps nothing that is read.
  */
 tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, const int32_t* used, void* out,
                            int64_t ldo, int64_t count, int64_t rows, int64_t top, int64_t d, int dtype,
@@ -357,7 +358,7 @@ tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, con
  *   weights   rows x top, or NULL: ones (what the gradient of tm_expert_gather is).
  *   residual  rows x d, or NULL.
  *   Slots that are negative or not below count are left out; the same one may be
- *   named twice.  out may be the residual (same stride).
+ *   named twice.  out may be the residual (same stride), and overlaps nothing else.
  */
 tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
                             const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count,
@@ -417,7 +418,8 @@ tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t ld
                           int64_t k, int64_t n, int dtype, int out_dtype, void* stream);
 
 /*
- * tm_token_logp (W) - over rows of logits l with target y, at temperature tau, with
+ * tm_token_logp (W, rows that are cut: up to 128 of more than 200 KB, and any of
+ * more than 512 KB) - over rows of logits l with target y, at temperature tau, with
  * m = max_v l_v and s = sum_v exp((l_v - m) / tau):
  *   logp     log p_y = (l_y - m) / tau - log s,
  *   entropy  -sum_v p_v log p_v,

@@ -381,14 +381,14 @@ def expert_route_backward(logits, chosen, ends, dweights=None, dbalance=None, re
     return dlogits
 
 
-def _used(ends, index: int):
-    """Address of the last of the experts' ends: how many rows are filled (None: all)."""
+def _filled(ends, index: int):
+    """ends checked, or None; the address of its last entry, how many rows are filled."""
     if ends is None:
-        return None
+        return None, None
     ends = _ends(ends, index)
     if ends.shape[0] < 1:
         raise ValueError("ends must hold one entry per expert")
-    return ends.data_ptr() + 4 * (ends.shape[0] - 1)
+    return ends, ends.data_ptr() + 4 * (ends.shape[0] - 1)
 
 
 def _matrix(t, name: str):
@@ -408,10 +408,11 @@ def expert_gather(x, slots, ends=None, stream=None):
     code, index = _code(x, "x"), x.get_device()
     x2, rows, d, ldx = _matrix(x, "x")
     slots = _table(slots, index, "slots", rows, None, _I32)
+    ends, used = _filled(ends, index)
     top = slots.shape[1]
     out = x.new_empty_strided((rows * top, d), (d, 1))
-    _call("tm_expert_gather", index, x2.data_ptr(), ldx, slots.data_ptr(), _used(ends, index), out.data_ptr(), d,
-          rows * top, rows, top, d, code)
+    _call("tm_expert_gather", index, x2.data_ptr(), ldx, slots.data_ptr(), used, out.data_ptr(), d, rows * top, rows,
+          top, d, code)
     return out
 
 
@@ -456,10 +457,11 @@ def expert_combine_backward(dout, y, slots, ends=None, weights=None, weight_grad
     top = slots.shape[1]
     if weights is not None:
         weights = _table(weights, index, "weights", rows, top, _F32)
+    ends, used = _filled(ends, index)
     dy = y.new_empty_strided((count, d), (d, 1))
     dweights = y.new_empty_strided((rows, top), (top, 1), dtype=_F32) if weight_grads else None
     _call("tm_expert_combine_backward", index, g2.data_ptr(), ldg, y2.data_ptr(), ldy, slots.data_ptr(),
-          _used(ends, index), _ptr(weights), dy.data_ptr(), d, _ptr(dweights), count, rows, top, d, code)
+          used, _ptr(weights), dy.data_ptr(), d, _ptr(dweights), count, rows, top, d, code)
     return dy, dweights
 
 

@@ -268,10 +268,11 @@ tm_status expert_route(const void* logits, int64_t ld, const uint8_t* active, in
   A.renormalize = renormalize != 0;
   A.scale = scale;
   tmk::plan_route(A);
-  // workspace: the blocks' counts and sums of probabilities, lines of whole vectors
+  // workspace: the blocks' counts and sums of probabilities, lines of whole vectors; none for a single block
   const uint64_t entries = uint64_t(A.blocks) * ((uint64_t(experts) + 7u) / 8u * 8u);
   const uint64_t dots = 256u + tmk::align256(uint64_t(A.blocks) * sizeof(double)), counts = tmk::align256(entries * sizeof(uint16_t));
-  return run_op(TM_PHASE_EXPERT_ROUTE, size_t(dots + counts + entries * sizeof(float)), stream, [&](char* ws, hipStream_t st) {
+  const uint64_t bytes = A.blocks > 1 ? dots + counts + entries * sizeof(float) : 0u;
+  return run_op(TM_PHASE_EXPERT_ROUTE, size_t(bytes), stream, [&](char* ws, hipStream_t st) {
     A.arrived = reinterpret_cast<int32_t*>(ws);
     A.dots = reinterpret_cast<double*>(ws + 256u);
     A.counts = reinterpret_cast<uint16_t*>(ws + dots);

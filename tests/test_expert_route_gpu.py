@@ -253,6 +253,31 @@ def test_autograd_and_differences():
                                                                 renormalize=renormalize))
 
 
+def test_more_rows_than_16_bits_of_counts_hold_eight_times():
+    log("case: route 8400000 x 4")
+    logits = _logits(8400000, 4, "f32", seed=11)
+    _check(tm.expert_route(logits, 1), logits, 1)
+
+
+def test_equal_scores_everywhere():
+    """A router that starts at zero: every row takes the first experts."""
+    for experts in (5, 64, 256, 300, 1000, 1500):
+        logits = torch.zeros((130, experts), device="cuda")
+        got = tm.expert_route(logits, 4)
+        _check(got, logits, 4)
+        assert (got[0] == torch.arange(4, device="cuda")).all() and abs(float(got[4]) - 1.0) < 1e-5
+
+
+def test_ends_of_other_strides():
+    logits = _logits(100, 6, "f32", seed=12)
+    chosen, _, slots, ends, _ = tm.expert_route(logits, 2)
+    apart = torch.stack([ends, 0 * ends], 1)[:, 0]
+    x = torch.randn((100, 33), generator=generator(13), device="cuda")
+    assert torch.equal(tm.expert_gather(x, slots, ends), tm.expert_gather(x, slots, apart))
+    assert torch.equal(tm.expert_route_backward(logits, chosen, ends, None, torch.ones((), device="cuda")),
+                       tm.expert_route_backward(logits, chosen, apart, None, torch.ones((), device="cuda")))
+
+
 def test_no_rows_and_refusals():
     logits = _logits(6, 5, "f32")
     chosen, weights, slots, ends, balance = tm.expert_route(logits[:0], 2)

@@ -116,6 +116,11 @@ def test_in_place(rows, d, dtype):
         assert tm.lib().tm_rms_norm(x.data_ptr(), d, r.data_ptr(), d, t["weight"].data_ptr(), to_s.data_ptr(), d,
                                     to_y.data_ptr(), d, scale.data_ptr(), rows, d, 1e-5, code, st) == 0
         assert torch.equal(to_s, s) and torch.equal(to_y, y) and torch.equal(scale, rstd)
+    x, scale = t["x"].clone(), torch.empty_like(rstd)
+    alone = tm.rms_norm(x, t["weight"])
+    assert tm.lib().tm_rms_norm(x.data_ptr(), d, None, 0, t["weight"].data_ptr(), None, 0, x.data_ptr(), d, scale.data_ptr(),
+                                rows, d, 1e-5, code, st) == 0
+    assert torch.equal(x, alone[0]) and torch.equal(scale, alone[2])
     for k in range(3):
         arrays = [t["dy"].clone(), s.clone(), t["dsum"].clone()]
         got = torch.empty_like(dw)

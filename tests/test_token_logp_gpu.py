@@ -92,7 +92,7 @@ def _check_gradient(s, got, stats, entropy, dlogp, dentropy, dtype, tau=TAU):
 # cut into parts; odd ones
 SIZES = [(1, 1, 1), (3, 2, 2), (5, 17, 5), (9, 64, 64), (1, 1000, 20), (700, 517, 3), (64, 1024, 1), (33, 1025, 20), (40, 2049, 8),
          (64, 4099, 20), (1, 8192, 64), (2, 50257, 20), (16, 50257, 5), (300, 8209, 20), (260, 24577, 20), (257, 50000, 1),
-         (256, 82000, 5), (255, 9000, 7), (600, 33001, 20), (3, 131072, 64), (1, 300001, 20), (270, 131080, 4), (2, 600011, 64)]
+         (256, 82000, 5), (255, 9000, 7), (600, 33001, 20), (3, 131072, 64), (1, 300001, 20), (270, 131080, 4), (2, 600011, 64), (130, 270001, 5), (100, 110000, 20)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
