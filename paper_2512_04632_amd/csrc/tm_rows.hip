@@ -224,12 +224,15 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A)
   zero_rest<T, L>(A, used);
 }
 
-// f(L) with the threads of a row.
+// f(L) with the threads of a row: what wastes least of them, vecs being a row's 16-byte parts.  A wave of 64 up to 192
+// (20000 rows of 125 parts to 4 slots: 41 us gathered and 45 joined, 51 and 59 with 256 threads a row; 129 parts: 30 and
+// 40 against 31 and 52), 256 beyond (8192 rows of 256 parts, 8 slots: 53 and 66 us, a wave 74 and 72; 4096 columns to 2
+// slots: 68, a wave 73; 16 such rows: 7 against 12); at 192 itself they are alike.  16 threads for the narrowest.
 template <class T, class F>
 void with_lanes(int d, F f) {
   const int vecs = (d + T::W - 1) / T::W;
   if (vecs <= 16) f(std::integral_constant<int, 16>{});
-  else if (vecs <= 256) f(std::integral_constant<int, 64>{});
+  else if (vecs <= 192) f(std::integral_constant<int, 64>{});
   else f(std::integral_constant<int, 256>{});
 }
 
