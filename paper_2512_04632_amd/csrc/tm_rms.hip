@@ -268,14 +268,23 @@ __global__ __launch_bounds__(256) void k_rms_columns(const RmsArgs A, int slices
   A.part[int64_t(blockIdx.y) * A.d + c] = aw;
 }
 
-// Workgroups of the forward pass, as for layer norm.
-inline int rms_blocks(int d) { return d <= 4096 ? 2048 : d <= 8192 ? 512 : 256; }
+// Most workgroups.  One a CU, where 16 KB or more are on the way to each while a row is worked on: that covers the
+// latency, and fewer streams of reads and writes take turns at the memory (16384 rows with residual, us, 256 / 2048 /
+// 4096 workgroups: 4096 bf16 92 / 105 / 101, 5120 bf16 119 / 128 / 124, 2048 fp32 92 / 104 / 101; backwards, 256 / 512:
+// 97 / 106, 125 / 137, 95 / 102).  Where it is less, more (16384 x 2500 bf16 117 / 64 / 63, backwards 95 / 68).  So do
+// rows of a wave forwards, whose loads are not that long (16384 x 1024 bf16 24 / 22 / 21).  Backwards each workgroup
+// has its line of partial sums, and the gradients' two streams, which are always there, are counted.
+template <class T>
+int rms_blocks(const RmsArgs& A) {
+  return A.d > 1024 && A.d * T::kBytes * (A.residual != nullptr ? 2 : 1) >= 16384 ? 256 : 4096;
+}
+inline int most_lines(int64_t d, bool f32) { return d * (f32 ? 4 : 2) * (d <= 1024 ? 4 : 1) >= 8192 ? 256 : 512; }
 constexpr int kRmsWideBlocks = 2048;
 
 template <class T, int NT, int E>
 hipError_t rms(const RmsArgs& A, hipStream_t st) {
   constexpr int RB = block_threads<NT>() / NT;
-  const dim3 grid(uint32_t(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, rms_blocks(A.d)))), block(block_threads<NT>());
+  const dim3 grid(uint32_t(std::min<int64_t>((int64_t(A.rows) + RB - 1) / RB, rms_blocks<T>(A)))), block(block_threads<NT>());
   const bool tail = A.d % T::W != 0, res = A.residual != nullptr;
   if (tail && res) hipLaunchKernelGGL((k_rms<T, NT, E, true, true>), grid, block, 0, st, A);
   else if (tail) hipLaunchKernelGGL((k_rms<T, NT, E, true, false>), grid, block, 0, st, A);
@@ -338,10 +347,12 @@ hipError_t rms_backward_t(const RmsArgs& A, int blocks, hipStream_t st) {
 
 }  // namespace norm
 
-// As norm_blocks, with the narrow rows' sixteen a workgroup.
+// As norm_blocks (a few rows are summed by one workgroup, which saves a launch), with sixteen narrow rows a workgroup.
 int rms_backward_blocks(int64_t rows, int64_t d, bool f32) {
-  if (d > norm::kNarrow) return norm_blocks(rows, d, f32);
-  return rows <= 64 ? rows > 0 : int(std::min<int64_t>((rows + 15) / 16, 512));
+  if (d > kNormMaxFused) return norm_blocks(rows, d, f32);
+  const int64_t held = d <= norm::kNarrow ? 16 : d <= 1024 ? 4 : 1;
+  if (rows <= 4 * held) return rows > 0;
+  return int(std::min<int64_t>((rows + held - 1) / held, norm::most_lines(d, f32)));
 }
 
 hipError_t launch_rms(const RmsArgs& A, bool f32, hipStream_t st) {
