@@ -11,12 +11,15 @@
 //             renormalised: dl = p (u - sum p u); renormalised, the chosen share a softmax of
 //             their own, q = w / scale: q_j (scale dw_j - sum q scale dw) is added at them
 //
-// Forward in two launches.  The first holds each row in the registers of L lanes, which
-// take the maximum `top` times; a block marks a choice with the row's bit in a word of 64 per
-// expert, so that a choice's place among the block's is a count of the bits below it, and
-// no order of atomics shows.  The second adds up the blocks' counts (16 bits each) and moves every
-// choice by what lies before its block.  Sums of probabilities are fp32 over a block's rows,
-// 64-bit over the blocks, in a fixed order.
+// Forward: rows are held in the registers of 16, 32, 64 or 256 lanes, which take the maximum `top` times; a block of 64
+// rows marks a choice with the row's bit in a word of 64 per expert, so that a choice's place among the block's is a
+// count of the bits below it, and no order of atomics shows.  Up to 64 rows are one block, which knows all places, ends
+// and the loss at once.  Else a second launch adds up the blocks' counts (16 bits each) and moves every choice by what lies
+// before its block.  Sums of probabilities are fp32 over a block's rows, 64-bit over the blocks, in a fixed order.
+//
+// Bound by instructions and by latency, not by memory: 32768 x 256 fp32, 8 chosen, reads 34 MB and writes 3 (7 us at the
+// rate of a copy) and takes 27 us, 17 of it the choices (about 22 instructions for each score, 18 of them the rounds) and
+// 10 the second launch, whose steps wait for one another.  64 rows x 8 take 11 us of the host for 6 of the kernel.
 #include <algorithm>
 
 #include "tm_elem.h"
@@ -581,15 +584,17 @@ __device__ inline void group_sync() {
 }
 
 // Backward: the row's lanes take a choice each (L at a time) and put its share of the gradient where the expert's lane
-// finds it.  A choice that the caller names twice counts twice, in the order of the choices.
+// finds it.  A choice that the caller names twice counts twice, in the order of the choices.  32768 rows of 256 experts,
+// 8 of fp32, 21 us and 67 MB: bound by the row's chain of loads, six reductions and LDS, about 600 vector
+// instructions a wave for four rows; 73% of the waves' time was waiting with nothing of the next row read ahead (24 us).
 template <class T, int L, int J>
 __global__ __launch_bounds__(kThreads, L > 64 ? 1 : 4) void k_route_backward(const RouteGradArgs A) {
   using H = Held<T, L, J>;
   constexpr int N = H::N, G = kThreads / L;
   __shared__ Slots<L> slots;
   __shared__ __attribute__((aligned(16))) float extra[G][H::MOST];
-  __shared__ int2 picks[G][TM_MAX_TOP];   // expert and gradient
-  const int t = threadIdx.x % L, grp = threadIdx.x / L, experts = A.experts, top = A.top;
+  __shared__ __attribute__((aligned(16))) int2 picks[G][TM_MAX_TOP];   // expert and gradient, to whole runs of four
+  const int t = threadIdx.x % L, grp = threadIdx.x / L, experts = A.experts, top = A.top, wide = (top + 3) / 4 * 4;
   const float used = float(A.ends[experts - 1]), taking = used / float(top);
   const float per = A.dbalance != nullptr && used > 0.f ? *A.dbalance * float(experts) / (used * taking) : 0.f;
   float u[N];
@@ -604,65 +609,92 @@ __global__ __launch_bounds__(kThreads, L > 64 ? 1 : 4) void k_route_backward(con
       last = end;
     }
   }
-  for (int64_t r = int64_t(blockIdx.x) * G + grp; r < A.rows; r += int64_t(gridDim.x) * G) {
+  constexpr bool AHEAD = T::kBytes == 2 || J < 4;   // registers
+  const int64_t step = int64_t(gridDim.x) * G;
+  int64_t r = int64_t(blockIdx.x) * G + grp;
+  // a row's values, whether it takes part, and this lane's first choice: its expert (-1: none) and, of the gradients,
+  // dw scale.  The next row's are on their way while this one is worked on.
+  u32x4_t q[J];
+  int part = -1, own = -1;
+  float own_at = 0.f;
+  const bool gradients = A.dweights != nullptr, shared = gradients && A.renormalize;
+  auto read = [&](int64_t at) __attribute__((always_inline)) {
+    part = A.chosen[at * top];
+    if (gradients && t < top) {
+      own = A.chosen[at * top + t];
+      own_at = A.dweights[at * top + t];
+    }
+    if constexpr (AHEAD) H::load(A.logits + at * A.ld * T::kBytes, t, experts, q);
+  };
+  if (r < A.rows) read(r);
+  for (; r < A.rows; r += step) {
     const char* row = A.logits + r * A.ld * T::kBytes;
     char* out = A.dlogits + r * A.ldd * T::kBytes;
-    const int32_t* chosen = A.chosen + r * top;
-    const float* dw = A.dweights != nullptr ? A.dweights + r * top : nullptr;
     float v[N];
-    if (chosen[0] < 0) {
+    if constexpr (!AHEAD) H::load(row, t, experts, q);
+    const bool on = part >= 0;
+    const int first = own >= 0 && own < experts ? own : -1;
+    const float first_at = A.scale * own_at;
+    float first_l = -INFINITY;
+    if (on && shared && first >= 0) first_l = T::load1(row + int64_t(first) * T::kBytes);
+    H::values(q, t, experts, v);
+    if (r + step < A.rows) read(r + step);
+    if (!on) {
 #pragma unroll
       for (int n = 0; n < N; ++n) v[n] = 0.f;
     } else {
-      u32x4_t q[J];
-      H::load(row, t, experts, q);
-      // choice j of this lane: its expert (-1: none) and, of the gradients, dw scale
-      auto choice = [&](int j, float& at) {
-        const int e = j < top ? chosen[j] : -1;
-        at = j < top ? A.scale * dw[j] : 0.f;
-        return e >= 0 && e < experts ? e : -1;
+      // choice j of this lane
+      auto choice = [&](int j, float& at, float& l) __attribute__((always_inline)) {
+        if (j < L) {
+          at = first_at;
+          l = first_l;
+          return first;
+        }
+        const int e = A.chosen[r * top + j];
+        const bool there = e >= 0 && e < experts;
+        at = A.scale * A.dweights[r * top + j];
+        l = there && shared ? T::load1(row + int64_t(e) * T::kBytes) : -INFINITY;
+        return there ? e : -1;
       };
       float most = -INFINITY, whole = 0.f, mean = 0.f;
-      if (dw != nullptr && A.renormalize) {   // the chosen's softmax, about their own maximum
-        for (int j = t; j < top; j += L) {
-          float at;
-          const int e = choice(j, at);
-          if (e >= 0) most = fmaxf(most, T::load1(row + int64_t(e) * T::kBytes));
-        }
+      if (shared) {   // the chosen's softmax, about their own maximum
+        float at, l;
+        for (int j = t; j < top; j += L)
+          if (choice(j, at, l) >= 0) most = fmaxf(most, l);
         most = row_max<L>(most, slots);
         for (int j = t; j < top; j += L) {
-          float at;
-          const int e = choice(j, at);
-          if (e < 0) continue;
-          const float p = expf(T::load1(row + int64_t(e) * T::kBytes) - most);
+          if (choice(j, at, l) < 0) continue;
+          const float p = expf(l - most);
           whole += p;
           mean += p * at;
         }
         whole = row_sum<L>(whole, slots);
         mean = row_sum<L>(mean, slots) / whole;
       }
-      if (dw != nullptr) {
+      if (gradients) {
 #pragma unroll
         for (int n = 0; n < N; ++n) extra[grp][H::place(t, n)] = 0.f;
-        for (int j = t; j < top; j += L) {
-          float at;
-          const int e = choice(j, at);
-          if (e >= 0 && A.renormalize) at = expf(T::load1(row + int64_t(e) * T::kBytes) - most) / whole * (at - mean);
+        for (int j = t; j < wide; j += L) {
+          float at = 0.f, l;
+          const int e = j < top ? choice(j, at, l) : -1;
+          if (e >= 0 && shared) at = expf(l - most) / whole * (at - mean);
           picks[grp][j] = make_int2(e, __float_as_int(at));
         }
         group_sync<L>();
         for (int j = t; j < top; j += L) {
           const int e = picks[grp][j].x;
           float sum = 0.f;
-          for (int i = 0; i < top; ++i) {
-            const int2 p = picks[grp][i];
+          for (int i = 0; i < wide; i += 4) {
+            const int4 p = *reinterpret_cast<const int4*>(&picks[grp][i]), q = *reinterpret_cast<const int4*>(&picks[grp][i + 2]);
             sum += p.x == e ? __int_as_float(p.y) : 0.f;
+            sum += p.z == e ? __int_as_float(p.w) : 0.f;
+            sum += q.x == e ? __int_as_float(q.y) : 0.f;
+            sum += q.z == e ? __int_as_float(q.w) : 0.f;
           }
           if (e >= 0) extra[grp][e] = sum;
         }
         group_sync<L>();
       }
-      H::values(q, t, experts, v);
       float m = v[0];
 #pragma unroll
       for (int n = 1; n < N; ++n) m = fmaxf(m, v[n]);
@@ -675,17 +707,17 @@ __global__ __launch_bounds__(kThreads, L > 64 ? 1 : 4) void k_route_backward(con
       }
       sum = row_sum<L>(sum, slots);
       const float inv = 1.f / sum;
-      float x[N], dot = 0.f;
+      auto more = [&](int n) __attribute__((always_inline)) { return gradients ? extra[grp][H::place(t, n)] : 0.f; };
+      float dot = 0.f;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        x[n] = dw != nullptr ? extra[grp][H::place(t, n)] : 0.f;
         v[n] *= inv;
-        dot += v[n] * (A.renormalize ? u[n] : u[n] + x[n]);
+        dot += v[n] * (A.renormalize ? u[n] : u[n] + more(n));
       }
       dot = row_sum<L>(dot, slots);
 #pragma unroll
-      for (int n = 0; n < N; ++n) v[n] = A.renormalize ? v[n] * (u[n] - dot) + x[n] : v[n] * (u[n] + x[n] - dot);
-      if (dw != nullptr) group_sync<L>();   // before the next row's zeros
+      for (int n = 0; n < N; ++n) v[n] = A.renormalize ? v[n] * (u[n] - dot) + more(n) : v[n] * (u[n] + more(n) - dot);
+      if (gradients) group_sync<L>();   // before the next row's zeros
     }
 #pragma unroll
     for (int j = 0; j < J; ++j) store_vec<T>(out, (j * L + t) * T::W, experts, v + j * T::W);
@@ -729,6 +761,8 @@ template <class T>
 hipError_t backward(const RouteGradArgs& A, hipStream_t st) {
   with_shape<T>(A.experts, [&](auto l, auto j) {
     constexpr int G = kThreads / decltype(l)::value;
+    // as many as are resident, each of which reads `ends` once (us by 512, 1024 and 2048: 32768 x 256, 8 of fp32, 26, 24,
+    // 29; 65536 x 128, 6 of bf16, 32, 23, 27)
     const dim3 grid(uint32_t(std::min<int64_t>((int64_t(A.rows) + G - 1) / G, 1024)));
     hipLaunchKernelGGL((k_route_backward<T, decltype(l)::value, decltype(j)::value>), grid, dim3(kThreads), 0, st, A);
   });
