@@ -404,7 +404,9 @@ constexpr int kPlace = 1024;
 
 typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
 
-// SPAN blocks of k_route a workgroup, each a share of its threads; the first workgroup writes ends.  The balance loss is
+// SPAN blocks of k_route a workgroup, as many as leave one workgroup a CU or so, each a share of its threads (us of the
+// call by one, two and four: 32768 x 256 in 512 blocks 32, 28, 28; 16384 x 512 in 256 25, 25, 26; 45000 x 128 in 704
+// two 27, four 24); the first workgroup writes ends.  The balance loss is
 // added up by vectors of eight experts, dealt out among the workgroups, and by the last of these to arrive.
 template <int MOST, int SPAN>
 __global__ __launch_bounds__(kPlace) void k_route_place(const RouteArgs A) {
@@ -724,7 +726,10 @@ __global__ __launch_bounds__(kThreads, L > 64 ? 1 : 4) void k_route_backward(con
   }
 }
 
-// f(L, J) with the lanes of a row and vectors of each that hold `experts`.
+// f(L, J) with the lanes of a row and vectors of each that hold `experts`: the fewest lanes whose registers hold a row, as
+// the reductions over them cost more than the rounds in a lane (us, with twice the lanes: forward 32768 x 256, 8 of fp32,
+// 28 and 30, bf16 25 and 28, 16384 x 512 29 and 33, bf16 26 and 30, 65536 x 128, 6 of fp32, 27 and 34; 8192 x 1024 42, by
+// 256 lanes, which meet at barriers and pick fp32 exactly, 604; backward alike up to 512, 20 and 25 for 65536 x 128).
 template <class T, class F>
 void with_shape(int experts, F f) {
   using std::integral_constant;
