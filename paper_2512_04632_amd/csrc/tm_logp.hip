@@ -276,12 +276,21 @@ __device__ inline void write_none(const LogpArgs& A, int64_t r, int t) {
 }
 
 // ---------------------------------------------------------------- forward
+// The values of the lanes that hold alternatives.
+constexpr int kStaged = 24;
+template <int N>
+struct Staged {
+  __attribute__((aligned(16))) float value[kStaged][N];
+  int lane[kStaged];
+};
+
 // A wave per row, which holds it in registers, K vectors a lane.  (Waves that go on to other rows, the next one on its
 // way, are slower: what the compiler keeps from row to row takes the registers of half the waves.)
 template <class T, int K, bool TOP>
 __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   constexpr int W = T::W;
   __shared__ List lists[TOP ? 4 : 1];
+  __shared__ Staged<TOP ? K * W : 4> staged[TOP ? 4 : 1];
   const int lane = threadIdx.x & 63, n = A.vocab;
   const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (r >= A.rows) return;
@@ -304,8 +313,28 @@ __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
   if constexpr (TOP) {
     Picker pick(lists[threadIdx.x >> 6], A.top);
     pick.start(mine);
+    const uint64_t who = __ballot(mine >= pick.low);
+    const int lanes = __popcll(who);
+    if (lanes <= kStaged) {
+      // as few lanes as alternatives reach the bound, but for equal values: theirs alone, dealt out to all
+      Staged<K * W>& to = staged[threadIdx.x >> 6];
+      if (mine >= pick.low) {
+        const int at = __popcll(who & ((uint64_t(1) << lane) - 1));
+        to.lane[at] = lane;
 #pragma unroll
-    for (int e = 0; e < K * W; ++e) pick.push(v[e], ((e / W) * 64 + lane) * W + e % W);
+        for (int e = 0; e < K * W; e += 4) *reinterpret_cast<float4*>(&to.value[at][e]) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+      }
+      wave_sync();
+      for (int base = 0; base < lanes * K * W; base += 64) {
+        const int i = base + lane, at = i / (K * W), e = i % (K * W);
+        const bool there = at < lanes;
+        const float value = there ? to.value[at][e] : -INFINITY;
+        pick.push(value, ((e / W) * 64 + (there ? to.lane[at] : 0)) * W + e % W);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < K * W; ++e) pick.push(v[e], ((e / W) * 64 + lane) * W + e % W);
+    }
     pick.settle();
     write_top(A, r, pick, row);
   }
