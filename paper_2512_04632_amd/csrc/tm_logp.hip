@@ -9,8 +9,11 @@
 //   dl_v = (g ([v = y] - p_v) - h p_v (log p_v + H)) / tau,  p_v = exp(u_v) / s,
 //          g and h the gradients by logp and H
 //
-// The logits are read once.  Each thread keeps a running maximum and, in powers of 2,
-// the sums of e and of e u of what it has seen; they are joined at the end of a row.
+// The logits are read once.  Each thread keeps the maximum of what it has seen and, in
+// powers of 2, the sums of e and of e u about a value that follows the maximum at a
+// distance: they are moved to another value only when a logit is 2^24 times as likely as
+// it, so that hardly a row moves them twice.  (With a move for every vector 4096 x 131072
+// took 335 us, so 152.)  They are joined at the end of a row.
 // p log p of an entry without probability is zero: u is held at -200 there, where e
 // is zero.  Sums are fp32; backwards p comes from m and s themselves, not from a rounded
 // logarithm.
@@ -22,6 +25,12 @@
 // one lay outside, `top` groups would hold better ones.  One wave picks these groups, reads
 // them again and picks the entries, both times from those that reach a bound that `top` of
 // them are known to reach.  -inf and NaN are no alternatives.
+//
+// Long rows and the backward pass are bound by HBM (in brackets the bytes at the 5.04 TB/s of
+// a large copy): 4096 x 131072 bf16, 5 alternatives, a quarter of the rows without target,
+// 152 us (160).  Short rows by instructions: 32768 x 1000 bf16 16 us (13), with 5
+// alternatives 27, as picking is half of a row's instructions.  A few rows by chains of
+// waits: 16 x 50257 bf16 7 us in the kernel, with 20 alternatives 14, picked by one wave.
 #include <algorithm>
 
 #include "tm_elem.h"
@@ -284,7 +293,8 @@ struct Staged {
   int lane[kStaged];
 };
 
-// A wave per row, which holds it in registers, K vectors a lane.  (Waves that go on to other rows, the next one on its
+// A wave per row, which holds it in registers, K vectors a lane.  The alternatives lie in the lanes whose own best
+// reaches the bound (by all lanes' values one after the other 32768 x 1000 with 5 took 30 us, so 27).  (Waves that go on to other rows, the next one on its
 // way, are slower: what the compiler keeps from row to row takes the registers of half the waves.)
 template <class T, int K, bool TOP>
 __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
@@ -534,7 +544,8 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs A) {
 }
 
 // ---------------------------------------------------------------- backward
-// A workgroup per chunk of a row.  Rows without a gradient are not read.
+// A workgroup per chunk of a row.  Rows without a gradient are not read.  3000 x 32001 fp32, a tenth without one, 134 us
+// for 730 MB, 5.4 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void k_logp_gradient(const LogpArgs A) {
   const int64_t r = blockIdx.x / A.chunks;
