@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void k_logp_held(const LogpArgs A) {
 }
 
 // Most groups of a chunk; a wave has rows of kWaveBytes at most, and the less LDS, the more of them there are.
-constexpr int kGroups = 2048, kWaveBytes = 12 * 1024;
+constexpr int kGroups = 2048, kWaveBytes = 24 * 1024;
 template <class T>
 constexpr int group_size() { return 16 * T::W; }
 
@@ -608,8 +608,10 @@ void plan_logp(LogpArgs& A, bool f32) {
 }
 
 // Threads of a row; 0: a wave holds it, four rows a workgroup (us, with alternatives: 20000 x 2000 fp32 held 40, by
-// 64 threads 58, by 256 55; 10000 x 4099 bf16 by 64 threads 32, by 256 51, by 512 105; 10000 x 4096 fp32, 16 KB a row,
-// by 64 52, by 256 45; 4096 x 131072 bf16 by 256 152, by 1024 250).
+// 64 threads 58, by 256 55).  One wave up to 24 KB a row, as each wave has its share of joins and of work on less than a
+// whole step (10000 rows of bf16 by 64, 128 and 256 threads: 4099 29, 35, 51; 8000 45, 52, 66; 10000 53, 52, 60; 16384
+// 70, 64, 67; 6000 x 6000 fp32 33 each).  Not more than 256 (4096 x 131072 bf16 by 256 152, by 1024 250; a few
+// rows by 256 to 1024 alike).
 int logp_threads(const LogpArgs& A, bool f32) {
   const int64_t bytes = int64_t(A.chunk) * (f32 ? 4 : 2);
   if (A.chunks == 1 && A.vocab <= 2048) return 0;

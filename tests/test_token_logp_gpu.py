@@ -1,8 +1,9 @@
 """Token log probabilities, entropies and alternatives on the GPU against their definition in 64 bits.
 
-Places of alternatives have to be equal.  Tolerances (u = 2^-24): a thread adds up at most n = min(256, V / 256 + 32) terms
-and moves its sums to another maximum at most n / 4 times, by a product of three roundings; some thirty joins follow; with
-Z the largest distance over tau of a logit from its row's maximum, exponentials and moves are off by 8 Z u more: the sum of
+Places of alternatives have to be equal.  Tolerances (u = 2^-24): a thread's longest chain of additions has at most
+n = min(256, V / 256 + 32) terms (64 threads: 16 of each 32 values in a chain, then V / 2048 such sums), and it moves its
+sums to another maximum at most n / 4 times, by a product of three roundings; some thirty joins follow; with Z the largest
+distance over tau of a logit from its row's maximum, exponentials and moves are off by 8 Z u more: the sum of
 exponentials, and so a logarithm, by D = (2 n + 100 + 8 Z) u.  The sum of e u is off by as much of the sum of sizes."""
 import pytest
 
@@ -92,7 +93,8 @@ def _check_gradient(s, got, stats, entropy, dlogp, dentropy, dtype, tau=TAU):
 # cut into parts; odd ones
 SIZES = [(1, 1, 1), (3, 2, 2), (5, 17, 5), (9, 64, 64), (1, 1000, 20), (700, 517, 3), (64, 1024, 1), (33, 1025, 20), (40, 2049, 8),
          (64, 4099, 20), (1, 8192, 64), (2, 50257, 20), (16, 50257, 5), (300, 8209, 20), (260, 24577, 20), (257, 50000, 1),
-         (256, 82000, 5), (255, 9000, 7), (600, 33001, 20), (3, 131072, 64), (1, 300001, 20), (270, 131080, 4), (2, 600011, 64), (130, 270001, 5), (100, 110000, 20)]
+         (256, 82000, 5), (255, 9000, 7), (600, 33001, 20), (3, 131072, 64), (1, 300001, 20), (270, 131080, 4), (2, 600011, 64), (130, 270001, 5), (100, 110000, 20),
+         (200, 6144, 20), (200, 6145, 64), (150, 12288, 64), (150, 12289, 5)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
