@@ -357,12 +357,14 @@ tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, con
  *   y         count x d;  out  rows x d.
  *   weights   rows x top, or NULL: ones (what the gradient of tm_expert_gather is).
  *   residual  rows x d, or NULL.
- *   Slots that are negative or not below count are left out; the same one may be
- *   named twice.  out may be the residual (same stride), and overlaps nothing else.
+ *   used      device int32: rows of y that are filled, or NULL: all.
+ *   Slots that are negative or not below *used are left out (nor below count, whatever
+ *   *used holds); the same one may be named twice.  out may be the residual (same
+ *   stride), and overlaps nothing else.
  */
-tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
-                            const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count,
-                            int64_t rows, int64_t top, int64_t d, int dtype, void* stream);
+tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const int32_t* used,
+                            const float* weights, const void* residual, int64_t ldr, void* out, int64_t ldo,
+                            int64_t count, int64_t rows, int64_t top, int64_t d, int dtype, void* stream);
 
 /*
  * tm_expert_combine_backward - dy[slots[i, j], :] = weights[i, j] dout[i, :],

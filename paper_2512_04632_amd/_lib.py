@@ -82,8 +82,8 @@ _SIGNATURES = {
                                                 _i64, _i64, _i64, ctypes.c_int, _vp]),
     "tm_expert_gather": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int,
                                         _vp]),
-    "tm_expert_combine": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64,
-                                         ctypes.c_int, _vp]),
+    "tm_expert_combine": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64,
+                                         _i64, ctypes.c_int, _vp]),
     "tm_expert_combine_backward": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
                                                   _i64, _i64, _i64, ctypes.c_int, _vp]),
     "tm_token_logp": (ctypes.c_int, [_vp, _i64, _vp, _f32, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i64,

@@ -416,14 +416,15 @@ def expert_gather(x, slots, ends=None, stream=None):
     return out
 
 
-def expert_combine(y, slots, weights=None, residual=None, stream=None):
+def expert_combine(y, slots, weights=None, residual=None, ends=None, stream=None):
     """out[i] = residual[i] + sum over j of weights[i, j] y[slots[i, j]], summed in fp32.
 
     y is (count, d), bf16 or fp32; slots int32 and weights fp32 (None: ones) are (rows, top);
-    residual is (rows, d) of y's type, or None.  Slots that are negative or past y are left out.
+    residual is (rows, d) of y's type, or None.  Slots that are negative, or not
+    below ends[-1] (ends None: past y), are left out.
     """
     if stream is not None:
-        return _on(stream, y, expert_combine, y, slots, weights, residual)
+        return _on(stream, y, expert_combine, y, slots, weights, residual, ends)
     code, index = _code(y, "y"), y.get_device()
     y2, count, d, ldy = _matrix(y, "y")
     if slots.dim() != 2:
@@ -437,8 +438,9 @@ def expert_combine(y, slots, weights=None, residual=None, stream=None):
         if residual.shape != (rows, d) or residual.dtype is not y.dtype or residual.get_device() != index:
             raise ValueError(f"residual must be ({rows}, {d}) of y's type and device")
         r2, _, _, ldr = _rows(residual)
+    ends, used = _filled(ends, index)
     out = y.new_empty_strided((rows, d), (d, 1))
-    _call("tm_expert_combine", index, y2.data_ptr(), ldy, slots.data_ptr(), _ptr(weights), _ptr(r2), ldr,
+    _call("tm_expert_combine", index, y2.data_ptr(), ldy, slots.data_ptr(), used, _ptr(weights), _ptr(r2), ldr,
           out.data_ptr(), d, count, rows, top, d, code)
     return out
 

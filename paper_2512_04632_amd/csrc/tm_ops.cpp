@@ -348,7 +348,7 @@ tm_status expert_gather(const void* x, int64_t ldx, const int32_t* slots, const 
                 [&](char*, hipStream_t st) { return tmk::launch_gather(A, dtype == TM_DTYPE_F32, st); });
 }
 
-tm_status expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
+tm_status expert_combine(const void* y, int64_t ldy, const int32_t* slots, const int32_t* used, const float* weights,
                          const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count, int64_t rows,
                          int64_t top, int64_t d, int dtype, void* stream) {
   TM_CHECK(check_dtype("dtype", dtype));
@@ -358,9 +358,10 @@ tm_status expert_combine(const void* y, int64_t ldy, const int32_t* slots, const
   if (count > 0) TM_CHECK(check_strides({{"ldy", ldy, d}}));
   TM_CHECK(check_strides({{"ldo", ldo, d}}));
   if (residual != nullptr) TM_CHECK(check_strides({{"ldr", ldr, d}}));
-  TM_CHECK(check_pointers({{"y", y, esz, count == 0}, {"slots", slots, 4, false}, {"weights", weights, 4, true},
-                           {"residual", residual, esz, true}, {"out", out, esz, false}}));
+  TM_CHECK(check_pointers({{"y", y, esz, count == 0}, {"slots", slots, 4, false}, {"used", used, 4, true},
+                           {"weights", weights, 4, true}, {"residual", residual, esz, true}, {"out", out, esz, false}}));
   tmk::RowsArgs A = rows_args(slots, count, rows, top, d);
+  A.used = used;
   A.x = static_cast<const char*>(residual);
   A.y = static_cast<const char*>(y);
   A.weights = weights;
@@ -758,11 +759,11 @@ tm_status tm_expert_gather(const void* x, int64_t ldx, const int32_t* slots, con
   return guarded([&] { return expert_gather(x, ldx, slots, used, out, ldo, count, rows, top, d, dtype, stream); });
 }
 
-tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const float* weights,
-                            const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t count, int64_t rows,
-                            int64_t top, int64_t d, int dtype, void* stream) {
+tm_status tm_expert_combine(const void* y, int64_t ldy, const int32_t* slots, const int32_t* used,
+                            const float* weights, const void* residual, int64_t ldr, void* out, int64_t ldo,
+                            int64_t count, int64_t rows, int64_t top, int64_t d, int dtype, void* stream) {
   return guarded([&] {
-    return expert_combine(y, ldy, slots, weights, residual, ldr, out, ldo, count, rows, top, d, dtype, stream);
+    return expert_combine(y, ldy, slots, used, weights, residual, ldr, out, ldo, count, rows, top, d, dtype, stream);
   });
 }
 

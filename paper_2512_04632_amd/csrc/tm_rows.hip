@@ -122,16 +122,17 @@ template <class T, int L, int K, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_combine(const RowsArgs A) {
   constexpr int G = kThreads / L, W = T::W;
   const int t = threadIdx.x % L;
+  const int64_t used = used_of(A);
   for (int64_t at = int64_t(blockIdx.x) * G + threadIdx.x / L; at < A.rows; at += int64_t(gridDim.x) * G) {
     const int64_t r = row_of<L>(at);
     Choices<K> from;
-    if constexpr (ONE) from.read(A, r, 0, A.count, A.weights != nullptr);
+    if constexpr (ONE) from.read(A, r, 0, used, A.weights != nullptr);
     for (int c = t * W; c < A.d; c += L * W) {
       float acc[W] = {}, v[W];
       u32x4_t res = {0u, 0u, 0u, 0u};
       if (A.x != nullptr) res = load_ahead<T, true>(A.x + r * A.ldx * T::kBytes, c, A.d);
       for (int first = 0; first < (ONE ? 1 : A.top); first += K) {
-        if constexpr (!ONE) from.read(A, r, first, A.count, A.weights != nullptr);
+        if constexpr (!ONE) from.read(A, r, first, used, A.weights != nullptr);
         u32x4_t q[K];
 #pragma unroll
         for (int j = 0; j < K; ++j) {

@@ -101,7 +101,7 @@ class _ExpertGather(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         slots, ends = ctx.saved_tensors
-        return _lib.expert_combine(dout, slots), None, None
+        return _lib.expert_combine(dout, slots, ends=ends), None, None
 
 
 def expert_gather(x, slots, ends=None):
@@ -114,7 +114,7 @@ class _ExpertCombine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, slots, weights, residual, ends):
         ctx.save_for_backward(y, slots, weights, ends)
-        return _lib.expert_combine(y, slots, weights, residual)
+        return _lib.expert_combine(y, slots, weights, residual, ends)
 
     @staticmethod
     @once_differentiable
@@ -130,8 +130,9 @@ class _ExpertCombine(torch.autograd.Function):
 
 def expert_combine(y, slots, weights=None, residual=None, ends=None):
     """residual[i] + sum over j of weights[i, j] y[slots[i, j]]: the experts' results back in the rows'
-    order.  ends (expert_route's) says which rows of y are filled: the others' gradient is zero, and
-    without it every row of y has to be in a slot."""
+    order.  ends (expert_route's) says which rows of y are filled: the others have no part in it and a
+    gradient of zero; without it every row of y has to be in a slot.  For gradients no two slots may
+    be the same."""
     return _ExpertCombine.apply(y, slots, weights, residual, ends)
 
 

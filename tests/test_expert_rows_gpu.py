@@ -164,7 +164,7 @@ def test_strides_and_in_place(d, dtype):
         assert torch.equal(got[0], dy) and torch.equal(got[1], dw)
     code, st = (0 if dtype == "bf16" else 1), torch.cuda.current_stream().cuda_stream
     res, y, got = t["residual"].clone(), t["y"].clone(), torch.empty_like(dw)
-    assert tm.lib().tm_expert_combine(y.data_ptr(), d, t["slots"].data_ptr(), t["weights"].data_ptr(), res.data_ptr(), d,
+    assert tm.lib().tm_expert_combine(y.data_ptr(), d, t["slots"].data_ptr(), None, t["weights"].data_ptr(), res.data_ptr(), d,
                                       res.data_ptr(), d, 120, 40, 3, d, code, st) == 0
     assert torch.equal(res, back)
     used = t["ends"].data_ptr() + 8
@@ -218,6 +218,30 @@ def test_autograd_and_differences():
     x = t["x"].clone().requires_grad_()
     ops.expert_combine(ops.expert_gather(x, t["slots"], t["ends"]), t["slots"], ends=t["ends"]).sum().backward()
     assert torch.equal(x.grad, 3.0 * (t["slots"] >= 0).any(1)[:, None].expand(30, 50))
+
+
+def test_slots_past_the_filled_rows_have_no_part_and_no_gradient():
+    """Rows that are cut off: ends that stop before the last slots."""
+    for d in (50, 600, 1800):
+        t = _inputs(30, 3, d, "f32", seed=8)
+        ends = t["ends"].clamp(max=40)
+        cut = torch.where((t["slots"] >= 0) & (t["slots"] < 40), t["slots"], -1)
+        assert ((cut < 0) & (t["slots"] >= 0)).any()
+        leaves = {k: t[k].clone().requires_grad_() for k in ("x", "y", "weights", "residual")}
+        g1 = torch.randn((90, d), generator=generator(9), device="cuda")
+        out = ops.expert_gather(leaves["x"], t["slots"], ends)
+        back = ops.expert_combine(leaves["y"], t["slots"], leaves["weights"], leaves["residual"], ends)
+        assert torch.equal(tm.expert_combine(t["y"], cut, t["weights"], t["residual"]), back)
+        ((out * g1).sum() + (back * t["dout"]).sum()).backward()
+        wide = {k: t[k].double().requires_grad_() for k in leaves}
+        total = _combined(dict(t, y=wide["y"], slots=cut), wide["weights"], wide["residual"])[0]
+        ((_gathered(wide["x"], cut, 90) * g1.double()).sum() + (total * t["dout"].double()).sum()).backward()
+        assert not out[40:].any()
+        # sums of three terms or one; the weights' of d products, at most d / 16 of them by one lane, then joined
+        dots = float((t["dout"].abs().sum(1) * t["y"].abs().amax()).max())
+        off = {"weights": (d / 16 + 16) * U * dots}
+        for k, leaf in leaves.items():
+            assert torch.allclose(leaf.grad.double(), wide[k].grad, rtol=1e-5, atol=off.get(k, 1e-6)), k
 
 
 def test_nothing_to_do_and_refusals():

@@ -34,8 +34,8 @@ def _gather(x=P, ldx=8, slots=P, used=P, out=P, ldo=8, count=8, rows=4, top=2, d
     return tm.lib().tm_expert_gather(x, ldx, slots, used, out, ldo, count, rows, top, d, dtype, None)
 
 
-def _combine(y=P, ldy=8, slots=P, w=P, r=P, ldr=8, out=P, ldo=8, count=8, rows=4, top=2, d=8, dtype=1):
-    return tm.lib().tm_expert_combine(y, ldy, slots, w, r, ldr, out, ldo, count, rows, top, d, dtype, None)
+def _combine(y=P, ldy=8, slots=P, used=P, w=P, r=P, ldr=8, out=P, ldo=8, count=8, rows=4, top=2, d=8, dtype=1):
+    return tm.lib().tm_expert_combine(y, ldy, slots, used, w, r, ldr, out, ldo, count, rows, top, d, dtype, None)
 
 
 def _combine_back(g=P, ldg=8, y=P, ldy=8, slots=P, used=P, w=P, dy=P, lddy=8, dw=P, count=8, rows=4, top=2, d=8, dtype=1):
