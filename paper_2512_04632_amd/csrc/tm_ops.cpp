@@ -1,7 +1,6 @@
 // C entry points of the operators beside the orthogonalizer: argument checks,
 // workspace layout and launches.  Nothing is enqueued for a refused call, and
 // no exception leaves an entry point.
-#include <algorithm>
 #include <new>
 #include <string>
 
@@ -487,6 +486,9 @@ tm_status check_blocks(int64_t rows, int64_t chunks, uint64_t threads) {
   return TM_OK;
 }
 
+// Rows of a wave each, four to a workgroup, the last of which counts in full.
+tm_status check_quads(int64_t rows) { return check_blocks((rows + 3) / 4, 1, 256); }
+
 // Length of a chunk: whole 16-byte vectors of either type.
 int64_t chunk_length(int64_t vocab, int64_t chunks) { return ((vocab + chunks - 1) / chunks + 7) / 8 * 8; }
 
@@ -534,9 +536,9 @@ tm_status policy_loss(const void* logits, int64_t ld, const int64_t* targets, co
   A.kl = kl;
   A.inv_temp = 1.f / temperature;
   const int64_t chunks = empty ? 1 : tmk::loss_chunks(rows, vocab);
-  // threads of a row at most (launch_rows)
+  // threads of a row at most (launch_rows); short ones go four to a workgroup
   const int64_t line_bytes = vocab * int64_t(esz);
-  TM_CHECK(check_blocks(rows, chunks, line_bytes <= 4096 ? 64 : line_bytes <= 48 * 1024 ? 256 : 1024));
+  TM_CHECK(line_bytes <= 4096 ? check_quads(rows) : check_blocks(rows, chunks, line_bytes <= 48 * 1024 ? 256 : 1024));
   A.chunks = int32_t(chunks);
   A.chunk = int32_t(chunk_length(vocab, chunks));
   // workspace: the rows' shares of the loss, lse and slope where the caller
@@ -620,7 +622,8 @@ tm_status token_logp(const void* logits, int64_t ld, const int64_t* targets, flo
   A.top = int32_t(top);
   A.inv_temp = 1.f / temperature;
   tmk::plan_logp(A, dtype == TM_DTYPE_F32);
-  TM_CHECK(check_blocks(rows, A.chunks, uint64_t(std::max(tmk::logp_threads(A, dtype == TM_DTYPE_F32), 64))));
+  const int threads = tmk::logp_threads(A, dtype == TM_DTYPE_F32);   // 0: a wave holds a row
+  TM_CHECK(threads == 0 ? check_quads(rows) : check_blocks(rows, A.chunks, uint64_t(threads)));
   const uint64_t chunks = A.chunks > 1 ? uint64_t(rows) * uint64_t(A.chunks) : 0u;
   return run_op(TM_PHASE_TOKEN_LOGP, size_t(chunks * (sizeof(float4) + uint64_t(top) * 8u)), stream,
                 [&](char* ws, hipStream_t st) {

@@ -132,3 +132,13 @@ def test_limits_match_the_header():
     text = open(os.path.join(root, "include", "turbomuon.h")).read()
     d = {k: int(v) for k, v in re.findall(r"#define\s+(TM_MAX_\w+)\s+(\d+)", text)}
     assert d["TM_MAX_TOP"] == tm.TM_MAX_TOP
+
+
+@pytest.mark.parametrize("rows", [(1 << 26) - 3, (1 << 26) - 2, (1 << 26) - 1])
+def test_four_rows_a_workgroup_are_counted_as_the_workgroup_that_they_fill(rows):
+    """Rows of up to 2048 logits go four to a workgroup of 256: the last workgroup counts in full, and 2^24 of them are
+    one thread too many for a launch."""
+    for vocab in (2, 1000, 2048):
+        for dtype in (0, 1):
+            assert _logp(rows=rows, vocab=vocab, ld=vocab, top=min(vocab, 2), dtype=dtype) == UNSUPPORTED
+            assert "too many blocks" in tm.last_error()

@@ -106,3 +106,11 @@ def test_launches_past_32_bits_of_threads_are_refused(call, size):
     """A dispatch counts its threads in 32 bits: more would wrap."""
     assert call(**size) == UNSUPPORTED
     assert "too many blocks" in tm.last_error()
+
+
+@pytest.mark.parametrize("rows", [(1 << 26) - 3, (1 << 26) - 2, (1 << 26) - 1])
+@pytest.mark.parametrize("vocab,dtype", [(2, 0), (2048, 0), (2, 1), (1024, 1)])
+def test_four_rows_a_workgroup_count_as_one_that_is_full(rows, vocab, dtype):
+    """Short rows go four to a workgroup of 256: 2^24 workgroups are one thread too many for a launch."""
+    assert _loss(rows=rows, vocab=vocab, ld=vocab, ldd=vocab, dtype=dtype) == UNSUPPORTED
+    assert "too many blocks" in tm.last_error()
