@@ -397,11 +397,20 @@ def _matrix(t, name: str):
     return _rows(t)
 
 
+def _by_slot(like, count: int, d: int, ends):
+    """A matrix of `count` rows that go to their slots.  Which of them have one is known on the device alone: with `ends`
+    the library writes every row, those that it finds filled and zeros behind them; without, those that no slot names
+    would be what the memory held before, so they are zeros to begin with."""
+    return like.new_zeros((count, d)) if ends is None else like.new_empty_strided((count, d), (d, 1))
+
+
 def expert_gather(x, slots, ends=None, stream=None):
     """The rows of x (rows, d) in the experts' order: out[slots[i, j]] = x[i], of rows times top rows.
 
-    slots and ends are expert_route's; slots that are negative, or not below ends[-1], are none, and
-    the rows from ends[-1] on come out as zeros (ends None: every row has its slot).
+    slots and ends are expert_route's: every row below ends[-1] has its slot, slots that are negative,
+    or not below ends[-1], are none, and the rows from ends[-1] on come out as zeros.  For other slots
+    (choices taken out, gaps) leave `ends` out: rows that no slot names are zeros then, which
+    takes another pass over the result.
     """
     if stream is not None:
         return _on(stream, x, expert_gather, x, slots, ends)
@@ -410,7 +419,7 @@ def expert_gather(x, slots, ends=None, stream=None):
     slots = _table(slots, index, "slots", rows, None, _I32)
     ends, used = _filled(ends, index)
     top = slots.shape[1]
-    out = x.new_empty_strided((rows * top, d), (d, 1))
+    out = _by_slot(x, rows * top, d, ends)
     _call("tm_expert_gather", index, x2.data_ptr(), ldx, slots.data_ptr(), used, out.data_ptr(), d, rows * top, rows,
           top, d, code)
     return out
@@ -447,7 +456,8 @@ def expert_combine(y, slots, weights=None, residual=None, ends=None, stream=None
 
 def expert_combine_backward(dout, y, slots, ends=None, weights=None, weight_grads: bool = True, stream=None):
     """Gradients of expert_combine by y and the weights: (dy, dweights), the second None without
-    weight_grads.  dout is (rows, d) of y's type; ends as for expert_gather.  (The residual's is dout.)"""
+    weight_grads.  dout is (rows, d) of y's type; ends as for expert_gather: with it every row of y below
+    ends[-1] has to be in a slot, without it rows in no slot have a gradient of zero.  (The residual's is dout.)"""
     if stream is not None:
         return _on(stream, y, expert_combine_backward, dout, y, slots, ends, weights, weight_grads)
     code, index = _code(y, "y"), y.get_device()
@@ -460,7 +470,7 @@ def expert_combine_backward(dout, y, slots, ends=None, weights=None, weight_grad
     if weights is not None:
         weights = _table(weights, index, "weights", rows, top, _F32)
     ends, used = _filled(ends, index)
-    dy = y.new_empty_strided((count, d), (d, 1))
+    dy = _by_slot(y, count, d, ends)
     dweights = y.new_empty_strided((rows, top), (top, 1), dtype=_F32) if weight_grads else None
     _call("tm_expert_combine_backward", index, g2.data_ptr(), ldg, y2.data_ptr(), ldy, slots.data_ptr(),
           used, _ptr(weights), dy.data_ptr(), d, _ptr(dweights), count, rows, top, d, code)

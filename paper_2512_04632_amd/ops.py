@@ -106,7 +106,9 @@ class _ExpertGather(torch.autograd.Function):
 
 def expert_gather(x, slots, ends=None):
     """The rows of x in the experts' order, as expert_linear takes them: out[slots[i, j]] = x[i] for
-    expert_route's slots; zeros from ends[-1] on."""
+    expert_route's slots and ends; zeros from ends[-1] on.  Without ends, zeros in every row that no slot
+    names (another pass): so for slots with choices taken out, as with ends every row below ends[-1]
+    has to be in a slot."""
     return _ExpertGather.apply(x, slots, ends)
 
 
@@ -131,8 +133,8 @@ class _ExpertCombine(torch.autograd.Function):
 def expert_combine(y, slots, weights=None, residual=None, ends=None):
     """residual[i] + sum over j of weights[i, j] y[slots[i, j]]: the experts' results back in the rows'
     order.  ends (expert_route's) says which rows of y are filled: the others have no part in it and a
-    gradient of zero; without it every row of y has to be in a slot.  For gradients no two slots may
-    be the same."""
+    gradient of zero, and every one that is has to be in a slot.  Without it rows of y in no slot
+    have a gradient of zero (another pass).  For gradients no two slots may be the same."""
     return _ExpertCombine.apply(y, slots, weights, residual, ends)
 
 

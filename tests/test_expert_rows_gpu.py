@@ -3,6 +3,8 @@
 Rows on their way out are copied bit for bit.  Tolerances (u = 2^-24): a weighted sum of `top` rows and a residual is
 off by (top + 2) u of the sum of sizes and rounded once; a weight's gradient is a sum over the columns of at most
 d / 256 + 40 additions a thread and tree."""
+import contextlib
+
 import pytest
 
 from gpu_helpers import log
@@ -275,3 +277,68 @@ def test_nothing_to_do_and_refusals():
         tm.expert_gather(t["x"], t["slots"][:, :0])
     with pytest.raises(tm.TurboMuonError):
         tm.expert_combine(t["y"], torch.zeros((2, 65), dtype=torch.int32, device="cuda"))
+
+
+@contextlib.contextmanager
+def new_memory_is_nan():
+    """Tensors that torch allocates without filling them hold NaN (or the largest integer)."""
+    was = torch.are_deterministic_algorithms_enabled(), torch.utils.deterministic.fill_uninitialized_memory
+    torch.use_deterministic_algorithms(True)
+    torch.utils.deterministic.fill_uninitialized_memory = True
+    try:
+        yield
+    finally:
+        torch.use_deterministic_algorithms(was[0])
+        torch.utils.deterministic.fill_uninitialized_memory = was[1]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [3, 60, 1001, 3000])
+def test_rows_of_no_slot_are_zeros_where_no_ends_are_given(d, dtype):
+    """Masked rows, and choices that the caller has taken out, with `ends` left out: the rows that no slot names, of the
+    rows on their way out and of the gradients on their way back, are zeros and not what stood in their memory."""
+    log(f"case: rows without slots, no ends, 50 x {d} {dtype}")
+    t = _inputs(50, 3, d, dtype, seed=10)
+    count, slots, st = 150, t["slots"].clone(), torch.cuda.Stream()
+    slots[::4, 1] = -1                         # gaps below the last of the filled rows too
+    named = torch.zeros(count, dtype=torch.bool, device="cuda")
+    named[slots[slots >= 0].long()] = True
+    assert not named[:int(t["ends"][-1])].all() and not named[int(t["ends"][-1]):].any()
+    weights = torch.where(slots >= 0, t["weights"], 0)
+    want = _gathered(t["x"], slots, count)
+    dy_want = _gathered((weights[..., None] * t["dout"].float()[:, None]).to(DT[dtype]).view(150, d),
+                        slots.view(150, 1), count)
+    torch.cuda.synchronize()
+    with new_memory_is_nan():
+        assert t["x"].new_empty_strided((count, d), (d, 1)).isnan().all()
+        for stream in (None, st):
+            out = tm.expert_gather(t["x"], slots, stream=stream)
+            dy, dw = tm.expert_combine_backward(t["dout"], t["y"], slots, None, weights, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(dy, dy_want) and not dw[slots < 0].any()
+        x, y, w = (v.clone().requires_grad_() for v in (t["x"], t["y"], weights))
+        out = ops.expert_gather(x, slots)
+        ops.expert_combine(y, slots, w).backward(t["dout"])
+        assert torch.equal(out, want) and torch.equal(y.grad, dy_want) and torch.equal(w.grad, dw)
+
+
+def test_rows_of_no_slot_are_zeros_in_every_replay():
+    log("case: rows without slots, no ends, captured")
+    t, st = _inputs(40, 2, 500, "bf16", masked=0.3, seed=11), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        out = tm.expert_gather(t["x"], t["slots"])
+        dy, dw = tm.expert_combine_backward(t["dout"], t["y"], t["slots"], None, t["weights"])
+    for seed in (12, 13, 14):
+        other = _inputs(40, 2, 500, "bf16", masked=0.5, seed=seed)
+        for k, v in t.items():
+            v.copy_(other[k])
+        for a in (out, dy, dw):
+            a.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, _gathered(t["x"], t["slots"], 80)), seed
+        want = tm.expert_combine_backward(t["dout"], t["y"], t["slots"], t["ends"], t["weights"])
+        assert torch.equal(dy, want[0]) and torch.equal(dw, want[1]), seed
