@@ -301,3 +301,36 @@ def test_no_rows_and_refusals():
         assert e.value.status == tm.TM_ERR_INVALID_ARG
     with pytest.raises(tm.TurboMuonError):
         tm.expert_route(_logits(4, 200, "f32"), 65)
+
+
+# rows, experts, top, most rows that a block goes through: many blocks, some of several runs of 64 rows, at every
+# number of lanes a row
+MANY = [(20001, 300, 8, 64), (33001, 256, 8, 64), (60001, 400, 4, 128), (60001, 700, 3, 192), (9001, 1500, 2, 64),
+        (30001, 1500, 2, 192), (9001, 8000, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,experts,top,run", MANY)
+def test_many_rows_and_many_experts(rows, experts, top, run, dtype):
+    """Masked rows among them.  A probability is off by P of itself, as above without the additions; the balance is a
+    sum of them over at most `run` rows, the groups and waves of a block (16 more), and 64-bit sums."""
+    log(f"case: route many {rows} x {experts} top {top} {dtype}")
+    logits = _logits(rows, experts, dtype, seed=rows + experts)
+    g = generator(4)
+    active = torch.rand(rows, generator=g, device="cuda") < 0.8
+    clean = logits.clone()
+    logits[~active] = float("nan")
+    got = tm.expert_route(logits, top, active)
+    want = _exact(torch.where(active[:, None], clean, 0), top, active, True, 1.0)
+    assert torch.equal(got[0], want[0].int()) and torch.equal(got[2], want[2].int()) and torch.equal(got[3], want[3].int())
+    z = clean.double()
+    P = (4 * float((z.amax(1, keepdim=True) - z).clamp(max=110).amax()) + 64) * U
+    close("weights", got[1], want[1], 2 * P * want[1].abs() + 1e-37)
+    close("balance", got[4], want[4], (P + (run + 16 + 2) * U) * want[4].abs())
+    again = tm.expert_route(logits, top, active)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    dw = torch.randn((rows, top), generator=g, device="cuda")
+    db = torch.full((), 0.7, device="cuda")
+    back = tm.expert_route_backward(logits, got[0], got[3], dw, db)
+    assert not back[~active].any()
+    _check_gradient(back, clean, got[0], got[3], dw, db, True, 1.0, dtype)
