@@ -274,16 +274,25 @@ __global__ __launch_bounds__(256) void k_rms_columns(const RmsArgs A, int slices
 }
 
 // Most workgroups.  One a CU, where 16 KB or more are on the way to each while a row is worked on: that covers the
-// latency, and fewer streams of reads and writes take turns at the memory (16384 rows with residual, us, 256 / 2048 /
-// 4096 workgroups: 4096 bf16 92 / 105 / 101, 5120 bf16 119 / 128 / 124, 2048 fp32 92 / 104 / 101; backwards, 256 / 512:
-// 97 / 106, 125 / 137, 95 / 102).  Where it is less, more (16384 x 2500 bf16 117 / 64 / 63, backwards 95 / 68).  So do
-// rows of a wave forwards, whose loads are not that long (16384 x 1024 bf16 24 / 22 / 21).  Backwards each workgroup
+// latency, and fewer streams of reads and writes take turns at the memory (16384 rows with residual, us, 256 / 4096
+// workgroups: 3504 bf16 87 / 91, 4096 91 / 99, 5120 118 / 123, 1752 fp32 85 / 91, 2048 91 / 99; backwards, 256 / 512:
+// 85 / 89, 98 / 106, 125 / 137, 84 / 86, 96 / 102).  Where it is less, more (2560 bf16 77 / 63, backwards 72 / 66).  So do
+// rows of a wave forwards, whose loads are not that long (16384 x 1024 bf16 24 / 21).  Backwards each workgroup
 // has its line of partial sums, and the gradients' two streams, which are always there, are counted.
+// An fp32 row that ends inside a vector has twice the vectors of a bf16 row to put right, which one workgroup a CU of up
+// to 256 threads does not cover (16384 rows, 256 / 4096: 2049 269 / 113, 3001 332 / 159, 4095 391 / 208; 2048 x 8190
+// 57 / 48; backwards, 256 / 512: 513 76 / 49, 1001 113 / 70, 2049 326 / 192, 4093 442 / 268; 8192 x 4097 184 / 187).
+// Such a bf16 row is alike both ways (4097 129 / 121, 8191 without residual 122 / 119, 2048 x 4099 16 / 18; backwards
+// 143 / 146, 188 / 198, 21 / 27).
 template <class T>
 int rms_blocks(const RmsArgs& A) {
+  if (T::kBytes == 4 && A.d % T::W != 0) return 4096;
   return A.d > 1024 && A.d * T::kBytes * (A.residual != nullptr ? 2 : 1) >= 16384 ? 256 : 4096;
 }
-inline int most_lines(int64_t d, bool f32) { return d * (f32 ? 4 : 2) * (d <= 1024 ? 4 : 1) >= 8192 ? 256 : 512; }
+inline int most_lines(int64_t d, bool f32) {
+  if (f32 && d % 4 != 0 && d <= 4096) return 512;
+  return d * (f32 ? 4 : 2) * (d <= 1024 ? 4 : 1) >= 8192 ? 256 : 512;
+}
 constexpr int kRmsWideBlocks = 2048;
 
 template <class T, int NT, int E>
