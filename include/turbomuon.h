@@ -316,7 +316,7 @@ tm_status tm_rms_norm_backward(const void* dy, int64_t lddy, const void* s, int6
  *   active   one byte per row, or NULL: rows of 0 take no part; they are not read,
  *            their choices and slots are -1, their weights 0.
  *   experts 1..TM_MAX_EXPERTS, top 1..min(experts, TM_MAX_TOP), rows top at most
- *   TM_MAX_ROWS.  A row of nothing but -inf, or with NaN, has weights of NaN, and so is
+ *   TM_MAX_ROWS.  A row of nothing but -inf, or with inf or NaN, has weights of NaN, and so is
  *   the balance; its choices are experts all the same.
  */
 tm_status tm_expert_route(const void* logits, int64_t ld, const uint8_t* active, int renormalize, float scale,
@@ -340,7 +340,7 @@ tm_status tm_expert_route_backward(const void* logits, int64_t ld, const int32_t
  * tm_expert_gather - out[slots[i, j], :] = x[i, :].
  *   x      rows x d;  out  count x d, of the same type.
  *   slots  rows x top.  A slot that is negative, or not below *used, is none.  No two
- *          may be the same: their row would hold either.
+ *          may be the same: their row would hold parts of both.
  *   used   device int32: rows of `out` that are filled (tm_expert_route's last entry of
  *          ends), or NULL: all.  Rows from there on come out as zeros; one below it
  *          that no slot names is left as it was.
@@ -432,7 +432,7 @@ tm_status tm_expert_wgrad(const void* x, int64_t ldx, const void* dy, int64_t ld
  *   targets  int64 per row.  A negative target takes its row out: zeros, places of -1,
  *            its logits are not read; one of vocab or more makes its logp NaN.
  *   top      0..min(vocab, TM_MAX_TOP); with 0 top_logp and top_ids may be NULL.
- * A row of nothing but -inf, or with NaN, gives NaN.
+ * A row of nothing but -inf, or with inf or NaN, gives NaN.
  */
 tm_status tm_token_logp(const void* logits, int64_t ld, const int64_t* targets, float temperature, float* logp,
                         float* entropy, float* stats, int64_t top, float* top_logp, int64_t* top_ids,

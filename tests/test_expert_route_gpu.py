@@ -334,3 +334,21 @@ def test_many_rows_and_many_experts(rows, experts, top, run, dtype):
     back = tm.expert_route_backward(logits, got[0], got[3], dw, db)
     assert not back[~active].any()
     _check_gradient(back, clean, got[0], got[3], dw, db, True, 1.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,experts", [(20, 8), (300, 60), (150, 300), (90, 1500)])
+def test_plus_infinity(rows, experts, dtype):
+    """It is chosen first and its row's weights are not a number; the other rows are as without it."""
+    log(f"case: route, +inf in {rows} x {experts} {dtype}")
+    logits = _logits(rows, experts, dtype, seed=5)
+    logits[3, experts - 2] = float("inf")
+    logits[7, 1] = logits[7, 4] = float("inf")
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[3] = rest[7] = False
+    chosen, weights, slots, ends, balance = tm.expert_route(logits, 3)
+    want = _exact(logits, 3, None, True, 1.0)
+    assert torch.equal(chosen, want[0].int()) and torch.equal(slots, want[2].int()) and torch.equal(ends, want[3].int())
+    assert weights[~rest].isnan().all() and balance.isnan()
+    P = _tolerance(logits[rest], rows)
+    close("weights", weights[rest], want[1][rest], 2 * P * want[1][rest].abs() + 1e-37)

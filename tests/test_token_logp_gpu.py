@@ -287,3 +287,23 @@ def test_no_rows_and_refusals():
         assert e.value.status == tm.TM_ERR_INVALID_ARG
     with pytest.raises(tm.TurboMuonError):
         tm.token_logp(s["logits"][:, :5].contiguous(), s["targets"], 6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [30, 1500, 9000, 60000, 300000])
+def test_plus_infinity(vocab, dtype):
+    """A row with it gives NaN, the place itself is found; the other rows are as without it."""
+    log(f"case: log probabilities, +inf among {vocab} {dtype}")
+    logits = torch.randn((6, vocab), generator=generator(40), device="cuda").to(DT[dtype])
+    targets = torch.randint(vocab, (6,), generator=generator(41), device="cuda")
+    clean = tm.token_logp(logits, targets, 4)
+    logits[2, vocab - 3] = float("inf")
+    logits[4, 5] = logits[4, vocab // 2] = float("inf")
+    got = tm.token_logp(logits, targets, 4)
+    rest = torch.tensor([0, 1, 3, 5], device="cuda")
+    assert all(torch.equal(a[rest], b[rest]) for a, b in zip(got, clean))
+    for r in (2, 4):
+        assert got[0][r].isnan() and got[1][r].isnan() and got[3][r].isnan().all()
+    assert int(got[4][2, 0]) == vocab - 3 and got[4][4, :2].tolist() == [5, vocab // 2]
+    back = tm.token_logp_backward(logits, targets, got[2], got[1], torch.ones(6, device="cuda"))
+    assert back[rest].isfinite().all() and back[2].isnan().any() and back[4].isnan().any()
