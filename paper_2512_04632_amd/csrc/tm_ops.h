@@ -103,8 +103,8 @@ struct RouteArgs {
   float* weights;
   int32_t* ends;          // experts
   float* balance;
-  uint16_t* counts;       // workspace: choices of each expert in each block of rows, [blocks][experts]
-  float* shares;          // workspace: sums of its probabilities there, [blocks][experts]
+  uint16_t* counts;       // workspace: choices of each expert in each block of rows, [blocks][experts up to a multiple of 8]
+  float* shares;          // workspace: sums of its probabilities there, laid out the same
   double* dots;           // workspace: parts of the balance loss, one for a block or for several
   int32_t* arrived;       // workspace: how many of them are there
   int64_t ld;

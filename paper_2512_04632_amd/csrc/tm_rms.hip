@@ -98,7 +98,8 @@ __global__ __launch_bounds__(block_threads<NT>()) void k_rms(const RmsArgs A) {
 // Backward: dy, s and dsum are read once, ds is written once.  16384 x 4096 bf16 with
 // dsum 95 us for 537 MB, 5.7 TB/s, and 5 us to add up the 256 lines of partial sums;
 // 2048 x 8190 fp32 70 us for 268 MB, 3.8 TB/s: a row whose width is no whole number of
-// vectors needs registers of its own for its end.
+// vectors needs registers of its own for its end.  fp32 rows of more than 8192 with dsum keep 8 to 10
+// registers a lane in memory.
 template <class T, int NT, int E, bool TAIL, bool ADD>
 __global__ __launch_bounds__(block_threads<NT>()) void k_rms_backward(const RmsArgs A) {
   constexpr int W = T::W, V = E / W, RB = block_threads<NT>() / NT, NW = NT > 64 ? NT / 64 : 1;

@@ -17,9 +17,14 @@
 // and the loss at once.  Else a second launch adds up the blocks' counts (16 bits each) and moves every choice by what lies
 // before its block.  Sums of probabilities are fp32 over a block's rows, 64-bit over the blocks, in a fixed order.
 //
-// Bound by instructions and by latency, not by memory: 32768 x 256 fp32, 8 chosen, reads 34 MB and writes 3 (7 us at the
-// rate of a copy) and takes 27 us, 17 of it the choices (about 22 instructions for each score, 18 of them the rounds) and
-// 10 the second launch, whose steps wait for one another.  64 rows x 8 take 11 us of the host for 6 of the kernel.
+// Bound by instructions and by latency, not by memory: 32768 x 256 fp32, 8 chosen, has 34 MB to read and 3 to write (7 us at
+// the rate of a copy) and takes 27 us, 18 of it the choices and 10 the second launch, whose steps wait for one another.
+// The choices take 53 vector instructions for each score of 256: 18 the nine rounds, 6 the keys, the others exponentials and
+// sums, the end of each row (the chosen's shares, their marks) and of the block.  The rows of 129 to 1024 experts
+// stand at the 128 registers of four waves a SIMD, 2 to 4 of them kept in memory (3 of the 7 MB that the choices write).
+// 64 rows x 8 take 10 us of the host for 6 of the kernel.  65 to some 2000 rows are a few workgroups, each with four
+// rows or more to a group one after the other, and the second launch: 100 x 384 22 us, 17 and 6 in the kernels; 1000 x 512
+// 23, 17 and 7; 512 x 64 14, 7 and 7.
 #include <algorithm>
 
 #include "tm_elem.h"
@@ -157,7 +162,9 @@ __device__ inline void pick_exact(const char* row, int t, int experts, int top, 
 // is least below the last: one subtraction and half a minimum for each value.  Not for rows with NaN.  A bf16 value has its 16 bits beside a place of 16.  Of an fp32 value the last bits make way for
 // the place: one key more is taken, and where two neighbours in the list are the same in what is left, keys are taken
 // until the list's end is clear and its entries ranked by their whole values (256 scores: one row in 200).  Rows whose
-// list would pass the L lanes are picked exactly: many of the same value, all of them for a router that starts at zero.
+// list would pass the L lanes are picked exactly: many of the same value, all of them for a router that starts at zero, and
+// all fp32 rows with as many choices as lanes or more: 16 of up to 256 experts, 32 of up to 512, 64 of up to 1024 (32768 x
+// 256, 15 and 16 of fp32 49 and 83 us, of bf16 29 each).
 template <class T, int L, int J>
 struct Keys {
   static constexpr int N = Held<T, L, J>::N;

@@ -6,11 +6,12 @@
 //   backward  dy[slot_ij] = w_ij dout_i (zeros past the filled rows),
 //             dw_ij = sum over the columns of dout_i y[slot_ij]
 //
-// Each goes by the rows i: a row is read once and written to its slots, or its slots are
+// Each goes by the rows i: a row is read and written to its slots, or its slots are
 // read and summed in the order of j, in fp32, and rounded once.  L threads have a row;
-// they go along it 16 bytes at a time.  A row's slots (and weights) are read once, by scalar loads
+// they go along it 16 bytes at a time.  Up to eight slots (and weights) of a row are read once, by scalar loads
 // where a wave or more has the row, and all of them are on the way together; what is read and
-// written is what the definition asks for.
+// written is what the definition asks for.  More go eight at a time: on the way out and backwards the row
+// itself is read again for each eight, on the way back the slots are, for every 16 bytes.
 //
 // All three are bound by HBM (us; bytes at the 5.04 TB/s of a large copy in brackets): rows of 16384 x 4096 bf16 to two
 // slots 68 to 76 (80, as the card writes faster than it copies), 8192 x 2048 bf16 joined from eight slots with residual 67
